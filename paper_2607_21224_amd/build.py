@@ -14,6 +14,8 @@ LIB_CPDP = os.path.join(PKG, "libcpdp.so")
 # the same sources with 256-thread blocks: a different launch shape for the
 # tests that check results do not depend on it
 LIB_CPDP_BLOCK256 = os.path.join(PKG, "libcpdp_block256.so")
+# the 8-bit activation path (include/cpdp_q8.h)
+LIB_Q8 = os.path.join(PKG, "libcpdp_q8.so")
 LIB_SYNTH = os.path.join(ROOT, "synth", "libsynth.so")
 
 # -ffp-contract=off: only the explicit fmaf calls fuse, so the arithmetic is
@@ -34,6 +36,9 @@ KERNEL_HEADERS = ("cpdp_device.h", "cpdp_sync_impl.h", "cpdp_split.h", "cpdp_dis
 HOST_SOURCES = ("cpdp_api.cpp",)
 # the library's own device memory (no kernels): the static plan table
 SCRATCH_SOURCES = ("plan_scratch.hip",)
+# libcpdp_q8.so: kernel translation units and the host validation layer
+Q8_SOURCES = ("q8_rows.hip", "q8_norm.hip", "q8_act.hip", "q8_matmul.hip", "q8_grad.hip",
+              "q8_api.cpp")
 OBJ_ROOT = os.path.join(ROOT, "_build")
 
 
@@ -43,12 +48,12 @@ def _run(cmd):
         raise RuntimeError("build failed:\n" + " ".join(cmd) + "\n" + r.stdout + r.stderr)
 
 
-def build_cpdp(out: str = LIB_CPDP, extra=()) -> str:
+def build_cpdp(out: str = LIB_CPDP, extra=(),
+               sources=KERNEL_SOURCES + HOST_SOURCES + SCRATCH_SOURCES) -> str:
     from concurrent.futures import ThreadPoolExecutor
     csrc = os.path.join(PKG, "csrc")
     objdir = os.path.join(OBJ_ROOT, os.path.basename(out) + ".objs")
     os.makedirs(objdir, exist_ok=True)
-    sources = KERNEL_SOURCES + HOST_SOURCES + SCRATCH_SOURCES
 
     def compile_one(name):
         obj = os.path.join(objdir, name + ".o")
@@ -62,6 +67,10 @@ def build_cpdp(out: str = LIB_CPDP, extra=()) -> str:
     _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs])
     os.replace(tmp, out)
     return out
+
+
+def build_q8(out: str = LIB_Q8) -> str:
+    return build_cpdp(out, sources=Q8_SOURCES)
 
 
 def build_synth(out: str = LIB_SYNTH) -> str:
@@ -86,8 +95,8 @@ def build_consumer(out: str = CONSUMER) -> str:
 
 def build_all() -> None:
     from concurrent.futures import ThreadPoolExecutor
-    with ThreadPoolExecutor(3) as ex:
-        jobs = [ex.submit(build_cpdp), ex.submit(build_synth),
+    with ThreadPoolExecutor(4) as ex:
+        jobs = [ex.submit(build_cpdp), ex.submit(build_q8), ex.submit(build_synth),
                 ex.submit(build_cpdp, LIB_CPDP_BLOCK256, ("-DCPDP_BLOCK=256",))]
         for j in jobs:
             j.result()

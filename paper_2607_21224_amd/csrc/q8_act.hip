@@ -1,0 +1,232 @@
+// Activations with 8-bit output and 8-bit checkpoint, and their backward pass
+// from the checkpoint.
+#include "q8_device.h"
+
+namespace cpdp {
+namespace q8 {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kSqrtHalf = 0.70710678118654752f;
+constexpr float kInvSqrt2Pi = 0.39894228040143268f;
+
+// e^x and 1 / x by the hardware's instructions, each good to one unit in the
+// last place; e^x also takes the rounding of x log2(e), |x| 2^-24 relative.
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float sigmoid(float x) {
+    return __builtin_amdgcn_rcpf(1.0f + fast_exp(-x));
+}
+__device__ __forceinline__ float normal_cdf(float x) {
+    return 0.5f * (1.0f + erff(x * kSqrtHalf));
+}
+
+template <Act K>
+__device__ __forceinline__ float activation(float g, float u) {
+    if constexpr (K == Act::GELU) return g * normal_cdf(g);
+    else return g * sigmoid(g) * u;
+}
+
+// Bound by HBM: 6 bytes an element for GELU with bf16 values written, 9 for the
+// gated one (bf16 inputs); the inputs and the result of a row are held until
+// their three scales are known.
+template <Act K, class E, class Y, int TPR, int CH>
+__global__ __launch_bounds__(block_of(TPR)) void act_kernel(
+    const typename E::T* g, const typename E::T* u, int64_t ldg, int64_t T, int F, int8_t* q,
+    int64_t ldq, float* scale, typename Y::T* y, int64_t ldy, int8_t* cg, float* cg_scale,
+    int8_t* cu, float* cu_scale, int64_t ldc) {
+    constexpr bool kGated = K == Act::SWIGLU;
+    constexpr int kTops = kGated ? 3 : 2;
+    __shared__ RowWords<TPR, kTops> words;
+    const int64_t row = (int64_t)blockIdx.x * rows_of(TPR) + (int)threadIdx.x / TPR;
+    const int lane = (int)threadIdx.x % TPR;
+    if (row >= T) return;  // a whole wavefront, in the one-wavefront form only
+    float gv[CH][kPiece], uv[kGated ? CH : 1][kPiece], a[CH][kPiece], none;
+    uint32_t top[kTops] = {};
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int c = (j * TPR + lane) * kPiece;
+        if (c < F) {
+            load8(g + row * ldg + c, F - c, gv[j]);
+            if constexpr (kGated) load8(u + row * ldg + c, F - c, uv[j]);
+#pragma unroll
+            for (int k = 0; k < kPiece; ++k) {
+                a[j][k] = activation<K>(gv[j][k], kGated ? uv[kGated ? j : 0][k] : 0.0f);
+                top[0] = max(top[0], magnitude(a[j][k]));
+                top[1] = max(top[1], magnitude(gv[j][k]));
+                if constexpr (kGated) top[2] = max(top[2], magnitude(uv[j][k]));
+            }
+        }
+    }
+    row_reduce<TPR, false, kTops>(none, top, words);
+    RowScale r[kTops];
+#pragma unroll
+    for (int i = 0; i < kTops; ++i) r[i] = row_scale(__uint_as_float(top[i]));
+    if (lane == 0) {
+        scale[row] = r[0].s;
+        if (cg != nullptr) cg_scale[row] = r[1].s;
+        if constexpr (kGated)
+            if (cu != nullptr) cu_scale[row] = r[2].s;
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int c = (j * TPR + lane) * kPiece;
+        if (c < F) {
+            write_piece<Y>(a[j], r[0], q + row * ldq + c, y == nullptr ? y : y + row * ldy + c,
+                           F - c);
+            if (cg != nullptr) write_piece<F32>(gv[j], r[1], cg + row * ldc + c, nullptr, F - c);
+            if constexpr (kGated)
+                if (cu != nullptr)
+                    write_piece<F32>(uv[j], r[2], cu + row * ldc + c, nullptr, F - c);
+        }
+    }
+}
+
+// A row too long to be held: its inputs are read again.
+template <Act K, class E, class Y>
+__global__ __launch_bounds__(1024) void act_long_kernel(
+    const typename E::T* g, const typename E::T* u, int64_t ldg, int F, int8_t* q, int64_t ldq,
+    float* scale, typename Y::T* y, int64_t ldy, int8_t* cg, float* cg_scale, int8_t* cu,
+    float* cu_scale, int64_t ldc) {
+    constexpr bool kGated = K == Act::SWIGLU;
+    __shared__ RowWords<1024, 3> words;
+    const int64_t row = blockIdx.x;
+    float gv[kPiece], uv[kPiece] = {}, a[kPiece], none;
+    uint32_t top[3] = {};
+    for (int c = (int)threadIdx.x * kPiece; c < F; c += 1024 * kPiece) {
+        load8(g + row * ldg + c, F - c, gv);
+        if constexpr (kGated) load8(u + row * ldg + c, F - c, uv);
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) {
+            top[0] = max(top[0], magnitude(activation<K>(gv[k], uv[k])));
+            top[1] = max(top[1], magnitude(gv[k]));
+            top[2] = max(top[2], magnitude(uv[k]));
+        }
+    }
+    row_reduce<1024, false, 3>(none, top, words);
+    RowScale r[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) r[i] = row_scale(__uint_as_float(top[i]));
+    if (threadIdx.x == 0) {
+        scale[row] = r[0].s;
+        if (cg != nullptr) cg_scale[row] = r[1].s;
+        if (kGated && cu != nullptr) cu_scale[row] = r[2].s;
+    }
+    for (int c = (int)threadIdx.x * kPiece; c < F; c += 1024 * kPiece) {
+        load8(g + row * ldg + c, F - c, gv);
+        if constexpr (kGated) load8(u + row * ldg + c, F - c, uv);
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) a[k] = activation<K>(gv[k], uv[k]);
+        write_piece<Y>(a, r[0], q + row * ldq + c, y == nullptr ? y : y + row * ldy + c, F - c);
+        if (cg != nullptr) write_piece<F32>(gv, r[1], cg + row * ldc + c, nullptr, F - c);
+        if (kGated && cu != nullptr)
+            write_piece<F32>(uv, r[2], cu + row * ldc + c, nullptr, F - c);
+    }
+}
+
+template <Act K, class E, class Y>
+int act_typed(Mat g, Mat u, int64_t T, int F, Held out, Mat y, Held cg, Held cu, void* stream) {
+    using ET = typename E::T;
+    using YT = typename Y::T;
+    return with_row_shape(T, F, [&](auto tpr, auto ch) {
+        return in_parts(T, 1024, [&](int64_t t, int64_t n) {
+            const ET* gt = static_cast<const ET*>(g.p) + t * g.ld;
+            const ET* ut = u.p == nullptr ? nullptr : static_cast<const ET*>(u.p) + t * u.ld;
+            YT* yt = y.p == nullptr ? nullptr : static_cast<YT*>(y.p) + t * y.ld;
+            int8_t* cgt = cg.q == nullptr ? nullptr : cg.q + t * cg.ld;
+            int8_t* cut = cu.q == nullptr ? nullptr : cu.q + t * cu.ld;
+            float* cgs = cg.q == nullptr ? nullptr : cg.scale + t;
+            float* cus = cu.q == nullptr ? nullptr : cu.scale + t;
+            if constexpr (tpr == 0)
+                return launch(act_long_kernel<K, E, Y>, dim3((uint32_t)n), 1024, stream, gt, ut,
+                              g.ld, F, out.q + t * out.ld, out.ld, out.scale + t, yt, y.ld, cgt,
+                              cgs, cut, cus, cg.ld);
+            else
+                return launch(act_kernel<K, E, Y, tpr, ch>,
+                              dim3((uint32_t)((n + rows_of(tpr) - 1) / rows_of(tpr))),
+                              block_of(tpr), stream, gt, ut, g.ld, n, F, out.q + t * out.ld, out.ld,
+                              out.scale + t, yt, y.ld, cgt, cgs, cut, cus, cg.ld);
+        });
+    });
+}
+
+template <Act K>
+int act_kind(Mat g, Mat u, int64_t T, int F, Held out, Mat y, Held cg, Held cu, void* stream) {
+    if (g.bf16)
+        return y.bf16 ? act_typed<K, BF16, BF16>(g, u, T, F, out, y, cg, cu, stream)
+                      : act_typed<K, BF16, F32>(g, u, T, F, out, y, cg, cu, stream);
+    return y.bf16 ? act_typed<K, F32, BF16>(g, u, T, F, out, y, cg, cu, stream)
+                  : act_typed<K, F32, F32>(g, u, T, F, out, y, cg, cu, stream);
+}
+
+// Bound by HBM: 5 bytes an element for GELU, 8 for the gated one (bf16).  One
+// piece a thread; a block covers 4 rows of 64 pieces.
+template <Act K, class E>
+__global__ __launch_bounds__(256) void act_bwd_kernel(const typename E::T* da, int64_t ldda,
+                                                      const int8_t* cg, const float* cg_scale,
+                                                      const int8_t* cu, const float* cu_scale,
+                                                      int64_t ldc, int64_t T, int F,
+                                                      int blocks_across, typename E::T* dg,
+                                                      typename E::T* du, int64_t lddg) {
+    const int64_t row = (int64_t)(blockIdx.x / blocks_across) * 4 + (threadIdx.x >> 6);
+    const int c = ((int)(blockIdx.x % blocks_across) * 64 + (int)(threadIdx.x & 63)) * kPiece;
+    if (row >= T || c >= F) return;
+    const int n = F - c;
+    float d[kPiece], G[kPiece], U[kPiece];
+    load8(da + row * ldda + c, n, d);
+    load8(cg + row * ldc + c, n, G);
+    const float sg = cg_scale[row];
+    if constexpr (K == Act::GELU) {
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) {
+            const float x = G[k] * sg;
+            const float pdf = fast_exp(-0.5f * x * x) * kInvSqrt2Pi;
+            G[k] = d[k] * fmaf(x, pdf, normal_cdf(x));
+        }
+    } else {
+        load8(cu + row * ldc + c, n, U);
+        const float su = cu_scale[row];
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) {
+            const float x = G[k] * sg, s = sigmoid(x);
+            G[k] = d[k] * (U[k] * su) * s * fmaf(x, 1.0f - s, 1.0f);
+            U[k] = d[k] * x * s;
+        }
+        store8(du + row * lddg + c, n, U);
+    }
+    store8(dg + row * lddg + c, n, G);
+}
+
+template <Act K, class E>
+int act_bwd_typed(Mat da, Held cg, Held cu, int64_t T, int F, Mat dg, Mat du, void* stream) {
+    using ET = typename E::T;
+    const int64_t across = (F + 64 * kPiece - 1) / (64 * kPiece);
+    return in_parts(T, across * 64, [&](int64_t t, int64_t n) {
+        return launch(act_bwd_kernel<K, E>, dim3((uint32_t)((n + 3) / 4 * across)), 256, stream,
+                      static_cast<const ET*>(da.p) + t * da.ld, da.ld, cg.q + t * cg.ld,
+                      cg.scale + t, cu.q == nullptr ? cu.q : cu.q + t * cu.ld,
+                      cu.q == nullptr ? cu.scale : cu.scale + t, cg.ld, n, F, (int)across,
+                      static_cast<ET*>(dg.p) + t * dg.ld,
+                      du.p == nullptr ? nullptr : static_cast<ET*>(du.p) + t * du.ld, dg.ld);
+    });
+}
+
+}  // namespace
+
+int launch_act(Act kind, Mat g, Mat u, int64_t T, int64_t F, Held out, Mat y, Held cg, Held cu,
+               void* stream) {
+    return kind == Act::GELU ? act_kind<Act::GELU>(g, u, T, (int)F, out, y, cg, cu, stream)
+                             : act_kind<Act::SWIGLU>(g, u, T, (int)F, out, y, cg, cu, stream);
+}
+
+int launch_act_bwd(Act kind, Mat da, Held cg, Held cu, int64_t T, int64_t F, Mat dg, Mat du,
+                   void* stream) {
+    const int f = (int)F;
+    if (kind == Act::GELU)
+        return da.bf16 ? act_bwd_typed<Act::GELU, BF16>(da, cg, cu, T, f, dg, du, stream)
+                       : act_bwd_typed<Act::GELU, F32>(da, cg, cu, T, f, dg, du, stream);
+    return da.bf16 ? act_bwd_typed<Act::SWIGLU, BF16>(da, cg, cu, T, f, dg, du, stream)
+                   : act_bwd_typed<Act::SWIGLU, F32>(da, cg, cu, T, f, dg, du, stream);
+}
+
+}  // namespace q8
+}  // namespace cpdp

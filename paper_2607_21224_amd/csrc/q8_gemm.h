@@ -1,0 +1,392 @@
+// Matrix products C[M x N] = A[M x K] B[N x K]^T on the matrix cores, both
+// operands with K contiguous: int8 with 32-bit integer sums, or bf16 with fp32
+// sums.
+//
+// A block computes a BM x BN tile of C with WM x WN wavefronts.  It walks K in
+// steps of 128 bytes a row; the step's rows of A and B go from memory straight
+// into one of two LDS buffers (16 bytes a lane, no registers in between) while
+// the matrix cores work on the other.  The 16-byte pieces of a row are stored
+// permuted (piece p of row r at place p ^ f(r)), so that the 16 lanes that read
+// the same piece of 16 rows touch all 64 banks.  The permutation is applied to
+// the address that a lane loads from; a row's 128 bytes stay one request.
+//
+// The 16 x 16 instructions take the rows of B as their first operand, in an
+// order that leaves each lane with 4 NT consecutive columns of one row of C:
+// row r of instruction tile j is column (r / 4) 4 NT + 4 j + r % 4 of the
+// wavefront's 16 NT.  Stores are then 16 bytes and more a lane.
+#pragma once
+
+#include "q8_device.h"
+
+namespace cpdp {
+namespace q8 {
+namespace {
+
+constexpr int kStep = 128;  // bytes of a row in one step
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// The matrix-core instruction of an operand type, its sums and their type.
+struct Int8 {
+    using Acc = i32x4;
+    using Sum = int32_t;
+    static constexpr int kBytes = 1;
+    static __device__ __forceinline__ Acc mfma(u32x4 a, u32x4 b, Acc c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a),
+                                                     __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+    }
+};
+struct Bf16 {
+    using Acc = f32x4;
+    using Sum = float;
+    static constexpr int kBytes = 2;
+    static __device__ __forceinline__ Acc mfma(u32x4 a, u32x4 b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                       __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+
+// Operands of a product.  K runs over `parts` passes of `row` bytes each (row a
+// multiple of kStep where parts > 1); pass p reads A at a + p a_part and the same B.
+struct Operands {
+    const char* a;
+    const char* b;
+    int64_t lda, ldb;  // bytes from row to row, below 2^23
+    int64_t a_part;
+    int64_t M, N;
+    int row;    // bytes of a row that are there
+    int parts;
+};
+
+// Where the sums of a product go: C in its own type, or (slices > 1) the sums of
+// one slice of K as they are, at ws[slice][row][column].
+struct Target {
+    void* c;
+    int64_t ldc;
+    bool bf16;
+    const float* row_scale;  // of the rows and columns of C, or null
+    const float* col_scale;
+    void* ws;
+    int64_t ldws, slice;  // elements
+};
+
+__device__ __forceinline__ void to_lds(const char* src, char* dst) {
+    __builtin_amdgcn_global_load_lds(
+        (__attribute__((address_space(1))) void*)(src),
+        (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
+}
+
+// 16 bytes at p, of which the first n exist (n may be negative)
+template <int BYTES>
+__device__ __forceinline__ u32x4 load_tail(const char* p, int n) {
+    if (n >= 16) return *reinterpret_cast<const u32x4*>(p);
+    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; i += BYTES)
+        if (i < n) {
+            uint32_t e;
+            if constexpr (BYTES == 1) e = *reinterpret_cast<const uint8_t*>(p + i);
+            else e = *reinterpret_cast<const uint16_t*>(p + i);
+            v[i / 4] |= e << (8 * (i % 4));
+        }
+    return v;
+}
+
+// n (at most COLS) consecutive results of one row
+template <int COLS>
+__device__ __forceinline__ void store_cols(const Target& t, int64_t m, int64_t n0, int n,
+                                           const float (&v)[COLS]) {
+    static_assert(COLS % 8 == 0 || COLS == 4, "whole pieces");
+    if (t.bf16) {
+        uint16_t* p = static_cast<uint16_t*>(t.c) + m * t.ldc + n0;
+        if (n >= COLS) {
+#pragma unroll
+            for (int k = 0; k < COLS; k += 4)
+                *reinterpret_cast<u32x2*>(p + k) =
+                    u32x2{narrow2(v[k], v[k + 1]), narrow2(v[k + 2], v[k + 3])};
+        } else {
+#pragma unroll
+            for (int k = 0; k < COLS; ++k)
+                if (k < n) narrow(v[k], p + k);
+        }
+    } else {
+        float* p = static_cast<float*>(t.c) + m * t.ldc + n0;
+        if (n >= COLS) {
+#pragma unroll
+            for (int k = 0; k < COLS; k += 4)
+                *reinterpret_cast<f32x4*>(p + k) = f32x4{v[k], v[k + 1], v[k + 2], v[k + 3]};
+        } else {
+#pragma unroll
+            for (int k = 0; k < COLS; ++k)
+                if (k < n) p[k] = v[k];
+        }
+    }
+}
+
+// The tile of a block.  Blocks are dealt to the 8 XCDs in turn; each XCD takes a
+// run of consecutive tiles, and those go down 8 rows of tiles before the next
+// column, so that the tiles an XCD works on share rows of A and B in its L2.
+struct TileAt {
+    int64_t m, n;
+    int slice;
+};
+__device__ __forceinline__ TileAt tile_at(int64_t tiles_m, int64_t tiles_n, int BM, int BN) {
+    const int64_t tiles = tiles_m * tiles_n;
+    const int64_t b = blockIdx.x, slice = b / tiles;
+    int64_t t = b % tiles;
+    const int64_t each = tiles / 8, rest = tiles % 8, xcd = t % 8;
+    t = xcd * each + (xcd < rest ? xcd : rest) + t / 8;
+    const int64_t band = t / (8 * tiles_n);
+    const int64_t high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+    const int64_t in = t - band * 8 * tiles_n;
+    return {(band * 8 + in % high) * BM, in / high * BN, (int)slice};
+}
+
+template <class Op, int BM, int BN, int WM, int WN>
+struct Gemm {
+    static constexpr int kWaves = WM * WN;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
+    static constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;
+    static constexpr int kBuffer = (BM + BN) * kStep;
+    static_assert(kLoadsA * 8 * kWaves == BM && kLoadsB * 8 * kWaves == BN, "whole loads");
+
+    static __device__ __forceinline__ int place_a(int row) { return (row >> 1) & 7; }
+    static __device__ __forceinline__ int place_b(int row) {
+        return ((row >> 1) & 1) | ((row / (4 * NT) & 3) << 1);
+    }
+
+    // 32-bit offsets of a lane's loads from the tile's first row; rows past the
+    // matrix take its last one (their sums are not stored)
+    struct Loads {
+        uint32_t a[kLoadsA], b[kLoadsB];
+    };
+    static __device__ __forceinline__ Loads loads(const Operands& o, int64_t m0, int64_t n0,
+                                                  int wave, int lane) {
+        Loads l;
+#pragma unroll
+        for (int j = 0; j < kLoadsA; ++j) {
+            const int row = (j * kWaves + wave) * 8 + (lane >> 3);
+            const int64_t at = m0 + row < o.M ? row : o.M - 1 - m0;
+            l.a[j] = (uint32_t)(at * o.lda) + (((lane & 7) ^ place_a(row)) << 4);
+        }
+#pragma unroll
+        for (int j = 0; j < kLoadsB; ++j) {
+            const int row = (j * kWaves + wave) * 8 + (lane >> 3);
+            const int64_t at = n0 + row < o.N ? row : o.N - 1 - n0;
+            l.b[j] = (uint32_t)(at * o.ldb) + (((lane & 7) ^ place_b(row)) << 4);
+        }
+        return l;
+    }
+
+    static __device__ __forceinline__ void fetch(const char* a, const char* b, const Loads& l,
+                                                 char* lds, int wave) {
+#pragma unroll
+        for (int j = 0; j < kLoadsA; ++j) to_lds(a + l.a[j], lds + (j * kWaves + wave) * 1024);
+#pragma unroll
+        for (int j = 0; j < kLoadsB; ++j)
+            to_lds(b + l.b[j], lds + BM * kStep + (j * kWaves + wave) * 1024);
+    }
+
+    // the last, short step of a row: through registers, zeros past the end
+    static __device__ __forceinline__ void fetch_tail(const char* a, const char* b, const Loads& l,
+                                                      char* lds, int wave, int lane, int bytes) {
+        const int at = lane << 4;
+#pragma unroll
+        for (int j = 0; j < kLoadsA; ++j) {
+            const int row = (j * kWaves + wave) * 8 + (lane >> 3);
+            const int k = ((lane & 7) ^ place_a(row)) << 4;
+            *reinterpret_cast<u32x4*>(lds + (j * kWaves + wave) * 1024 + at) =
+                load_tail<Op::kBytes>(a + l.a[j], bytes - k);
+        }
+#pragma unroll
+        for (int j = 0; j < kLoadsB; ++j) {
+            const int row = (j * kWaves + wave) * 8 + (lane >> 3);
+            const int k = ((lane & 7) ^ place_b(row)) << 4;
+            *reinterpret_cast<u32x4*>(lds + BM * kStep + (j * kWaves + wave) * 1024 + at) =
+                load_tail<Op::kBytes>(b + l.b[j], bytes - k);
+        }
+    }
+
+    static __device__ __forceinline__ void compute(const char* at_a, const char* at_b, int ka,
+                                                   int kb, typename Op::Acc (&acc)[MT][NT]) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            u32x4 a[MT], b[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                b[j] = *reinterpret_cast<const u32x4*>(at_b + j * 4 * kStep + (kb ^ (half << 6)));
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                a[i] = *reinterpret_cast<const u32x4*>(at_a + i * 16 * kStep + (ka ^ (half << 6)));
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = Op::mfma(b[j], a[i], acc[i][j]);
+        }
+    }
+
+    static __device__ void run(const Operands& o, const Target& t, int64_t tiles_m,
+                               int64_t tiles_n, int slices) {
+        __shared__ __attribute__((aligned(1024))) char lds[2 * kBuffer];
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63;
+        const TileAt tile = tile_at(tiles_m, tiles_n, BM, BN);
+        const Loads l = loads(o, tile.m, tile.n, wave, lane);
+        const char* a0 = o.a + tile.m * o.lda;
+        const char* b0 = o.b + tile.n * o.ldb;
+
+        // whole steps of this slice: k0 to k1 of parts * per_part, and the short
+        // one at the end of the last slice
+        const int per_part = o.row / kStep, tail = o.row % kStep;
+        const int steps = per_part * o.parts;
+        const int k0 = (int)((int64_t)steps * tile.slice / slices);
+        const int k1 = (int)((int64_t)steps * (tile.slice + 1) / slices);
+        const auto a_at = [&](int k) {
+            return a0 + (k / per_part) * o.a_part + (int64_t)(k % per_part) * kStep;
+        };
+        const auto b_at = [&](int k) {
+            return b0 + (int64_t)(k % per_part) * kStep;
+        };
+
+        typename Op::Acc acc[MT][NT] = {};
+        const int wm = wave / WN, wn = wave % WN, r = lane & 15, g = lane >> 4;
+        const int off_a = (wm * MT * 16 + r) * kStep;
+        const int off_b = BM * kStep + (wn * NT * 16 + (r >> 2) * 4 * NT + (r & 3)) * kStep;
+        const int ka = (g ^ (r >> 1)) << 4, kb = ka;
+
+        if (k0 < k1) fetch(a_at(k0), b_at(k0), l, lds, wave);
+        for (int k = k0; k < k1; ++k) {
+            char* now = lds + ((k - k0) & 1) * kBuffer;
+            __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+            __syncthreads();
+            if (k + 1 < k1)
+                fetch(a_at(k + 1), b_at(k + 1), l, lds + ((k + 1 - k0) & 1) * kBuffer, wave);
+            compute(now + off_a, now + off_b, ka, kb, acc);
+        }
+        if (tail != 0 && tile.slice == slices - 1) {
+            // the buffer that the last whole step did not use
+            char* now = lds + ((k1 - k0) & 1) * kBuffer;
+            fetch_tail(a0 + (int64_t)per_part * kStep, b0 + (int64_t)per_part * kStep, l, now, wave,
+                       lane, tail);
+            __syncthreads();
+            compute(now + off_a, now + off_b, ka, kb, acc);
+        }
+
+        constexpr int COLS = 4 * NT;
+        const int64_t n0 = tile.n + wn * NT * 16 + g * COLS;
+        const int n = (int)(o.N - n0 < COLS ? o.N - n0 : COLS);
+        if (n <= 0) return;
+        float cs[COLS];
+        if (slices == 1 && t.col_scale != nullptr) {
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) cs[k] = t.col_scale[n0 + (k < n ? k : 0)];
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int64_t m = tile.m + (wm * MT + i) * 16 + r;
+            if (m >= o.M) continue;
+            if (slices > 1) {
+                auto* p = static_cast<typename Op::Sum*>(t.ws) + tile.slice * t.slice + m * t.ldws +
+                          n0;
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    *reinterpret_cast<typename Op::Acc*>(p + 4 * j) = acc[i][j];
+                continue;
+            }
+            float v[COLS];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[4 * j + k] = (float)acc[i][j][k];
+            if (t.row_scale != nullptr) {
+                const float rs = t.row_scale[m];
+#pragma unroll
+                for (int k = 0; k < COLS; ++k) v[k] = v[k] * rs * cs[k];
+            }
+            store_cols<COLS>(t, m, n0, n, v);
+        }
+    }
+};
+
+template <class Op, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(Operands o, Target t, int64_t tiles_m,
+                                                            int64_t tiles_n, int slices) {
+    Gemm<Op, BM, BN, WM, WN>::run(o, t, tiles_m, tiles_n, slices);
+}
+
+// Joins the slices of a product in their order: 4 columns a thread.
+template <class Op>
+__global__ __launch_bounds__(256) void join_kernel(Target t, int64_t M, int64_t N, int slices) {
+    const int64_t across = (N + 3) / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t m = i / across, n0 = i % across * 4;
+    if (m >= M) return;
+    const auto* p = static_cast<const typename Op::Sum*>(t.ws) + m * t.ldws + n0;
+    typename Op::Acc s = *reinterpret_cast<const typename Op::Acc*>(p);
+    for (int z = 1; z < slices; ++z)
+        s += *reinterpret_cast<const typename Op::Acc*>(p + z * t.slice);
+    const int n = (int)(N - n0 < 4 ? N - n0 : 4);
+    float v[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+    if (t.row_scale != nullptr) {
+        const float rs = t.row_scale[m];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = v[k] * rs * t.col_scale[n0 + (k < n ? k : 0)];
+    }
+    store_cols<4>(t, m, n0, n, v);
+}
+
+// ---- which tile takes a product ----------------------------------------------------
+
+struct Shape {
+    int tile;    // 256, 128 or 64
+    int slices;  // of K
+};
+
+inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The largest tile that gives each CU about one block; below that, 64 x 64 tiles
+// over slices of K.
+inline Shape shape_of(int64_t M, int64_t N, int64_t steps) {
+    if (up(M, 256) * up(N, 256) >= 192) return {256, 1};
+    if (up(M, 128) * up(N, 128) >= 192) return {128, 1};
+    const int64_t tiles = up(M, 64) * up(N, 64);
+    int64_t slices = 1;
+    while (tiles * slices < 512 && slices < 16 && steps / (2 * slices) >= 4) slices *= 2;
+    return {64, (int)slices};
+}
+
+// Workspace of a product's slices.
+inline int64_t slices_ld(int64_t N) { return up(N, 64) * 64; }
+inline int64_t slices_bytes(int64_t M, int64_t N, int64_t steps) {
+    const Shape s = shape_of(M, N, steps);
+    return s.slices == 1 ? 0 : s.slices * M * slices_ld(N) * 4;
+}
+
+template <class Op, int BM, int BN, int WM, int WN>
+int launch_tiles(const Operands& o, const Target& t, int slices, void* stream) {
+    const int64_t tm = up(o.M, BM), tn = up(o.N, BN);
+    // (work items of a launch stay below 2^32)
+    if (tm * tn * slices * 64 * WM * WN >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
+    return launch(gemm_kernel<Op, BM, BN, WM, WN>, dim3((uint32_t)(tm * tn * slices)),
+                  64 * WM * WN, stream, o, t, tm, tn, slices);
+}
+
+template <class Op>
+int launch_gemm(const Operands& o, Target t, void* ws, void* stream) {
+    const Shape s = shape_of(o.M, o.N, (int64_t)(o.row / kStep) * o.parts);
+    t.ws = ws;
+    t.ldws = slices_ld(o.N);
+    t.slice = o.M * t.ldws;
+    if (s.tile == 256) return launch_tiles<Op, 256, 256, 2, 4>(o, t, 1, stream);
+    if (s.tile == 128) return launch_tiles<Op, 128, 128, 2, 2>(o, t, 1, stream);
+    if (int e = launch_tiles<Op, 64, 64, 2, 2>(o, t, s.slices, stream)) return e;
+    if (s.slices == 1) return 0;
+    return launch(join_kernel<Op>, dim3((uint32_t)up(o.M * up(o.N, 4), 256)), 256, stream, t, o.M,
+                  o.N, s.slices);
+}
+
+}  // namespace
+}  // namespace q8
+}  // namespace cpdp
