@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import os
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -16,6 +17,8 @@ LIB_CPDP = os.path.join(PKG, "libcpdp.so")
 LIB_CPDP_BLOCK256 = os.path.join(PKG, "libcpdp_block256.so")
 # the 8-bit activation path (include/cpdp_q8.h)
 LIB_Q8 = os.path.join(PKG, "libcpdp_q8.so")
+# its Python extension (host code)
+EXT_Q8 = os.path.join(PKG, "_q8" + sysconfig.get_config_var("EXT_SUFFIX"))
 LIB_SYNTH = os.path.join(ROOT, "synth", "libsynth.so")
 
 # -ffp-contract=off: only the explicit fmaf calls fuse, so the arithmetic is
@@ -73,6 +76,25 @@ def build_q8(out: str = LIB_Q8) -> str:
     return build_cpdp(out, sources=Q8_SOURCES)
 
 
+def build_q8_extension(out: str = EXT_Q8) -> str:
+    """The Python extension that marshals the 8-bit path's arguments, linked to
+    libcpdp_q8.so beside it and to the torch libraries that torch has loaded."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    tmp = out + ".tmp"
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+          "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROOT, "include"),
+          "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(root, "include"),
+          "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+          "-isystem", os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include"),
+          "-o", tmp, os.path.join(PKG, "csrc", "q8_bind.cpp"), "-L", PKG, "-lcpdp_q8",
+          "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip",
+          "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, out)
+    return out
+
+
 def build_synth(out: str = LIB_SYNTH) -> str:
     tmp = out + ".tmp"
     _run([HIPCC, *HIP_FLAGS, "-o", tmp, os.path.join(ROOT, "synth", "synth.hip")])
@@ -101,6 +123,7 @@ def build_all() -> None:
         for j in jobs:
             j.result()
     build_consumer()
+    build_q8_extension()
 
 
 if __name__ == "__main__":
