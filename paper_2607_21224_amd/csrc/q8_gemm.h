@@ -77,6 +77,20 @@ __device__ __forceinline__ void to_lds(const char* src, char* dst) {
         (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
 }
 
+// Waits until at most N of the wavefront's loads are on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
+}
+// A barrier that waits for no load (the caller has waited for those it needs).
+__device__ __forceinline__ void barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // 16 bytes at p, of which the first n exist (n may be negative)
 template <int BYTES>
 __device__ __forceinline__ u32x4 load_tail(const char* p, int n) {
@@ -209,21 +223,36 @@ struct Gemm {
         }
     }
 
-    static __device__ __forceinline__ void compute(const char* at_a, const char* at_b, int ka,
-                                                   int kb, typename Op::Acc (&acc)[MT][NT]) {
+    // the operands of half a step: 64 bytes of the wavefront's rows
+    struct Half {
+        u32x4 a[MT], b[NT];
+    };
+    static __device__ __forceinline__ void read(Half& h, const char* at_a, const char* at_b,
+                                                int half, int swap) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            u32x4 a[MT], b[NT];
+        for (int j = 0; j < NT; ++j)
+            h.b[j] = *reinterpret_cast<const u32x4*>(at_b + j * 4 * kStep + (swap ^ (half << 6)));
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                b[j] = *reinterpret_cast<const u32x4*>(at_b + j * 4 * kStep + (kb ^ (half << 6)));
+        for (int i = 0; i < MT; ++i)
+            h.a[i] = *reinterpret_cast<const u32x4*>(at_a + i * 16 * kStep + (swap ^ (half << 6)));
+    }
+    static __device__ __forceinline__ void multiply(const Half& h,
+                                                    typename Op::Acc (&acc)[MT][NT]) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-                a[i] = *reinterpret_cast<const u32x4*>(at_a + i * 16 * kStep + (ka ^ (half << 6)));
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int j = 0; j < NT; ++j) acc[i][j] = Op::mfma(h.b[j], h.a[i], acc[i][j]);
+    }
+    // tells the scheduler to spread LOADS loads of a step to come and the reads of
+    // the next half over the matrix instructions of this one
+    template <int LOADS>
+    static __device__ __forceinline__ void spread() {
+        constexpr int kReads = MT + NT, kEach = MT * NT / kReads > 0 ? MT * NT / kReads : 1;
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = Op::mfma(b[j], a[i], acc[i][j]);
+        for (int i = 0; i < kReads; ++i) {
+            if (i < LOADS) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);  // a load
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                 // an LDS read
+            __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);             // multiplies
         }
     }
 
@@ -243,35 +272,72 @@ struct Gemm {
         const int steps = per_part * o.parts;
         const int k0 = (int)((int64_t)steps * tile.slice / slices);
         const int k1 = (int)((int64_t)steps * (tile.slice + 1) / slices);
-        const auto a_at = [&](int k) {
-            return a0 + (k / per_part) * o.a_part + (int64_t)(k % per_part) * kStep;
-        };
-        const auto b_at = [&](int k) {
-            return b0 + (int64_t)(k % per_part) * kStep;
-        };
 
         typename Op::Acc acc[MT][NT] = {};
         const int wm = wave / WN, wn = wave % WN, r = lane & 15, g = lane >> 4;
         const int off_a = (wm * MT * 16 + r) * kStep;
         const int off_b = BM * kStep + (wn * NT * 16 + (r >> 2) * 4 * NT + (r & 3)) * kStep;
-        const int ka = (g ^ (r >> 1)) << 4, kb = ka;
+        const int swap = (g ^ (r >> 1)) << 4;
 
-        if (k0 < k1) fetch(a_at(k0), b_at(k0), l, lds, wave);
-        for (int k = k0; k < k1; ++k) {
-            char* now = lds + ((k - k0) & 1) * kBuffer;
-            __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-            __syncthreads();
-            if (k + 1 < k1)
-                fetch(a_at(k + 1), b_at(k + 1), l, lds + ((k + 1 - k0) & 1) * kBuffer, wave);
-            compute(now + off_a, now + off_b, ka, kb, acc);
+        // Two steps are on their way or in LDS, and half a step in registers.  A
+        // step's first half is multiplied while its second is read; then, its LDS
+        // buffer done with, one barrier, and the step after next is sent for into
+        // that buffer while the second half is multiplied and the next step's
+        // first is read.
+        int part_at = k0 / (per_part > 0 ? per_part : 1), at = k0 - part_at * per_part;
+        const char* a_at = a0 + part_at * o.a_part + (int64_t)at * kStep;
+        const char* b_at = b0 + (int64_t)at * kStep;
+        const int64_t a_jump = o.a_part - o.row;
+        const auto next = [&] {
+            const bool wrap = ++at == per_part;
+            at = wrap ? 0 : at;
+            a_at += wrap ? kStep + a_jump : kStep;
+            b_at += wrap ? kStep - o.row : kStep;
+        };
+        Half h0, h1;
+        if (k0 < k1) {
+            fetch(a_at, b_at, l, lds, wave);
+            next();
+            if (k0 + 1 < k1) fetch(a_at, b_at, l, lds + kBuffer, wave);
+            next();
+            // the first of the two: the second one's loads may still be on their way
+            if (k0 + 1 < k1) wait_loads<kLoadsA + kLoadsB>();
+            else wait_loads<0>();
+            barrier();
+            read(h0, lds + off_a, lds + off_b, 0, swap);
         }
+        // one step; FETCH: there is a step after next, READ: there is a next one
+        const auto step = [&](int k, auto fetch_on, auto read_on) {
+            char* now = lds + ((k - k0) & 1) * kBuffer;
+            char* then = lds + ((k - k0 + 1) & 1) * kBuffer;
+            read(h1, now + off_a, now + off_b, 1, swap);
+            multiply(h0, acc);
+            spread<0>();
+            wait_loads<0>();
+            __syncthreads();
+            if constexpr (fetch_on) {
+                fetch(a_at, b_at, l, now, wave);
+                next();
+            }
+            if constexpr (read_on) read(h0, then + off_a, then + off_b, 0, swap);
+            multiply(h1, acc);
+            if constexpr (read_on) spread<fetch_on ? kLoadsA + kLoadsB : 0>();
+        };
+        int k = k0;
+        for (; k < k1 - 2; ++k) step(k, std::true_type(), std::true_type());
+        if (k < k1 - 1) step(k++, std::false_type(), std::true_type());
+        if (k < k1) step(k, std::false_type(), std::false_type());
         if (tail != 0 && tile.slice == slices - 1) {
-            // the buffer that the last whole step did not use
+            // no load is on its way, and all wavefronts are past their last read
+            // of both buffers but the last step's, whose reads the barrier follows
             char* now = lds + ((k1 - k0) & 1) * kBuffer;
             fetch_tail(a0 + (int64_t)per_part * kStep, b0 + (int64_t)per_part * kStep, l, now, wave,
                        lane, tail);
             __syncthreads();
-            compute(now + off_a, now + off_b, ka, kb, acc);
+            read(h0, now + off_a, now + off_b, 0, swap);
+            read(h1, now + off_a, now + off_b, 1, swap);
+            multiply(h0, acc);
+            multiply(h1, acc);
         }
 
         constexpr int COLS = 4 * NT;
