@@ -256,7 +256,7 @@ using Int = std::integral_constant<int, N>;
 
 template <class F>
 int with_row_shape(int64_t T, int64_t D, F f) {
-    const bool few = T < 1024;
+    const bool few = T < 4096;
     if (D <= 512) return f(Int<64>(), Int<1>());
     if (!few && D <= 1024) return f(Int<64>(), Int<2>());
     if (D <= 2048) return few ? f(Int<256>(), Int<1>()) : f(Int<64>(), Int<4>());

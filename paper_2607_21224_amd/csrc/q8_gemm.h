@@ -91,11 +91,20 @@ __device__ __forceinline__ void barrier() {
     asm volatile("" ::: "memory");
 }
 
-// 16 bytes at p, of which the first n exist (n may be negative)
+// 16 bytes at p, of which the first n exist (n may be negative) and `before` bytes
+// of the row come before p.  A piece that is cut short is read as the row's last
+// 16 bytes, shifted into place; a row shorter than that, element by element.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
 template <int BYTES>
-__device__ __forceinline__ u32x4 load_tail(const char* p, int n) {
+__device__ __forceinline__ u32x4 load_tail(const char* p, int n, int before) {
     if (n >= 16) return *reinterpret_cast<const u32x4*>(p);
     u32x4 v = {0, 0, 0, 0};
+    if (n <= 0) return v;
+    if (before + n >= 16) {
+        const u32x4 x = *reinterpret_cast<const u32x4_any*>(p + n - 16);
+        const unsigned __int128 all = __builtin_bit_cast(unsigned __int128, x);
+        return __builtin_bit_cast(u32x4, all >> (8 * (16 - n)));
+    }
 #pragma unroll
     for (int i = 0; i < 16; i += BYTES)
         if (i < n) {
@@ -205,21 +214,22 @@ struct Gemm {
 
     // the last, short step of a row: through registers, zeros past the end
     static __device__ __forceinline__ void fetch_tail(const char* a, const char* b, const Loads& l,
-                                                      char* lds, int wave, int lane, int bytes) {
+                                                      char* lds, int wave, int lane, int bytes,
+                                                      int before) {
         const int at = lane << 4;
 #pragma unroll
         for (int j = 0; j < kLoadsA; ++j) {
             const int row = (j * kWaves + wave) * 8 + (lane >> 3);
             const int k = ((lane & 7) ^ place_a(row)) << 4;
             *reinterpret_cast<u32x4*>(lds + (j * kWaves + wave) * 1024 + at) =
-                load_tail<Op::kBytes>(a + l.a[j], bytes - k);
+                load_tail<Op::kBytes>(a + l.a[j], bytes - k, before + k);
         }
 #pragma unroll
         for (int j = 0; j < kLoadsB; ++j) {
             const int row = (j * kWaves + wave) * 8 + (lane >> 3);
             const int k = ((lane & 7) ^ place_b(row)) << 4;
             *reinterpret_cast<u32x4*>(lds + BM * kStep + (j * kWaves + wave) * 1024 + at) =
-                load_tail<Op::kBytes>(b + l.b[j], bytes - k);
+                load_tail<Op::kBytes>(b + l.b[j], bytes - k, before + k);
         }
     }
 
@@ -332,7 +342,7 @@ struct Gemm {
             // of both buffers but the last step's, whose reads the barrier follows
             char* now = lds + ((k1 - k0) & 1) * kBuffer;
             fetch_tail(a0 + (int64_t)per_part * kStep, b0 + (int64_t)per_part * kStep, l, now, wave,
-                       lane, tail);
+                       lane, tail, per_part * kStep);
             __syncthreads();
             read(h0, now + off_a, now + off_b, 0, swap);
             read(h1, now + off_a, now + off_b, 1, swap);

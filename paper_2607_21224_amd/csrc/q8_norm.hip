@@ -254,22 +254,34 @@ __global__ __launch_bounds__(256) void norm_dw_kernel(const typename E::T* dy, i
     store8(parts + (int64_t)blockIdx.y * D + c, D - c, acc);
 }
 
-// dw <- the sum of `groups` parts: 64 columns a block, 16 threads a column.
+// dw <- the sum of `groups` parts: 32 columns a block, 32 threads a column, each
+// with 8 parts on their way at a time.
 template <class W>
 __global__ __launch_bounds__(1024) void norm_dw_join_kernel(const float* parts, int64_t groups,
                                                             int D, typename W::T* dw) {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ float sums[32][33];
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.0f;
-    if (c < D)
-        for (int64_t g = part; g < groups; g += 16) s += parts[g * D + c];
+    if (c < D) {
+        int64_t g = part;
+        for (; g + 7 * 32 < groups; g += 8 * 32) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = parts[(g + 32 * i) * D + c];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += v[i];
+        }
+        for (; g < groups; g += 32) s += parts[g * D + c];
+    }
     sums[part][lane] = s;
     __syncthreads();
-    if (part == 0 && c < D) {
-        for (int i = 1; i < 16; ++i) s += sums[i][lane];
-        narrow(s, dw + c);
-    }
+    // a wavefront's half takes a column: its 32 sums, added pairwise
+    s = sums[lane][part];
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor(s, off);
+    const int64_t col = (int64_t)blockIdx.x * 32 + part;
+    if (lane == 0 && col < D) narrow(s, dw + col);
 }
 
 // How the backward pass holds a row (it keeps three numbers a column, so fewer
@@ -284,10 +296,11 @@ int with_bwd_shape(int64_t D, F f) {
     return f(Int<0>(), Int<0>());
 }
 
-// Parts of dw: as many as keep the card busy, each of 8 rows at least.
+// Blocks of the backward pass, each with one part of dw a row it holds: two a CU,
+// and as many as there are rows for where they are fewer.
 int64_t bwd_blocks(int64_t T, int rows) {
-    const int64_t blocks = (T + 8 * rows - 1) / (8 * rows);
-    return blocks < 1 ? 1 : blocks > 1024 ? 1024 : blocks;
+    const int64_t blocks = (T + rows - 1) / rows;
+    return blocks < 1 ? 1 : blocks > 512 ? 512 : blocks;
 }
 
 template <class E>
@@ -321,7 +334,7 @@ int norm_bwd_typed(Mat dy, Mat h, Mat dres, const void* w, bool w_bf16, const fl
         }
     });
     if (e) return e;
-    const dim3 grid((uint32_t)((D + 63) / 64));
+    const dim3 grid((uint32_t)((D + 31) / 32));
     return dw_bf16 ? launch(norm_dw_join_kernel<BF16>, grid, 1024, stream, parts, groups, D,
                             static_cast<uint16_t*>(dw))
                    : launch(norm_dw_join_kernel<F32>, grid, 1024, stream, parts, groups, D,
