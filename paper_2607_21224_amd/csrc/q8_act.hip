@@ -7,7 +7,6 @@ namespace q8 {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 
 // e^x and 1 / x by the hardware's instructions, each good to one unit in the
@@ -16,13 +15,34 @@ __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp
 __device__ __forceinline__ float sigmoid(float x) {
     return __builtin_amdgcn_rcpf(1.0f + fast_exp(-x));
 }
-__device__ __forceinline__ float normal_cdf(float x) {
-    return 0.5f * (1.0f + erff(x * kSqrtHalf));
+
+// Phi(x) = e^(-x^2 / 2) Q(1 / (1 + |x| / 4)) for x < 0, and 1 minus that of -x for
+// x > 0: one exponential, which the density shares, instead of an error function
+// and an exponential.  Q is a polynomial of degree 9 without a constant term,
+// fitted to e^(x^2 / 2) Phi(x) on [-14, 0] for the least largest relative error
+// (6e-8); in fp32 Phi is within 2e-7, and within a relative 1e-6 down to -4.
+struct Normal {
+    float cdf, pdf;
+};
+__device__ __forceinline__ Normal normal(float x) {
+    const float e = __builtin_amdgcn_exp2f(x * x * (-0.5f * kLog2e));
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.25f, 1.0f));
+    float q = 2.572378214e-02f;
+    q = fmaf(q, t, -1.528107217e-01f);
+    q = fmaf(q, t, 2.961246659e-01f);
+    q = fmaf(q, t, -2.057864473e-01f);
+    q = fmaf(q, t, 2.017605353e-01f);
+    q = fmaf(q, t, 3.292692005e-02f);
+    q = fmaf(q, t, 1.037469470e-01f);
+    q = fmaf(q, t, 9.851680666e-02f);
+    q = fmaf(q, t, 9.979748346e-02f);
+    q = q * t * e;
+    return {x > 0.0f ? 1.0f - q : q, e * kInvSqrt2Pi};
 }
 
 template <Act K>
 __device__ __forceinline__ float activation(float g, float u) {
-    if constexpr (K == Act::GELU) return g * normal_cdf(g);
+    if constexpr (K == Act::GELU) return g * normal(g).cdf;
     else return g * sigmoid(g) * u;
 }
 
@@ -179,8 +199,8 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(const typename E::T* da, i
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) {
             const float x = G[k] * sg;
-            const float pdf = fast_exp(-0.5f * x * x) * kInvSqrt2Pi;
-            G[k] = d[k] * fmaf(x, pdf, normal_cdf(x));
+            const Normal p = normal(x);
+            G[k] = d[k] * fmaf(x, p.pdf, p.cdf);
         }
     } else {
         load8(cu + row * ldc + c, n, U);

@@ -91,6 +91,34 @@ __device__ __forceinline__ void load8(const int8_t* p, int n, float (&x)[kPiece]
     for (int k = 0; k < kPiece; ++k) x[k] = k < n ? (float)p[k] : 0.0f;
 }
 
+// A piece as it lies in memory, so that one can be on its way, or waiting, in half
+// the registers (bf16) its values take.
+template <class E>
+struct Raw;
+template <>
+struct Raw<BF16> {
+    u32x4 v;
+    __device__ __forceinline__ void load(const uint16_t* p, int n) {
+        if (n >= kPiece) {
+            v = *reinterpret_cast<const u32x4*>(p);
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = (2 * k < n ? (uint32_t)p[2 * k] : 0) |
+                   (2 * k + 1 < n ? (uint32_t)p[2 * k + 1] << 16 : 0);
+    }
+    __device__ __forceinline__ float operator[](int k) const {
+        return __uint_as_float(k % 2 == 0 ? v[k / 2] << 16 : v[k / 2] & 0xffff0000u);
+    }
+};
+template <>
+struct Raw<F32> {
+    float v[kPiece];
+    __device__ __forceinline__ void load(const float* p, int n) { load8(p, n, v); }
+    __device__ __forceinline__ float operator[](int k) const { return v[k]; }
+};
+
 __device__ __forceinline__ void store8(uint16_t* p, int n, const float (&x)[kPiece]) {
     if (n >= kPiece) {
         *reinterpret_cast<u32x4*>(p) = u32x4{narrow2(x[0], x[1]), narrow2(x[2], x[3]),

@@ -29,16 +29,30 @@ __global__ __launch_bounds__(1024) void few_kernel(const int8_t* a, int64_t lda,
         ap[i] = reinterpret_cast<const char*>(a) + (i * 16 + r < M ? i * 16 + r : M - 1) * lda +
                 g * 32;
     i32x4 acc[MT] = {};
+    // U steps are on their way together
+    constexpr int U = MT == 1 ? 4 : 2;
     const int steps = K / kStep;
-#pragma unroll 4
-    for (int k = wave; k < steps; k += waves) {
-        const int64_t at = (int64_t)k * kStep;
+    for (int k = wave; k < steps; k += waves * U) {
+        u32x4 w[U][2], x[U][MT][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(bp + at + h * 16);
+        for (int u = 0; u < U; ++u) {
+            if (k + u * waves >= steps) break;
+            const int64_t at = (int64_t)(k + u * waves) * kStep;
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-                acc[i] = Int8::mfma(w, *reinterpret_cast<const u32x4*>(ap[i] + at + h * 16), acc[i]);
+            for (int h = 0; h < 2; ++h) {
+                w[u][h] = *reinterpret_cast<const u32x4*>(bp + at + h * 16);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    x[u][i][h] = *reinterpret_cast<const u32x4*>(ap[i] + at + h * 16);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (k + u * waves >= steps) break;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < MT; ++i) acc[i] = Int8::mfma(w[u][h], x[u][i][h], acc[i]);
         }
     }
     if (K % kStep != 0 && wave == steps % waves) {

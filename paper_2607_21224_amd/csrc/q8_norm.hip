@@ -161,23 +161,41 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_bwd_kernel(
         const int c = (j * TPR + lane) * kPiece;
         load_w(w, w_bf16, c < D ? c : 0, c < D ? D - c : 0, wv[j]);
     }
-    int turn = 0;
-    for (int64_t row = group; row < T; row += groups, turn ^= 1) {
-        const float rs = rstd[row];
-        float g[CH][kPiece], n[CH][kPiece], sum = 0.0f;
-        uint32_t none[1];
+    // a row's dy and h are sent for while the row before is worked on
+    Raw<E> g[CH], n[CH], r[CH];
+    const auto fetch = [&](int64_t row) {
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int c = (j * TPR + lane) * kPiece;
             if (c < D) {
-                load8(dy + row * lddy + c, D - c, g[j]);
-                load8(h + row * ldh + c, D - c, n[j]);
+                g[j].load(dy + row * lddy + c, D - c);
+                n[j].load(h + row * ldh + c, D - c);
+            }
+        }
+    };
+    if (group < T) fetch(group);
+    int turn = 0;
+    for (int64_t row = group; row < T; row += groups, turn ^= 1) {
+        const float rs = rstd[row];
+        float sum = 0.0f;
+        uint32_t none[1];
+        Raw<E> g0[CH], n0[CH];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int c = (j * TPR + lane) * kPiece;
+            g0[j] = g[j];
+            n0[j] = n[j];
+            if (c < D && dres != nullptr) r[j].load(dres + row * lddres + c, D - c);
+        }
+        if (row + groups < T) fetch(row + groups);
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            if ((j * TPR + lane) * kPiece < D) {
 #pragma unroll
                 for (int k = 0; k < kPiece; ++k) {
-                    n[j][k] *= rs;
-                    acc[j][k] = fmaf(g[j][k], n[j][k], acc[j][k]);
-                    g[j][k] *= wv[j][k];
-                    sum = fmaf(g[j][k], n[j][k], sum);
+                    const float nk = n0[j][k] * rs;
+                    acc[j][k] = fmaf(g0[j][k], nk, acc[j][k]);
+                    sum = fmaf(g0[j][k] * wv[j][k], nk, sum);
                 }
             }
         }
@@ -187,11 +205,11 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_bwd_kernel(
         for (int j = 0; j < CH; ++j) {
             const int c = (j * TPR + lane) * kPiece;
             if (c < D) {
-                float d[kPiece] = {};
-                if (dres != nullptr) load8(dres + row * lddres + c, D - c, d);
+                float d[kPiece];
 #pragma unroll
                 for (int k = 0; k < kPiece; ++k)
-                    d[k] = fmaf(fmaf(-n[j][k], mean, g[j][k]), rs, d[k]);
+                    d[k] = fmaf(fmaf(-(n0[j][k] * rs), mean, g0[j][k] * wv[j][k]), rs,
+                                dres != nullptr ? r[j][k] : 0.0f);
                 store8(dx + row * lddx + c, D - c, d);
             }
         }
@@ -296,11 +314,11 @@ int with_bwd_shape(int64_t D, F f) {
     return f(Int<0>(), Int<0>());
 }
 
-// Blocks of the backward pass, each with one part of dw a row it holds: two a CU,
+// Blocks of the backward pass, each with one part of dw a row it holds: four a CU,
 // and as many as there are rows for where they are fewer.
 int64_t bwd_blocks(int64_t T, int rows) {
     const int64_t blocks = (T + rows - 1) / rows;
-    return blocks < 1 ? 1 : blocks > 512 ? 512 : blocks;
+    return blocks < 1 ? 1 : blocks > 1024 ? 1024 : blocks;
 }
 
 template <class E>
