@@ -66,8 +66,8 @@ __global__ __launch_bounds__(block_of(TPR)) void act_kernel(
     for (int j = 0; j < CH; ++j) {
         const int c = (j * TPR + lane) * kPiece;
         if (c < F) {
-            load8(g + row * ldg + c, F - c, gv[j]);
-            if constexpr (kGated) load8(u + row * ldg + c, F - c, uv[j]);
+            load8(g + row * ldg + c, F - c, c, gv[j]);
+            if constexpr (kGated) load8(u + row * ldg + c, F - c, c, uv[j]);
 #pragma unroll
             for (int k = 0; k < kPiece; ++k) {
                 a[j][k] = activation<K>(gv[j][k], kGated ? uv[kGated ? j : 0][k] : 0.0f);
@@ -113,8 +113,8 @@ __global__ __launch_bounds__(1024) void act_long_kernel(
     float gv[kPiece], uv[kPiece] = {}, a[kPiece], none;
     uint32_t top[3] = {};
     for (int c = (int)threadIdx.x * kPiece; c < F; c += 1024 * kPiece) {
-        load8(g + row * ldg + c, F - c, gv);
-        if constexpr (kGated) load8(u + row * ldg + c, F - c, uv);
+        load8(g + row * ldg + c, F - c, c, gv);
+        if constexpr (kGated) load8(u + row * ldg + c, F - c, c, uv);
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) {
             top[0] = max(top[0], magnitude(activation<K>(gv[k], uv[k])));
@@ -132,8 +132,8 @@ __global__ __launch_bounds__(1024) void act_long_kernel(
         if (kGated && cu != nullptr) cu_scale[row] = r[2].s;
     }
     for (int c = (int)threadIdx.x * kPiece; c < F; c += 1024 * kPiece) {
-        load8(g + row * ldg + c, F - c, gv);
-        if constexpr (kGated) load8(u + row * ldg + c, F - c, uv);
+        load8(g + row * ldg + c, F - c, c, gv);
+        if constexpr (kGated) load8(u + row * ldg + c, F - c, c, uv);
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) a[k] = activation<K>(gv[k], uv[k]);
         write_piece<Y>(a, r[0], q + row * ldq + c, y == nullptr ? y : y + row * ldy + c, F - c);
@@ -192,8 +192,8 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(const typename E::T* da, i
     if (row >= T || c >= F) return;
     const int n = F - c;
     float d[kPiece], G[kPiece], U[kPiece];
-    load8(da + row * ldda + c, n, d);
-    load8(cg + row * ldc + c, n, G);
+    load8(da + row * ldda + c, n, c, d);
+    load8(cg + row * ldc + c, n, c, G);
     const float sg = cg_scale[row];
     if constexpr (K == Act::GELU) {
 #pragma unroll
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(const typename E::T* da, i
             G[k] = d[k] * fmaf(x, p.pdf, p.cdf);
         }
     } else {
-        load8(cu + row * ldc + c, n, U);
+        load8(cu + row * ldc + c, n, c, U);
         const float su = cu_scale[row];
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) {

@@ -52,43 +52,79 @@ __device__ __forceinline__ float stored(float x) {
     else return x;
 }
 
-// n (at most 8) elements at p; the missing ones are 0
-__device__ __forceinline__ void load8(const uint16_t* p, int n, float (&x)[kPiece]) {
-    if (n >= kPiece) {
-        const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+// A piece that the row's end cuts short (n < 8 of its elements exist) is read as
+// the row's last 8 elements, wherever they start, and shifted into place; what
+// was read of the piece before is dropped.  Only a row of fewer than 8 elements
+// is read one by one: a load behind a branch for each element made the last
+// wavefront of every row wait for memory up to 7 times.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+
+// x[k] <- x[k + 8 - n], zeros past the end
+__device__ __forceinline__ void shift_down(float (&x)[kPiece], int n) {
+    const int s = kPiece - n;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[2 * k] = __uint_as_float(v[k] << 16);
-            x[2 * k + 1] = __uint_as_float(v[k] & 0xffff0000u);
-        }
-        return;
-    }
+    for (int step = 4; step > 0; step >>= 1)
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) x[k] = k < n ? widen(p[k]) : 0.0f;
+        for (int k = 0; k < kPiece; ++k)
+            x[k] = (s & step) == 0 ? x[k] : k + step < kPiece ? x[k + step] : 0.0f;
 }
-__device__ __forceinline__ void load8(const float* p, int n, float (&x)[kPiece]) {
-    if (n >= kPiece) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(p);
-        const f32x4 b = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[k] = a[k];
-            x[4 + k] = b[k];
-        }
-        return;
+
+// n elements at p, the column c of their row; the missing ones of 8 are 0
+// (8 bytes of bf16 or int8 hold whole elements: a shift of the bits will do)
+__device__ __forceinline__ u32x4 bits8(const uint16_t* p, int n, int c) {
+    if (n >= kPiece) return *reinterpret_cast<const u32x4*>(p);
+    if (c + n >= kPiece) {
+        const u32x4 v = *reinterpret_cast<const u32x4_any*>(p + n - kPiece);
+        return __builtin_bit_cast(
+            u32x4, __builtin_bit_cast(unsigned __int128, v) >> (16 * (kPiece - n)));
     }
+    u32x4 v = {0, 0, 0, 0};
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) x[k] = k < n ? p[k] : 0.0f;
+    for (int k = 0; k < kPiece; ++k)
+        if (k < n) v[k / 2] |= (uint32_t)p[k] << (16 * (k % 2));
+    return v;
 }
-__device__ __forceinline__ void load8(const int8_t* p, int n, float (&x)[kPiece]) {
-    if (n >= kPiece) {
-        const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+__device__ __forceinline__ u32x2 bits8(const int8_t* p, int n, int c) {
+    if (n >= kPiece) return *reinterpret_cast<const u32x2*>(p);
+    if (c + n >= kPiece) {
+        const u32x2 v = *reinterpret_cast<const u32x2_any*>(p + n - kPiece);
+        return __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, v) >> (8 * (kPiece - n)));
+    }
+    u32x2 v = {0, 0};
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) x[k] = (float)(int8_t)(v[k / 4] >> (8 * (k % 4)));
+    for (int k = 0; k < kPiece; ++k)
+        if (k < n) v[k / 4] |= (uint32_t)(uint8_t)p[k] << (8 * (k % 4));
+    return v;
+}
+__device__ __forceinline__ void load8(const uint16_t* p, int n, int c, float (&x)[kPiece]) {
+    const u32x4 v = bits8(p, n, c);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        x[2 * k] = __uint_as_float(v[k] << 16);
+        x[2 * k + 1] = __uint_as_float(v[k] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float* p, int n, int c, float (&x)[kPiece]) {
+    if (n < kPiece && c + n < kPiece) {
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) x[k] = k < n ? p[k] : 0.0f;
         return;
     }
+    const float* q = n >= kPiece ? p : p + n - kPiece;
+    const u32x4 a = *reinterpret_cast<const u32x4_any*>(q);
+    const u32x4 b = *reinterpret_cast<const u32x4_any*>(q + 4);
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) x[k] = k < n ? (float)p[k] : 0.0f;
+    for (int k = 0; k < 4; ++k) {
+        x[k] = __uint_as_float(a[k]);
+        x[4 + k] = __uint_as_float(b[k]);
+    }
+    if (n < kPiece) shift_down(x, n);
+}
+__device__ __forceinline__ void load8(const int8_t* p, int n, int c, float (&x)[kPiece]) {
+    const u32x2 v = bits8(p, n, c);
+#pragma unroll
+    for (int k = 0; k < kPiece; ++k) x[k] = (float)(int8_t)(v[k / 4] >> (8 * (k % 4)));
 }
 
 // A piece as it lies in memory, so that one can be on its way, or waiting, in half
@@ -98,16 +134,7 @@ struct Raw;
 template <>
 struct Raw<BF16> {
     u32x4 v;
-    __device__ __forceinline__ void load(const uint16_t* p, int n) {
-        if (n >= kPiece) {
-            v = *reinterpret_cast<const u32x4*>(p);
-            return;
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            v[k] = (2 * k < n ? (uint32_t)p[2 * k] : 0) |
-                   (2 * k + 1 < n ? (uint32_t)p[2 * k + 1] << 16 : 0);
-    }
+    __device__ __forceinline__ void load(const uint16_t* p, int n, int c) { v = bits8(p, n, c); }
     __device__ __forceinline__ float operator[](int k) const {
         return __uint_as_float(k % 2 == 0 ? v[k / 2] << 16 : v[k / 2] & 0xffff0000u);
     }
@@ -115,14 +142,20 @@ struct Raw<BF16> {
 template <>
 struct Raw<F32> {
     float v[kPiece];
-    __device__ __forceinline__ void load(const float* p, int n) { load8(p, n, v); }
+    __device__ __forceinline__ void load(const float* p, int n, int c) { load8(p, n, c, v); }
     __device__ __forceinline__ float operator[](int k) const { return v[k]; }
 };
 
+// Results leave as they are made, nontemporal: what a launch leaves in an XCD's
+// L2 the next one, whose blocks run on other XCDs, cannot use.  With ordinary
+// stores the norm of 16384 x 1024 bf16 took 33 us and not 25, of 16384 x 8192
+// 226 and not 219.  (Not the fp32 results, whose two stores a lane fill a line only
+// together: 3 % slower that way.)
 __device__ __forceinline__ void store8(uint16_t* p, int n, const float (&x)[kPiece]) {
     if (n >= kPiece) {
-        *reinterpret_cast<u32x4*>(p) = u32x4{narrow2(x[0], x[1]), narrow2(x[2], x[3]),
-                                             narrow2(x[4], x[5]), narrow2(x[6], x[7])};
+        __builtin_nontemporal_store(u32x4{narrow2(x[0], x[1]), narrow2(x[2], x[3]),
+                                          narrow2(x[4], x[5]), narrow2(x[6], x[7])},
+                                    reinterpret_cast<u32x4*>(p));
         return;
     }
 #pragma unroll
@@ -141,7 +174,7 @@ __device__ __forceinline__ void store8(float* p, int n, const float (&x)[kPiece]
 }
 __device__ __forceinline__ void store_bytes(int8_t* p, int n, u32x2 v) {
     if (n >= kPiece) {
-        *reinterpret_cast<u32x2*>(p) = v;
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(p));
         return;
     }
 #pragma unroll

@@ -94,7 +94,7 @@ __device__ __forceinline__ void barrier() {
 // 16 bytes at p, of which the first n exist (n may be negative) and `before` bytes
 // of the row come before p.  A piece that is cut short is read as the row's last
 // 16 bytes, shifted into place; a row shorter than that, element by element.
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+
 template <int BYTES>
 __device__ __forceinline__ u32x4 load_tail(const char* p, int n, int before) {
     if (n >= 16) return *reinterpret_cast<const u32x4*>(p);

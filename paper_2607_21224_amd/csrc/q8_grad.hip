@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256) void transpose_kernel(const In* in, int64_t ld
         const int64_t n = r0 + r < R ? C - c0 - c : 0;
         float x[kPiece] = {};
         if (n > 0) {
-            load8(in + (r0 + r) * ld + c0 + c, n < kPiece ? (int)n : kPiece, x);
+            load8(in + (r0 + r) * ld + c0 + c, n < kPiece ? (int)n : kPiece, (int)c0 + c, x);
             if (scale != nullptr) {
                 const float s = scale[r0 + r];
 #pragma unroll
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void spread_kernel(const In* in, int64_t ld, c
     if (r >= R) return;
     float x[kPiece] = {};
     const int64_t n = C - c;
-    if (n > 0) load8(in + r * ld + c, n < kPiece ? (int)n : kPiece, x);
+    if (n > 0) load8(in + r * ld + c, n < kPiece ? (int)n : kPiece, (int)c, x);
     uint16_t part[kPiece][P];
 #pragma unroll
     for (int k = 0; k < kPiece; ++k) {

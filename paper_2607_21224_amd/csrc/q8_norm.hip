@@ -7,8 +7,8 @@ namespace q8 {
 namespace {
 
 __device__ __forceinline__ void load_w(const void* w, bool bf16, int c, int n, float (&x)[kPiece]) {
-    if (bf16) load8(static_cast<const uint16_t*>(w) + c, n, x);
-    else load8(static_cast<const float*>(w) + c, n, x);
+    if (bf16) load8(static_cast<const uint16_t*>(w) + c, n, c, x);
+    else load8(static_cast<const float*>(w) + c, n, c, x);
 }
 
 // h and p = h w of one piece; h is stored where there is a residual
@@ -17,10 +17,10 @@ __device__ __forceinline__ void norm_piece(const typename E::T* x, const typenam
                                            typename E::T* h, const void* w, bool w_bf16, int c,
                                            int n, float& sum, uint32_t& top, float (&p)[kPiece]) {
     float a[kPiece], b[kPiece];
-    load8(x, n, a);
+    load8(x, n, c, a);
     load_w(w, w_bf16, c, n, p);
     if (r != nullptr) {
-        load8(r, n, b);
+        load8(r, n, c, b);
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) a[k] = stored<E>(a[k] + b[k]);
         store8(h, n, a);
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(
     // every thread reads back what it wrote itself
     const typename E::T* hr = res == nullptr ? x + row * ldx : h + row * ldh;
     for (int c = (int)threadIdx.x * kPiece; c < D; c += 1024 * kPiece) {
-        load8(hr + c, D - c, v);
+        load8(hr + c, D - c, c, v);
         load_w(w, w_bf16, c, D - c, p);
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) p[k] = v[k] * p[k] * s.rstd;
@@ -168,8 +168,8 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_bwd_kernel(
         for (int j = 0; j < CH; ++j) {
             const int c = (j * TPR + lane) * kPiece;
             if (c < D) {
-                g[j].load(dy + row * lddy + c, D - c);
-                n[j].load(h + row * ldh + c, D - c);
+                g[j].load(dy + row * lddy + c, D - c, c);
+                n[j].load(h + row * ldh + c, D - c, c);
             }
         }
     };
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_bwd_kernel(
             const int c = (j * TPR + lane) * kPiece;
             g0[j] = g[j];
             n0[j] = n[j];
-            if (c < D && dres != nullptr) r[j].load(dres + row * lddres + c, D - c);
+            if (c < D && dres != nullptr) r[j].load(dres + row * lddres + c, D - c, c);
         }
         if (row + groups < T) fetch(row + groups);
 #pragma unroll
@@ -233,8 +233,8 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(
     float sum = 0.0f, g[kPiece], n[kPiece], v[kPiece];
     uint32_t none[1];
     for (int c = (int)threadIdx.x * kPiece; c < D; c += 1024 * kPiece) {
-        load8(dy + row * lddy + c, D - c, g);
-        load8(h + row * ldh + c, D - c, n);
+        load8(dy + row * lddy + c, D - c, c, g);
+        load8(h + row * ldh + c, D - c, c, n);
         load_w(w, w_bf16, c, D - c, v);
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) sum = fmaf(g[k] * v[k], n[k] * rs, sum);
@@ -243,10 +243,10 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(
     const float mean = sum / (float)D;
     for (int c = (int)threadIdx.x * kPiece; c < D; c += 1024 * kPiece) {
         float d[kPiece] = {};
-        load8(dy + row * lddy + c, D - c, g);
-        load8(h + row * ldh + c, D - c, n);
+        load8(dy + row * lddy + c, D - c, c, g);
+        load8(h + row * ldh + c, D - c, c, n);
         load_w(w, w_bf16, c, D - c, v);
-        if (dres != nullptr) load8(dres + row * lddres + c, D - c, d);
+        if (dres != nullptr) load8(dres + row * lddres + c, D - c, c, d);
 #pragma unroll
         for (int k = 0; k < kPiece; ++k)
             d[k] = fmaf(fmaf(-(n[k] * rs), mean, g[k] * v[k]), rs, d[k]);
@@ -264,8 +264,8 @@ __global__ __launch_bounds__(256) void norm_dw_kernel(const typename E::T* dy, i
     float acc[kPiece] = {}, g[kPiece], n[kPiece];
     for (int64_t row = blockIdx.y; row < T; row += gridDim.y) {
         const float rs = rstd[row];
-        load8(dy + row * lddy + c, D - c, g);
-        load8(h + row * ldh + c, D - c, n);
+        load8(dy + row * lddy + c, D - c, c, g);
+        load8(h + row * ldh + c, D - c, c, n);
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) acc[k] = fmaf(g[k], n[k] * rs, acc[k]);
     }

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(block_of(TPR)) void rows_kernel(const typename E::T
     for (int j = 0; j < CH; ++j) {
         const int c = (j * TPR + lane) * kPiece;
         if (c < D) {
-            load8(x + row * ldx + c, D - c, v[j]);
+            load8(x + row * ldx + c, D - c, c, v[j]);
 #pragma unroll
             for (int k = 0; k < kPiece; ++k) top[0] = max(top[0], magnitude(v[j][k]));
         }
@@ -51,7 +51,7 @@ __global__ __launch_bounds__(1024) void rows_long_kernel(const typename E::T* x,
     uint32_t top[1] = {0};
     float v[kPiece];
     for (int c = (int)threadIdx.x * kPiece; c < D; c += 1024 * kPiece) {
-        load8(x + row * ldx + c, D - c, v);
+        load8(x + row * ldx + c, D - c, c, v);
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) top[0] = max(top[0], magnitude(v[k]));
     }
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(1024) void rows_long_kernel(const typename E::T* x,
     const RowScale r = row_scale(__uint_as_float(top[0]));
     if (threadIdx.x == 0) scale[row] = r.s;
     for (int c = (int)threadIdx.x * kPiece; c < D; c += 1024 * kPiece) {
-        load8(x + row * ldx + c, D - c, v);
+        load8(x + row * ldx + c, D - c, c, v);
         write_piece<Y>(v, r, q + row * ldq + c, y == nullptr ? y : y + row * ldy + c, D - c);
     }
 }
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void values_kernel(const int8_t* q, int64_t ld
     if (row >= T || c >= D) return;
     float v[kPiece];
     const float s = scale[row];
-    load8(q + row * ldq + c, D - c, v);
+    load8(q + row * ldq + c, D - c, c, v);
 #pragma unroll
     for (int k = 0; k < kPiece; ++k) v[k] *= s;
     store8(y + row * ldy + c, D - c, v);
