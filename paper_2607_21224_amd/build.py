@@ -41,7 +41,7 @@ HOST_SOURCES = ("cpdp_api.cpp",)
 SCRATCH_SOURCES = ("plan_scratch.hip",)
 # libcpdp_q8.so: kernel translation units and the host validation layer
 Q8_SOURCES = ("q8_rows.hip", "q8_norm.hip", "q8_act.hip", "q8_matmul.hip", "q8_grad.hip",
-              "q8_api.cpp")
+              "q8_grad_few.hip", "q8_api.cpp")
 OBJ_ROOT = os.path.join(ROOT, "_build")
 
 

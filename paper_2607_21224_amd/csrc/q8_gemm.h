@@ -400,9 +400,20 @@ __global__ __launch_bounds__(256) void join_kernel(Target t, int64_t M, int64_t 
     const int64_t m = i / across, n0 = i % across * 4;
     if (m >= M) return;
     const auto* p = static_cast<const typename Op::Sum*>(t.ws) + m * t.ldws + n0;
-    typename Op::Acc s = *reinterpret_cast<const typename Op::Acc*>(p);
-    for (int z = 1; z < slices; ++z)
-        s += *reinterpret_cast<const typename Op::Acc*>(p + z * t.slice);
+    // slices are a power of two; up to 8 are on their way together
+    typename Op::Acc s = {};
+    const auto add = [&](int z, auto count) {
+        typename Op::Acc v[count];
+#pragma unroll
+        for (int i = 0; i < count; ++i)
+            v[i] = *reinterpret_cast<const typename Op::Acc*>(p + (z + i) * t.slice);
+#pragma unroll
+        for (int i = 0; i < count; ++i) s += v[i];
+    };
+    if (slices == 2) add(0, Int<2>());
+    else if (slices == 4) add(0, Int<4>());
+    else
+        for (int z = 0; z < slices; z += 8) add(z, Int<8>());
     const int n = (int)(N - n0 < 4 ? N - n0 : 4);
     float v[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
     if (t.row_scale != nullptr) {
@@ -422,15 +433,32 @@ struct Shape {
 
 inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The largest tile that gives each CU about one block; below that, 64 x 64 tiles
-// over slices of K.
+// The tile and the slices of K that should take the least time.  A step of a
+// tile's block takes `least` ns while its CU has few others, and the CU gets
+// through one such step in `each` ns when it has many (measured on products of
+// 64 to 8192 rows with 4096 columns and K = 4096, where the best choice is taken
+// or missed by less than a tenth).  Slices are added up by a second launch: its
+// start, and each sum written and read again at 3 TB/s.
 inline Shape shape_of(int64_t M, int64_t N, int64_t steps) {
-    if (up(M, 256) * up(N, 256) >= 192) return {256, 1};
-    if (up(M, 128) * up(N, 128) >= 192) return {128, 1};
-    const int64_t tiles = up(M, 64) * up(N, 64);
-    int64_t slices = 1;
-    while (tiles * slices < 512 && slices < 16 && steps / (2 * slices) >= 4) slices *= 2;
-    return {64, (int)slices};
+    const struct {
+        int tile, least, each;
+    } tiles[] = {{256, 1500, 1850}, {128, 900, 640}, {64, 700, 230}};
+    Shape best = {256, 1};
+    double least = -1;
+    for (const auto& t : tiles) {
+        const int64_t n = up(M, t.tile) * up(N, t.tile);
+        for (int slices = 1; slices <= 64; slices *= 2) {
+            if (slices > 1 && (t.tile != 64 || n * slices > 2048 || steps < 4 * slices)) break;
+            const double each = (double)up(n * slices, 256) * t.each;
+            const double time = (double)up(steps, slices) * (each > t.least ? each : t.least) +
+                                (slices > 1 ? 4500.0 + slices * (double)M * (double)N / 375.0 : 0);
+            if (least < 0 || time < least) {
+                least = time;
+                best = {t.tile, slices};
+            }
+        }
+    }
+    return best;
 }
 
 // Workspace of a product's slices.
@@ -450,6 +478,13 @@ int launch_tiles(const Operands& o, const Target& t, int slices, void* stream) {
 }
 
 template <class Op>
+int launch_join(const Target& t, int64_t M, int64_t N, int slices, void* stream) {
+    const int64_t items = M * up(N, 4);
+    if (items >= ((int64_t)1 << 32) - 256) return (int)hipErrorInvalidValue;
+    return launch(join_kernel<Op>, dim3((uint32_t)up(items, 256)), 256, stream, t, M, N, slices);
+}
+
+template <class Op>
 int launch_gemm(const Operands& o, Target t, void* ws, void* stream) {
     const Shape s = shape_of(o.M, o.N, (int64_t)(o.row / kStep) * o.parts);
     t.ws = ws;
@@ -459,8 +494,7 @@ int launch_gemm(const Operands& o, Target t, void* ws, void* stream) {
     if (s.tile == 128) return launch_tiles<Op, 128, 128, 2, 2>(o, t, 1, stream);
     if (int e = launch_tiles<Op, 64, 64, 2, 2>(o, t, s.slices, stream)) return e;
     if (s.slices == 1) return 0;
-    return launch(join_kernel<Op>, dim3((uint32_t)up(o.M * up(o.N, 4), 256)), 256, stream, t, o.M,
-                  o.N, s.slices);
+    return launch_join<Op>(t, o.M, o.N, s.slices, stream);
 }
 
 }  // namespace

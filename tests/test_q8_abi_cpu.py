@@ -56,11 +56,11 @@ CALLS = {
     "cpdp_q8_act_bwd": dict(kind=1, da=at(0), ldda=64, act_dt=BF16, cg=at(1), cg_scale=at(2),
                             cu=at(3), cu_scale=at(4), ldc=64, T=8, F=64, dg=at(5), du=at(6),
                             lddg=64, stream=None),
-    "cpdp_q8_grad_input": dict(dy=at(0), lddy=32, dy_dt=BF16, b=at(1), ldb=64, b_scale=at(2), T=8,
+    "cpdp_q8_grad_input": dict(dy=at(0), lddy=32, dy_dt=BF16, b=at(1), ldb=64, b_scale=at(2), T=80,
                                N=32, K=64, dx=at(3), lddx=64, out_dt=F32, workspace=at(4),
                                workspace_bytes=1 << 30, stream=None),
     "cpdp_q8_grad_weight": dict(dy=at(0), lddy=32, dy_dt=BF16, a=at(1), lda=64, a_scale=at(2),
-                                T=8, N=32, K=64, dw=at(3), lddw=64, out_dt=F32, workspace=at(4),
+                                T=80, N=32, K=64, dw=at(3), lddw=64, out_dt=F32, workspace=at(4),
                                 workspace_bytes=1 << 30, stream=None),
 }
 ROWS = {n: "M" if n == "cpdp_q8_matmul" else "T" for n in CALLS}
