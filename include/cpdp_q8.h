@@ -18,7 +18,9 @@
  * any fp32 scales and any q in [-128, 127].
  *
  * Layout.  A matrix argument of R rows and C columns has its element (r, c) at
- * base[r * ld + c].  Elements past a row's end are never read or written.
+ * base[r * ld + c].  Elements past a row's end are never written, and not used:
+ * the gradients of a product read their operands in whole 16-byte pieces, up to 15
+ * bytes past a row's end, the other calls read nothing there.
  * Every matrix starts on a 16-byte boundary and ld * sizeof(element) is a
  * multiple of 16 (CPDP_ERR_MISALIGNED); ld >= C.  Vectors (scales, w, dw) are
  * contiguous; w and dw start on a 16-byte boundary, scales and rstd on a 4-byte

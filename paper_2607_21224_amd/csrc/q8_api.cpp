@@ -319,7 +319,7 @@ int cpdp_q8_grad_input(const void* dy, int64_t lddy, int dy_dt, const int8_t* b,
     s.out(dx, lddx, T, K, esize(out_dt == CPDP_BF16));
     if (need > 0) s.out(workspace, need, 1, 16);
     if (int e = s.status()) return e;
-    if (grad_too_large(N) || lddy > kMaxTileLd / 2) return CPDP_ERR_TOO_LARGE;
+    if (grad_too_large(N) || lddy > kMaxTileLd / 2 || ldb > kMaxTileLd) return CPDP_ERR_TOO_LARGE;
     if (T == 0) return CPDP_OK;
     return hip_status(cpdp::q8::launch_grad_input(mat(dy, lddy, dy_dt), held(b, ldb, b_scale), T, N,
                                                   K, mat(dx, lddx, out_dt), workspace, stream));
@@ -349,7 +349,7 @@ int cpdp_q8_grad_weight(const void* dy, int64_t lddy, int dy_dt, const int8_t* a
     s.out(dw, lddw, N, K, esize(out_dt == CPDP_BF16));
     if (need > 0) s.out(workspace, need, 1, 16);
     if (int e = s.status()) return e;
-    if (grad_too_large(T)) return CPDP_ERR_TOO_LARGE;
+    if (grad_too_large(T) || lddy > kMaxTileLd / 2 || lda > kMaxTileLd) return CPDP_ERR_TOO_LARGE;
     if (N == 0) return CPDP_OK;
     return hip_status(cpdp::q8::launch_grad_weight(mat(dy, lddy, dy_dt), held(a, lda, a_scale), T,
                                                    N, K, mat(dw, lddw, out_dt), workspace,
