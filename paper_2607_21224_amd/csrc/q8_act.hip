@@ -7,13 +7,31 @@ namespace q8 {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 
-// e^x and 1 / x by the hardware's instructions, each good to one unit in the
-// last place; e^x also takes the rounding of x log2(e), |x| 2^-24 relative.
-__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// The forward pass rounds its result to one of 255 steps, where a bit decides now
+// and then, and a row's largest element its scale: it takes the math library's
+// functions and a correctly rounded quotient.  That is one step of Newton's method
+// from the hardware's reciprocal (Markstein's theorem: exact rounding for every
+// number but one all of whose bits are ones), a fifth of a division's instructions;
+// the reciprocal of infinity, where e^-g has no fp32 number, is taken as it is.
+__device__ __forceinline__ float reciprocal(float x) {
+    const float r = __builtin_amdgcn_rcpf(x);
+    const float n = fmaf(fmaf(-x, r, 1.0f), r, r);
+    return magnitude(x) < 0x7f800000u ? n : r;
+}
+template <Act K>
+__device__ __forceinline__ float activation(float g, float u) {
+    if constexpr (K == Act::GELU) return 0.5f * g * (1.0f + erff(g * kSqrtHalf));
+    else return g * reciprocal(1.0f + expf(-g)) * u;
+}
+
+// The backward pass has no such steps.  e^x and 1 / x are the hardware's
+// instructions, each good to one unit in the last place; e^x also takes the rounding
+// of x log2(e), |x| 2^-24 relative.
 __device__ __forceinline__ float sigmoid(float x) {
-    return __builtin_amdgcn_rcpf(1.0f + fast_exp(-x));
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -kLog2e));
 }
 
 // Phi(x) = e^(-x^2 / 2) Q(1 / (1 + |x| / 4)) for x < 0, and 1 minus that of -x for
@@ -38,12 +56,6 @@ __device__ __forceinline__ Normal normal(float x) {
     q = fmaf(q, t, 9.979748346e-02f);
     q = q * t * e;
     return {x > 0.0f ? 1.0f - q : q, e * kInvSqrt2Pi};
-}
-
-template <Act K>
-__device__ __forceinline__ float activation(float g, float u) {
-    if constexpr (K == Act::GELU) return g * normal(g).cdf;
-    else return g * sigmoid(g) * u;
 }
 
 // Bound by HBM: 6 bytes an element for GELU with bf16 values written, 9 for the
