@@ -437,12 +437,15 @@ inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // tile's block takes `least` ns while its CU has few others, and the CU gets
 // through one such step in `each` ns when it has many (measured on products of
 // 64 to 8192 rows with 4096 columns and K = 4096, where the best choice is taken
-// or missed by less than a tenth).  Slices are added up by a second launch: its
+// or missed by less than a tenth).  A step with several parts of A takes them one
+// after the other (256), or together, with the loads of B once.  Slices are added up by a second launch: its
 // start, and each sum written and read again at 3 TB/s.
-inline Shape shape_of(int64_t M, int64_t N, int64_t steps) {
+inline Shape shape_of(int64_t M, int64_t N, int64_t steps, int parts = 1) {
     const struct {
         int tile, least, each;
-    } tiles[] = {{256, 1500, 1850}, {128, 900, 640}, {64, 700, 230}};
+    } tiles[] = {{256, parts * 1500, parts * 1850},
+                 {128, 700 + 200 * parts, 640 * parts},
+                 {64, 600 + 100 * parts, 115 + 115 * parts}};
     Shape best = {256, 1};
     double least = -1;
     for (const auto& t : tiles) {
@@ -463,8 +466,8 @@ inline Shape shape_of(int64_t M, int64_t N, int64_t steps) {
 
 // Workspace of a product's slices.
 inline int64_t slices_ld(int64_t N) { return up(N, 64) * 64; }
-inline int64_t slices_bytes(int64_t M, int64_t N, int64_t steps) {
-    const Shape s = shape_of(M, N, steps);
+inline int64_t slices_bytes(int64_t M, int64_t N, int64_t steps, int parts = 1) {
+    const Shape s = shape_of(M, N, steps, parts);
     return s.slices == 1 ? 0 : s.slices * M * slices_ld(N) * 4;
 }
 

@@ -28,67 +28,90 @@ struct Source {
     int64_t blocks;  // that lay it out
 };
 
-// in [R x C] -> out [P][C][pad], scaled by row, zeros from R to pad.  A block takes
-// 64 x 64 elements through LDS; rows of the LDS tile are 66 numbers long, so that
-// neither direction meets one bank with more than two lanes at a time.
-template <class In, int P>
-__device__ void transpose(const Source& s, int64_t block, uint16_t (&tile)[P][64][66]) {
-    const In* in = static_cast<const In*>(s.p);
-    const int64_t tiles_r = s.pad / 64;
-    const int64_t r0 = block % tiles_r * 64, c0 = block / tiles_r * 64;
+// Columns of a block of the transposing layout: 8 threads across, 16 bytes or more
+// of a row each.
+template <class In>
+constexpr int tile_cols() {
+    return sizeof(In) == 1 ? 128 : 64;
+}
+
+// LDS of one: columns of 32 pairs of rows, a word more, so that the 64 lanes of a
+// wavefront, 8 pairs of rows and 8 columns 8 apart, write to 64 banks.
+template <int P, int COLS>
+using Tile = uint32_t[P][COLS][33];
+
+// 8 columns of two rows, each scaled, as pairs in P parts
+template <class In, int P, int COLS>
+__device__ __forceinline__ void turn8(const Source& s, int64_t r, int64_t c, int col, int pair,
+                                      Tile<P, COLS>& tile) {
+    float x[2][kPiece] = {};
+    const int n = s.C - c < kPiece ? (int)(s.C - c) : kPiece;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int r = h * 32 + (int)threadIdx.x / 8, c = (int)threadIdx.x % 8 * kPiece;
-        const int64_t n = r0 + r < s.R ? s.C - c0 - c : 0;
-        float x[kPiece] = {};
-        if (n > 0) {
-            load8(in + (r0 + r) * s.ld + c0 + c, n < kPiece ? (int)n : kPiece, (int)c0 + c, x);
+    for (int h = 0; h < 2; ++h)
+        if (r + h < s.R && n > 0) {
+            load8(static_cast<const In*>(s.p) + (r + h) * s.ld + c, n, (int)(c < 8 ? c : 8), x[h]);
             if (s.scale != nullptr) {
-                const float f = s.scale[r0 + r];
+                const float f = s.scale[r + h];
 #pragma unroll
-                for (int k = 0; k < kPiece; ++k) x[k] = k < n ? x[k] * f : 0.0f;
+                for (int k = 0; k < kPiece; ++k) x[h][k] = k < n ? x[h][k] * f : 0.0f;
             }
         }
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) {
-            uint16_t part[P];
-            split<P>(x[k], part);
+    for (int k = 0; k < kPiece; ++k) {
+        uint16_t lo[P], hi[P];
+        split<P>(x[0][k], lo);
+        split<P>(x[1][k], hi);
 #pragma unroll
-            for (int p = 0; p < P; ++p) tile[p][c + k][r] = part[p];
-        }
+        for (int p = 0; p < P; ++p) tile[p][col + k][pair] = (uint32_t)lo[p] | (uint32_t)hi[p] << 16;
     }
+}
+
+// in [R x C] -> out [P][C][pad], scaled by row, zeros from R to pad.  A block takes
+// 64 rows through LDS, two neighbouring ones a thread.
+template <class In, int P>
+__device__ void transpose(const Source& s, uint32_t block, Tile<P, tile_cols<In>()>& tile) {
+    constexpr int COLS = tile_cols<In>();
+    const uint32_t tiles_r = (uint32_t)(s.pad / 64);
+    const int64_t r0 = (int64_t)(block % tiles_r) * 64, c0 = (int64_t)(block / tiles_r) * COLS;
+    const int pair = (int)threadIdx.x / 8, col = (int)threadIdx.x % 8 * kPiece;
+#pragma unroll
+    for (int h = 0; h < COLS; h += 64)
+        turn8<In, P, COLS>(s, r0 + 2 * pair, c0 + h + col, h + col, pair, tile);
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = h * 32 + (int)threadIdx.x / 8, r = (int)threadIdx.x % 8 * kPiece;
+        for (int h = 0; h < COLS; h += 32) {
+            const int c = h + (int)threadIdx.x / 8, w = (int)threadIdx.x % 8 * 4;
             if (c0 + c >= s.C) continue;
-            u32x4 v;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                v[k] = *reinterpret_cast<const uint32_t*>(&tile[p][c][r + 2 * k]);
-            *reinterpret_cast<u32x4*>(s.out + ((int64_t)p * s.C + c0 + c) * s.pad + r0 + r) = v;
+            const u32x4 v = {tile[p][c][w], tile[p][c][w + 1], tile[p][c][w + 2],
+                             tile[p][c][w + 3]};
+            *reinterpret_cast<u32x4*>(s.out + ((int64_t)p * s.C + c0 + c) * s.pad + r0 + 2 * w) = v;
         }
 }
 
 // in [R x C] -> out [P][R][pad], scaled by column, zeros from C to pad
 template <class In, int P>
-__device__ void spread(const Source& s, int64_t block) {
-    const int64_t across = s.pad / kPiece;
-    const int64_t i = block * 256 + threadIdx.x;
-    const int64_t r = i / across, c = i % across * kPiece;
+__device__ void spread(const Source& s, uint32_t block) {
+    // (a launch holds fewer than 2^32 work items)
+    const uint32_t across = (uint32_t)(s.pad / kPiece), i = block * 256u + threadIdx.x;
+    const int64_t r = i / across, c = (int64_t)(i % across) * kPiece;
     if (r >= s.R) return;
     float x[kPiece] = {};
-    const int64_t n = s.C - c;
-    if (n > 0)
-        load8(static_cast<const In*>(s.p) + r * s.ld + c, n < kPiece ? (int)n : kPiece, (int)c, x);
+    const int n = s.C - c < kPiece ? (int)(s.C - c) : kPiece;
+    if (n > 0) {
+        const int before = (int)(c < 8 ? c : 8);
+        load8(static_cast<const In*>(s.p) + r * s.ld + c, n, before, x);
+        if (s.scale != nullptr) {
+            float f[kPiece];
+            load8(s.scale + c, n, before, f);
+#pragma unroll
+            for (int k = 0; k < kPiece; ++k) x[k] = k < n ? x[k] * f[k] : 0.0f;
+        }
+    }
     uint16_t part[kPiece][P];
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) {
-        if (s.scale != nullptr && k < n) x[k] *= s.scale[c + k];
-        split<P>(x[k], part[k]);
-    }
+    for (int k = 0; k < kPiece; ++k) split<P>(x[k], part[k]);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         u32x4 v;
@@ -103,13 +126,16 @@ __device__ void spread(const Source& s, int64_t block) {
 // others dy.
 template <class In, int P, bool ALONG>
 __global__ __launch_bounds__(256) void layout_kernel(Source held, Source dy) {
-    __shared__ uint16_t tile[ALONG ? 1 : P][64][66];
+    __shared__ union {
+        Tile<1, tile_cols<int8_t>()> held;
+        Tile<ALONG ? 1 : P, tile_cols<In>()> dy;
+    } tile;
     if (blockIdx.x < held.blocks)
-        transpose<int8_t, 1>(held, blockIdx.x, *reinterpret_cast<uint16_t(*)[1][64][66]>(tile));
+        transpose<int8_t, 1>(held, blockIdx.x, tile.held);
     else if constexpr (ALONG)
-        spread<In, P>(dy, blockIdx.x - held.blocks);
+        spread<In, P>(dy, blockIdx.x - (uint32_t)held.blocks);
     else
-        transpose<In, P>(dy, blockIdx.x - held.blocks, tile);
+        transpose<In, P>(dy, blockIdx.x - (uint32_t)held.blocks, tile.dy);
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(char* p, int64_t ld, int64_t R,
@@ -159,7 +185,7 @@ Layout layout(int64_t M, int64_t N, int64_t R, bool dy_bf16, bool out_bf16, bool
     return l;
 }
 int64_t workspace_of(const Layout& l, int64_t M, int64_t N) {
-    return l.dy_bytes + l.held_bytes + slices_bytes(M, N, l.Rp / kRound * l.parts);
+    return l.dy_bytes + l.held_bytes + slices_bytes(M, N, l.Rp / kRound, l.parts);
 }
 
 // c [M x N] = the sum over R of dy, which has its rows, and the 8-bit operand,
@@ -173,7 +199,7 @@ int gradient(Mat dy, Held held, int64_t R, int64_t M, int64_t N, Mat c, void* wo
              reinterpret_cast<uint16_t*>(ws + l.dy_bytes), l.Rp, 0};
     Source d{dy.p, dy.ld, l.held_scaled ? nullptr : held.scale, ALONG ? M : R, ALONG ? R : M,
              reinterpret_cast<uint16_t*>(ws), l.Rp, 0};
-    if (!l.held_as_is) h.blocks = l.Rp / 64 * up(N, 64);
+    if (!l.held_as_is) h.blocks = l.Rp / 64 * up(N, tile_cols<int8_t>());
     if (!l.dy_as_is) d.blocks = ALONG ? up(M * (l.Rp / kPiece), 256) : l.Rp / 64 * up(M, 64);
     if (h.blocks + d.blocks > 0) {
         if ((h.blocks + d.blocks) * 256 >= (int64_t)1 << 32) return (int)hipErrorInvalidValue;
@@ -203,8 +229,10 @@ int gradient(Mat dy, Held held, int64_t R, int64_t M, int64_t N, Mat c, void* wo
     t.ldc = c.ld;
     t.bf16 = c.bf16;
     void* slices = ws + l.dy_bytes + l.held_bytes;
-    return l.held_as_is ? launch_grad_gemm<!ALONG, true>(o, t, slices, stream)
-                        : launch_grad_gemm<false, false>(o, t, slices, stream);
+    if (l.held_as_is) return launch_grad_gemm<!ALONG, true, 1>(o, t, slices, stream);
+    if (l.parts == 1) return launch_grad_gemm<false, false, 1>(o, t, slices, stream);
+    return l.parts == 2 ? launch_grad_gemm<false, false, 2>(o, t, slices, stream)
+                        : launch_grad_gemm<false, false, 3>(o, t, slices, stream);
 }
 
 }  // namespace

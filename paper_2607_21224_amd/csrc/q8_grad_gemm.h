@@ -2,9 +2,10 @@
 //   C[m, n] = sum over r of A[m, r] B[n, r]
 // Each operand is laid out, bf16 with r contiguous, or read as it is, its rows
 // running across the sum (DOWN):
-//   A   a bf16 matrix [R x M]; or laid out in `parts` passes, whose sum is A
+//   A   a bf16 matrix [R x M]; or laid out in `parts`, whose sum is A: P of them
+//       taken in one pass, all P by the same B, or one a pass
 //   B   the 8-bit operand [R x N], scaled by row and rounded to bf16 on its way; or
-//       laid out, the same for every pass
+//       laid out, the same for every part
 //
 // The loop is that of Gemm (q8_gemm.h): steps of 64 values of r go from memory
 // straight into one of two LDS buffers, half a step is in registers, one barrier a
@@ -46,18 +47,19 @@ struct GradOperands {
 // What a lane reads for rows that are not there.
 __device__ __attribute__((aligned(16))) const uint32_t kNothing[4] = {0, 0, 0, 0};
 
-template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN>
+template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P>
 struct GradGemm {
     using G = Gemm<Bf16, BM, BN, WM, WN>;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
     static_assert(!BDOWN || NT == 4, "4 columns of B a lane");
     static_assert(BDOWN || !ADOWN, "as it is, A meets B as it is");
+    static_assert(P == 1 || !BDOWN, "parts are laid out");
     static constexpr int kRows = kStep / 2;  // of a step
-    static constexpr int kA = BM * kStep, kB = BDOWN ? kRows * BN : BN * kStep;
+    static constexpr int kPart = BM * kStep, kA = P * kPart, kB = BDOWN ? kRows * BN : BN * kStep;
     static constexpr int kBuffer = kA + kB + (BDOWN ? 256 : 0);
-    static constexpr int kLoadsA = kA / 1024 / kWaves, kLoadsB = kB / 1024 / kWaves;
-    static_assert(kLoadsA * kWaves * 1024 == kA && kLoadsB * kWaves * 1024 == kB, "whole loads");
+    static constexpr int kLoadsA = kPart / 1024 / kWaves, kLoadsB = kB / 1024 / kWaves;
+    static_assert(kLoadsA * kWaves * 1024 == kPart && kLoadsB * kWaves * 1024 == kB, "whole loads");
 
     // B: the row of a step at place s of LDS, and the exchange of its pieces.  A read
     // takes 64 bytes of each of 4 places: they have to fill 256 bytes together.
@@ -74,9 +76,9 @@ struct GradGemm {
     }
 
     struct Half {
-        u32x4 a[MT], b[NT];  // operands
-        uint32_t q[8];       // DOWN B, as it is: 8 rows of 4 columns,
-        f32x4 s[2];          // and their scales
+        u32x4 a[P][MT], b[NT];  // operands
+        uint32_t q[8];          // DOWN B, as it is: 8 rows of 4 columns,
+        f32x4 s[2];             // and their scales
     };
     // 32-bit offsets of a lane's loads from the tile's first row (DOWN: the step's
     // first row, the tile's first column).  Rows of C, and DOWN pieces of columns,
@@ -126,15 +128,18 @@ struct GradGemm {
     // Sends for a step that begins at a, b and `scale`; `rows` of its 64 rows are
     // there, all of them unless LAST.
     template <bool LAST>
-    static __device__ __forceinline__ void fetch(const char* a, const char* b, const float* scale,
-                                                 int64_t rows, const Offsets& l, char* lds,
-                                                 int wave, int lane) {
+    static __device__ __forceinline__ void fetch(const char* a, int64_t a_part, const char* b,
+                                                 const float* scale, int64_t rows,
+                                                 const Offsets& l, char* lds, int wave, int lane) {
         const char* nothing = reinterpret_cast<const char*>(kNothing);
 #pragma unroll
-        for (int j = 0; j < kLoadsA; ++j) {
-            const bool there = !LAST || !ADOWN || row_a(j, wave, lane) < rows;
-            to_lds(there ? a + l.a[j] : nothing, lds + (j * kWaves + wave) * 1024);
-        }
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int j = 0; j < kLoadsA; ++j) {
+                const bool there = !LAST || !ADOWN || row_a(j, wave, lane) < rows;
+                to_lds(there ? a + p * a_part + l.a[j] : nothing,
+                       lds + p * kPart + (j * kWaves + wave) * 1024);
+            }
 #pragma unroll
         for (int j = 0; j < kLoadsB; ++j) {
             const bool there = !LAST || !BDOWN || row_at(place_of_b(j, wave, lane)) < rows;
@@ -194,10 +199,12 @@ struct GradGemm {
                 // that count, so it is flipped in rather than added)
                 const char* p = lds + (t.a ^ i << 5) + half * 32 * BM * 2;
                 const u32x2 lo = read_down(p), hi = read_down(p + 4 * BM * 2);
-                h.a[i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                h.a[0][i] = u32x4{lo[0], lo[1], hi[0], hi[1]};
             } else {
-                h.a[i] = *reinterpret_cast<const u32x4*>(lds + t.a + i * 16 * kStep +
-                                                         (t.swap ^ (half << 6)));
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    h.a[p][i] = *reinterpret_cast<const u32x4*>(
+                        lds + p * kPart + t.a + i * 16 * kStep + (t.swap ^ (half << 6)));
             }
         }
     }
@@ -227,15 +234,18 @@ struct GradGemm {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) acc[i][j] = Bf16::mfma(h.b[j], h.a[i], acc[i][j]);
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+                    acc[i][j] = Bf16::mfma(h.b[j], h.a[p][i], acc[i][j]);
     }
 
     // (see Gemm) spreads the reads, and LOADS loads, over the matrix instructions
     template <int LOADS>
     static __device__ __forceinline__ void spread() {
         if constexpr (BDOWN) return;
-        constexpr int kReads = MT + NT;
-        constexpr int kEach = MT * NT / kReads > 0 ? MT * NT / kReads : 1;
+        constexpr int kReads = P * MT + NT;
+        constexpr int kEach = P * MT * NT / kReads > 0 ? P * MT * NT / kReads : 1;
 #pragma unroll
         for (int i = 0; i < kReads; ++i) {
             if (i < LOADS) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);  // a load
@@ -256,13 +266,13 @@ struct GradGemm {
         const char* b0 = o.b + (BDOWN ? tile.n : tile.n * o.ldb);
         const int64_t a_step = ADOWN ? kRows * o.lda : kStep;
         const int64_t b_step = BDOWN ? kRows * o.ldb : kStep;
-        const int steps = o.steps * o.parts;
+        const int passes = o.parts / P, steps = o.steps * passes;
         const int k0 = (int)((int64_t)steps * tile.slice / slices);
         const int k1 = (int)((int64_t)steps * (tile.slice + 1) / slices);
         int pass = k0 / o.steps, in_pass = k0 - pass * o.steps;
         // sends for the next step; LAST: it may be the last one, of fewer rows
         const auto send = [&](char* buffer, auto last) {
-            fetch<last>(a0 + pass * o.a_part + in_pass * a_step, b0 + in_pass * b_step,
+            fetch<last>(a0 + pass * o.a_part + in_pass * a_step, o.a_part, b0 + in_pass * b_step,
                         o.scale + (int64_t)in_pass * kRows, o.R - (int64_t)in_pass * kRows, l,
                         buffer, wave, lane);
             const bool wrap = ++in_pass == o.steps;
@@ -297,7 +307,7 @@ struct GradGemm {
             if constexpr (kAhead >= 1) read(h0, then, at_, 0);
             multiply(h1, acc);
             if constexpr (kAhead >= 1) {
-                spread<kAhead >= 2 ? kLoadsA + kLoadsB : 0>();
+                spread<kAhead >= 2 ? P * kLoadsA + kLoadsB : 0>();
                 convert(h0);
             }
         };
@@ -337,34 +347,35 @@ struct GradGemm {
     }
 };
 
-template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN>
+template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P>
 __global__ __launch_bounds__(64 * WM * WN) void grad_gemm_kernel(GradOperands o, Target t,
                                                                  int64_t tiles_m, int64_t tiles_n,
                                                                  int slices) {
-    GradGemm<BM, BN, WM, WN, ADOWN, BDOWN>::run(o, t, tiles_m, tiles_n, slices);
+    GradGemm<BM, BN, WM, WN, ADOWN, BDOWN, P>::run(o, t, tiles_m, tiles_n, slices);
 }
 
-template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN>
+template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P>
 int launch_grad_tiles(const GradOperands& o, const Target& t, int slices, void* stream) {
     const int64_t tm = up(o.M, BM), tn = up(o.N, BN);
     if (tm * tn * slices * 64 * WM * WN >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
-    return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN>,
+    return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P>,
                   dim3((uint32_t)(tm * tn * slices)), 64 * WM * WN, stream, o, t, tm, tn, slices);
 }
 
-template <bool ADOWN, bool BDOWN>
+template <bool ADOWN, bool BDOWN, int P>
 int launch_grad_gemm(const GradOperands& o, Target t, void* ws, void* stream) {
-    const Shape s = shape_of(o.M, o.N, (int64_t)o.steps * o.parts);
+    const Shape s = shape_of(o.M, o.N, o.steps, P);
     t.ws = ws;
     t.ldws = slices_ld(o.N);
     t.slice = o.M * t.ldws;
-    // (as it is, the 8-bit operand of dx meets at most 128 rows: never this tile)
+    // (as it is, the 8-bit operand of dx meets at most 128 rows: never this tile.
+    // Its LDS holds one part.)
     if constexpr (ADOWN || !BDOWN)
-        if (s.tile == 256) return launch_grad_tiles<256, 256, 2, 4, ADOWN, BDOWN>(o, t, 1, stream);
-    if (s.tile >= 128) return launch_grad_tiles<128, 128, 2, 2, ADOWN, BDOWN>(o, t, 1, stream);
+        if (s.tile == 256) return launch_grad_tiles<256, 256, 2, 4, ADOWN, BDOWN, 1>(o, t, 1, stream);
+    if (s.tile >= 128) return launch_grad_tiles<128, 128, 2, 2, ADOWN, BDOWN, P>(o, t, 1, stream);
     // (a DOWN B is read 4 columns a lane: 64 a wavefront)
     constexpr int WM = BDOWN ? 4 : 2;
-    if (int e = launch_grad_tiles<64, 64, WM, 4 / WM, ADOWN, BDOWN>(o, t, s.slices, stream))
+    if (int e = launch_grad_tiles<64, 64, WM, 4 / WM, ADOWN, BDOWN, P>(o, t, s.slices, stream))
         return e;
     if (s.slices == 1) return 0;
     return launch_join<Bf16>(t, o.M, o.N, s.slices, stream);
