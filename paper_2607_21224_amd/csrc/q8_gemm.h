@@ -4,8 +4,10 @@
 //
 // A block computes a BM x BN tile of C with WM x WN wavefronts.  It walks K in
 // steps of 128 bytes a row; the step's rows of A and B go from memory straight
-// into one of two LDS buffers (16 bytes a lane, no registers in between) while
-// the matrix cores work on the other.  The 16-byte pieces of a row are stored
+// into one of S LDS buffers (16 bytes a lane, no registers in between) while the
+// matrix cores work on another.  Two buffers do where a CU has several blocks, or a
+// step's work takes as long as its loads; with a block a CU or two, small tiles have
+// four, so that loads are sent for three steps ahead.  The 16-byte pieces of a row are stored
 // permuted (piece p of row r at place p ^ f(r)), so that the 16 lanes that read
 // the same piece of 16 rows touch all 64 banks.  The permutation is applied to
 // the address that a lane loads from; a row's 128 bytes stay one request.
@@ -47,16 +49,13 @@ struct Bf16 {
     }
 };
 
-// Operands of a product.  K runs over `parts` passes of `row` bytes each (row a
-// multiple of kStep where parts > 1); pass p reads A at a + p a_part and the same B.
+// Operands of a product.
 struct Operands {
     const char* a;
     const char* b;
     int64_t lda, ldb;  // bytes from row to row, below 2^23
-    int64_t a_part;
     int64_t M, N;
-    int row;    // bytes of a row that are there
-    int parts;
+    int row;  // bytes of a row that are there
 };
 
 // Where the sums of a product go: C in its own type, or (slices > 1) the sums of
@@ -77,12 +76,23 @@ __device__ __forceinline__ void to_lds(const char* src, char* dst) {
         (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
 }
 
-// Waits until at most N of the wavefront's loads are on their way.
+// Waits until at most N of the wavefront's loads are on their way, and all that it
+// reads from LDS has come.
 template <int N>
 __device__ __forceinline__ void wait_loads() {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);
     asm volatile("" ::: "memory");
+}
+// The same for the loads of `steps` (at most MOST) steps, EACH of a step.
+template <int MOST, int EACH>
+__device__ __forceinline__ void wait_steps(int steps) {
+    if constexpr (MOST == 0) {
+        wait_loads<0>();
+    } else {
+        if (steps >= MOST) wait_loads<MOST * EACH>();
+        else wait_steps<MOST - 1, EACH>(steps);
+    }
 }
 // A barrier that waits for no load (the caller has waited for those it needs).
 __device__ __forceinline__ void barrier() {
@@ -166,7 +176,7 @@ __device__ __forceinline__ TileAt tile_at(int64_t tiles_m, int64_t tiles_n, int 
     return {(band * 8 + in % high) * BM, in / high * BN, (int)slice};
 }
 
-template <class Op, int BM, int BN, int WM, int WN>
+template <class Op, int BM, int BN, int WM, int WN, int S>
 struct Gemm {
     static constexpr int kWaves = WM * WN;
     static constexpr int kThreads = 64 * kWaves;
@@ -268,7 +278,7 @@ struct Gemm {
 
     static __device__ void run(const Operands& o, const Target& t, int64_t tiles_m,
                                int64_t tiles_n, int slices) {
-        __shared__ __attribute__((aligned(1024))) char lds[2 * kBuffer];
+        __shared__ __attribute__((aligned(1024))) char lds[S * kBuffer];
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int lane = threadIdx.x & 63;
         const TileAt tile = tile_at(tiles_m, tiles_n, BM, BN);
@@ -276,10 +286,9 @@ struct Gemm {
         const char* a0 = o.a + tile.m * o.lda;
         const char* b0 = o.b + tile.n * o.ldb;
 
-        // whole steps of this slice: k0 to k1 of parts * per_part, and the short
-        // one at the end of the last slice
-        const int per_part = o.row / kStep, tail = o.row % kStep;
-        const int steps = per_part * o.parts;
+        // whole steps of this slice: k0 to k1, and the short one at the end of the
+        // last slice
+        const int steps = o.row / kStep, tail = o.row % kStep;
         const int k0 = (int)((int64_t)steps * tile.slice / slices);
         const int k1 = (int)((int64_t)steps * (tile.slice + 1) / slices);
 
@@ -289,60 +298,59 @@ struct Gemm {
         const int off_b = BM * kStep + (wn * NT * 16 + (r >> 2) * 4 * NT + (r & 3)) * kStep;
         const int swap = (g ^ (r >> 1)) << 4;
 
-        // Two steps are on their way or in LDS, and half a step in registers.  A
+        // Up to S steps are on their way or in LDS, and half a step in registers.  A
         // step's first half is multiplied while its second is read; then, its LDS
-        // buffer done with, one barrier, and the step after next is sent for into
-        // that buffer while the second half is multiplied and the next step's
-        // first is read.
-        int part_at = k0 / (per_part > 0 ? per_part : 1), at = k0 - part_at * per_part;
-        const char* a_at = a0 + part_at * o.a_part + (int64_t)at * kStep;
-        const char* b_at = b0 + (int64_t)at * kStep;
-        const int64_t a_jump = o.a_part - o.row;
-        const auto next = [&] {
-            const bool wrap = ++at == per_part;
-            at = wrap ? 0 : at;
-            a_at += wrap ? kStep + a_jump : kStep;
-            b_at += wrap ? kStep - o.row : kStep;
+        // buffer done with, one barrier, and the step S on is sent for into that
+        // buffer while the second half is multiplied and the next step's first is
+        // read.
+        const char* a_at = a0 + (int64_t)k0 * kStep;
+        const char* b_at = b0 + (int64_t)k0 * kStep;
+        const auto send = [&](int k) {
+            fetch(a_at, b_at, l, lds + (k - k0) % S * kBuffer, wave);
+            a_at += kStep;
+            b_at += kStep;
         };
         Half h0, h1;
         if (k0 < k1) {
-            fetch(a_at, b_at, l, lds, wave);
-            next();
-            if (k0 + 1 < k1) fetch(a_at, b_at, l, lds + kBuffer, wave);
-            next();
-            // the first of the two: the second one's loads may still be on their way
-            if (k0 + 1 < k1) wait_loads<kLoadsA + kLoadsB>();
-            else wait_loads<0>();
+#pragma unroll
+            for (int i = 0; i < S; ++i)
+                if (k0 + i < k1) send(k0 + i);
+            // the first step has come, later ones may be on their way
+            wait_steps<S - 1, kLoadsA + kLoadsB>(k1 - k0 - 1);
             barrier();
             read(h0, lds + off_a, lds + off_b, 0, swap);
         }
-        // one step; FETCH: there is a step after next, READ: there is a next one
-        const auto step = [&](int k, auto fetch_on, auto read_on) {
-            char* now = lds + ((k - k0) & 1) * kBuffer;
-            char* then = lds + ((k - k0 + 1) & 1) * kBuffer;
+        // one step; `ahead` steps (S: or more) come after it
+        const auto step = [&](int k, auto ahead) {
+            constexpr int kAhead = ahead;
+            char* now = lds + (k - k0) % S * kBuffer;
+            char* then = lds + (k - k0 + 1) % S * kBuffer;
             read(h1, now + off_a, now + off_b, 1, swap);
             multiply(h0, acc);
             spread<0>();
-            wait_loads<0>();
-            __syncthreads();
-            if constexpr (fetch_on) {
-                fetch(a_at, b_at, l, now, wave);
-                next();
-            }
-            if constexpr (read_on) read(h0, then + off_a, then + off_b, 0, swap);
+            // the next step has come, and `now` has been read
+            wait_loads<(kAhead >= S ? S - 2 : kAhead >= 2 ? kAhead - 1 : 0) *
+                       (kLoadsA + kLoadsB)>();
+            barrier();
+            if constexpr (kAhead >= S) send(k + S);
+            if constexpr (kAhead >= 1) read(h0, then + off_a, then + off_b, 0, swap);
             multiply(h1, acc);
-            if constexpr (read_on) spread<fetch_on ? kLoadsA + kLoadsB : 0>();
+            if constexpr (kAhead >= 1) spread<kAhead >= S ? kLoadsA + kLoadsB : 0>();
         };
         int k = k0;
-        for (; k < k1 - 2; ++k) step(k, std::true_type(), std::true_type());
-        if (k < k1 - 1) step(k++, std::false_type(), std::true_type());
-        if (k < k1) step(k, std::false_type(), std::false_type());
+        for (; k < k1 - S; ++k) step(k, Int<S>());
+        if constexpr (S > 3)
+            if (k < k1 - 3) step(k++, Int<3>());
+        if constexpr (S > 2)
+            if (k < k1 - 2) step(k++, Int<2>());
+        if (k < k1 - 1) step(k++, Int<1>());
+        if (k < k1) step(k, Int<0>());
         if (tail != 0 && tile.slice == slices - 1) {
-            // no load is on its way, and all wavefronts are past their last read
-            // of both buffers but the last step's, whose reads the barrier follows
-            char* now = lds + ((k1 - k0) & 1) * kBuffer;
-            fetch_tail(a0 + (int64_t)per_part * kStep, b0 + (int64_t)per_part * kStep, l, now, wave,
-                       lane, tail, per_part * kStep);
+            // no load is on its way, and all wavefronts are past their reads of every
+            // buffer but the last step's
+            char* now = lds + (k1 - k0) % S * kBuffer;
+            fetch_tail(a0 + (int64_t)steps * kStep, b0 + (int64_t)steps * kStep, l, now, wave, lane,
+                       tail, steps * kStep);
             __syncthreads();
             read(h0, now + off_a, now + off_b, 0, swap);
             read(h1, now + off_a, now + off_b, 1, swap);
@@ -386,10 +394,10 @@ struct Gemm {
     }
 };
 
-template <class Op, int BM, int BN, int WM, int WN>
+template <class Op, int BM, int BN, int WM, int WN, int S>
 __global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(Operands o, Target t, int64_t tiles_m,
                                                             int64_t tiles_n, int slices) {
-    Gemm<Op, BM, BN, WM, WN>::run(o, t, tiles_m, tiles_n, slices);
+    Gemm<Op, BM, BN, WM, WN, S>::run(o, t, tiles_m, tiles_n, slices);
 }
 
 // Joins the slices of a product in their order: 4 columns a thread.
@@ -471,13 +479,21 @@ inline int64_t slices_bytes(int64_t M, int64_t N, int64_t steps, int parts = 1) 
     return s.slices == 1 ? 0 : s.slices * M * slices_ld(N) * 4;
 }
 
+// Whether all blocks of a launch are on the card at once, each with `bytes` of LDS.
+inline bool all_at_once(int64_t blocks, int bytes) { return blocks <= 256 * (160 * 1024 / bytes); }
+
 template <class Op, int BM, int BN, int WM, int WN>
 int launch_tiles(const Operands& o, const Target& t, int slices, void* stream) {
-    const int64_t tm = up(o.M, BM), tn = up(o.N, BN);
+    const int64_t tm = up(o.M, BM), tn = up(o.N, BN), blocks = tm * tn * slices;
     // (work items of a launch stay below 2^32)
-    if (tm * tn * slices * 64 * WM * WN >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
-    return launch(gemm_kernel<Op, BM, BN, WM, WN>, dim3((uint32_t)(tm * tn * slices)),
-                  64 * WM * WN, stream, o, t, tm, tn, slices);
+    if (blocks * 64 * WM * WN >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
+    const dim3 grid((uint32_t)blocks);
+    if constexpr (BM < 256)
+        if (all_at_once(blocks, Gemm<Op, BM, BN, WM, WN, 4>::kBuffer * 4))
+            return launch(gemm_kernel<Op, BM, BN, WM, WN, 4>, grid, 64 * WM * WN, stream, o, t, tm,
+                          tn, slices);
+    return launch(gemm_kernel<Op, BM, BN, WM, WN, 2>, grid, 64 * WM * WN, stream, o, t, tm, tn,
+                  slices);
 }
 
 template <class Op>
@@ -489,7 +505,7 @@ int launch_join(const Target& t, int64_t M, int64_t N, int slices, void* stream)
 
 template <class Op>
 int launch_gemm(const Operands& o, Target t, void* ws, void* stream) {
-    const Shape s = shape_of(o.M, o.N, (int64_t)(o.row / kStep) * o.parts);
+    const Shape s = shape_of(o.M, o.N, o.row / kStep);
     t.ws = ws;
     t.ldws = slices_ld(o.N);
     t.slice = o.M * t.ldws;

@@ -8,7 +8,7 @@
 //       laid out, the same for every part
 //
 // The loop is that of Gemm (q8_gemm.h): steps of 64 values of r go from memory
-// straight into one of two LDS buffers, half a step is in registers, one barrier a
+// straight into one of S LDS buffers, half a step is in registers, one barrier a
 // step.  What differs is how a DOWN operand leaves LDS, where r runs down the
 // buffer and an instruction wants 8 values of r from each lane, for one row of its
 // operand.
@@ -47,9 +47,9 @@ struct GradOperands {
 // What a lane reads for rows that are not there.
 __device__ __attribute__((aligned(16))) const uint32_t kNothing[4] = {0, 0, 0, 0};
 
-template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P>
+template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P, int S>
 struct GradGemm {
-    using G = Gemm<Bf16, BM, BN, WM, WN>;
+    using G = Gemm<Bf16, BM, BN, WM, WN, 2>;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
     static constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
     static_assert(!BDOWN || NT == 4, "4 columns of B a lane");
@@ -256,7 +256,7 @@ struct GradGemm {
 
     static __device__ void run(const GradOperands& o, const Target& t, int64_t tiles_m,
                                int64_t tiles_n, int slices) {
-        __shared__ __attribute__((aligned(1024))) char lds[2 * kBuffer];
+        __shared__ __attribute__((aligned(1024))) char lds[S * kBuffer];
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int lane = threadIdx.x & 63;
         const TileAt tile = tile_at(tiles_m, tiles_n, BM, BN);
@@ -283,41 +283,53 @@ struct GradGemm {
         const At at_ = at(wave, lane);
         f32x4 acc[MT][NT] = {};
         Half h0, h1;
+        // loads of a step; the first wavefront has the scales too
+        constexpr int kLoads = P * kLoadsA + kLoadsB;
+        const auto wait = [&](auto steps) {
+            if (BDOWN && wave == 0) wait_loads<steps * (kLoads + 1)>();
+            else wait_loads<steps * kLoads>();
+        };
         if (k0 < k1) {
-            send(lds, std::true_type());
-            wait_loads<0>();
-            if (k0 + 1 < k1) send(lds + kBuffer, std::true_type());
+#pragma unroll
+            for (int i = 0; i < S; ++i)
+                if (k0 + i < k1) send(lds + i * kBuffer, std::true_type());
+            if (BDOWN && wave == 0) wait_steps<S - 1, kLoads + 1>(k1 - k0 - 1);
+            else wait_steps<S - 1, kLoads>(k1 - k0 - 1);
             barrier();
             read(h0, lds, at_, 0);
             convert(h0);
         }
-        // one step; `ahead`: steps that come after it, of which 2 is one that has all
-        // its rows, 3 one that may not
+        // one step; `ahead` steps (S: or more) come after it, S + 1: the step S on may
+        // be the last, of fewer rows
         const auto step = [&](int k, auto ahead) {
             constexpr int kAhead = ahead;
-            char* now = lds + ((k - k0) & 1) * kBuffer;
-            char* then = lds + ((k - k0 + 1) & 1) * kBuffer;
+            char* now = lds + (k - k0) % S * kBuffer;
+            char* then = lds + (k - k0 + 1) % S * kBuffer;
             read(h1, now, at_, 1);
             multiply(h0, acc);
             spread<0>();
             convert(h1);
-            wait_loads<0>();
-            __syncthreads();
-            if constexpr (kAhead >= 2) send(now, std::integral_constant<bool, kAhead == 3>());
+            wait(Int<(kAhead >= S ? S - 2 : kAhead >= 2 ? kAhead - 1 : 0)>());
+            barrier();
+            if constexpr (kAhead >= S) send(now, std::integral_constant<bool, (kAhead > S)>());
             if constexpr (kAhead >= 1) read(h0, then, at_, 0);
             multiply(h1, acc);
             if constexpr (kAhead >= 1) {
-                spread<kAhead >= 2 ? P * kLoadsA + kLoadsB : 0>();
+                spread<kAhead >= S ? kLoads : 0>();
                 convert(h0);
             }
         };
         int k = k0;
         if constexpr (ADOWN || BDOWN) {
-            for (; k < k1 - 3; ++k) step(k, Int<2>());
-            if (k < k1 - 2) step(k++, Int<3>());
+            for (; k < k1 - S - 1; ++k) step(k, Int<S>());
+            if (k < k1 - S) step(k++, Int<S + 1>());
         } else {
-            for (; k < k1 - 2; ++k) step(k, Int<2>());
+            for (; k < k1 - S; ++k) step(k, Int<S>());
         }
+        if constexpr (S > 3)
+            if (k < k1 - 3) step(k++, Int<3>());
+        if constexpr (S > 2)
+            if (k < k1 - 2) step(k++, Int<2>());
         if (k < k1 - 1) step(k++, Int<1>());
         if (k < k1) step(k, Int<0>());
 
@@ -347,19 +359,25 @@ struct GradGemm {
     }
 };
 
-template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P>
+template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P, int S>
 __global__ __launch_bounds__(64 * WM * WN) void grad_gemm_kernel(GradOperands o, Target t,
                                                                  int64_t tiles_m, int64_t tiles_n,
                                                                  int slices) {
-    GradGemm<BM, BN, WM, WN, ADOWN, BDOWN, P>::run(o, t, tiles_m, tiles_n, slices);
+    GradGemm<BM, BN, WM, WN, ADOWN, BDOWN, P, S>::run(o, t, tiles_m, tiles_n, slices);
 }
 
 template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P>
 int launch_grad_tiles(const GradOperands& o, const Target& t, int slices, void* stream) {
-    const int64_t tm = up(o.M, BM), tn = up(o.N, BN);
-    if (tm * tn * slices * 64 * WM * WN >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
-    return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P>,
-                  dim3((uint32_t)(tm * tn * slices)), 64 * WM * WN, stream, o, t, tm, tn, slices);
+    const int64_t tm = up(o.M, BM), tn = up(o.N, BN), blocks = tm * tn * slices;
+    if (blocks * 64 * WM * WN >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
+    const dim3 grid((uint32_t)blocks);
+    constexpr int kDeep = 4 * GradGemm<BM, BN, WM, WN, ADOWN, BDOWN, P, 4>::kBuffer;
+    if constexpr (BM < 256 && kDeep <= 160 * 1024)
+        if (all_at_once(blocks, kDeep))
+            return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, 4>, grid,
+                          64 * WM * WN, stream, o, t, tm, tn, slices);
+    return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, 2>, grid, 64 * WM * WN, stream,
+                  o, t, tm, tn, slices);
 }
 
 template <bool ADOWN, bool BDOWN, int P>

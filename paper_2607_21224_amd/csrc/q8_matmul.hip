@@ -128,7 +128,6 @@ int launch_matmul(Held a, Held b, int64_t M, int64_t N, int64_t K, Mat y, void* 
     o.M = M;
     o.N = N;
     o.row = (int)K;
-    o.parts = 1;
     return launch_gemm<Int8>(o, t, workspace, stream);
 }
 
