@@ -9,9 +9,11 @@ Submodules
   multi  the same for a model held as separate tensors (multi-tensor plans)
   q8     ctypes binding of include/cpdp_q8.h (libcpdp_q8.so): norm, products and
          activations on rows of 8-bit numbers, and their backward passes
+  layer  the MLP half of a transformer block on that path, with its weights and
+         gradients in replica rows
   build  hipcc build of the shared libraries
 
 Importing ``cpdp`` or ``q8`` (directly or through ``state``) raises ImportError
 when its HIP library is not built: there is no CPU fallback.
 """
-__all__ = ["cpdp", "state", "multi", "q8", "build"]
+__all__ = ["cpdp", "state", "multi", "q8", "layer", "build"]

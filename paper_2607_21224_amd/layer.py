@@ -1,0 +1,168 @@
+"""The MLP half of a transformer block on the 8-bit activation path, trained by the
+CPDP steps.
+
+``Q8Mlp`` holds no weights: they are slices of a replica's row of
+``CpdpState.params``, and its gradients go into the same slices of a row of
+gradients, so one model of any number of such layers is one row.  A layer's
+forward pass keeps one byte an activation for its backward pass (``Saved``), a
+quarter of fp32 and half of bf16, for each of the replicas on the GPU::
+
+    mlp = Q8Mlp(dim=384, hidden=1536)
+    st = CpdpState(W=8, P=mlp.numel, K=4)
+    st.init(theta0)                            # (P,) fp32: mlp.init(generator)
+    grads = torch.zeros((8, st.ld), device="cuda")
+    saved = mlp.saved(tokens)
+    for t in range(1, T + 1):
+        for i in range(8):
+            mlp.forward(st.params[i], x[i], saved)     # saved.y
+            dy = ...                                   # the loss' gradient of saved.y
+            mlp.backward(st.params[i], dy, saved, grads[i])
+        st.step(t, grads, hyper, T)
+
+Forward, with `8(.)` for rounding to 8-bit rows (cpdp_q8.h):
+    h = x + residual;  n = 8(norm(h) * w);  z = n 8(W1)^T;  a = 8(act(z))
+    y = a 8(W2)^T
+Backward passes gradients through the roundings unchanged, and uses the rounded
+operands.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import q8
+from .state import round_up
+
+_DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+class Saved:
+    """What a forward pass over `T` tokens leaves for its backward pass, and the
+    tensors both write; it serves one replica after another."""
+
+    def __init__(self, mlp: "Q8Mlp", T: int, device="cuda"):
+        def rows(r, c, dt=mlp.act_dtype):
+            return q8.empty_rows(r, c, dt, device)
+
+        def vec(n):
+            return torch.empty(n, device=device)
+
+        D, F, i8 = mlp.dim, mlp.hidden, torch.int8
+        self.T = T
+        # one byte an activation: the norm's output, the activation's inputs and
+        # output, and the weights as they were used
+        self.n, self.n_scale, self.rstd = rows(T, D, i8), vec(T), vec(T)
+        self.cg, self.g_scale = rows(T, F, i8), vec(T)
+        self.cu, self.u_scale = (rows(T, F, i8), vec(T)) if mlp.gated else (None, None)
+        self.a, self.a_scale = rows(T, F, i8), vec(T)
+        self.w1 = [(rows(F, D, i8), vec(F)) for _ in range(2 if mlp.gated else 1)]
+        self.w2 = rows(D, F, i8), vec(D)
+        # the sum that the norm is taken of, the result, and what lives for a while
+        self.h, self.y, self.dx = rows(T, D), rows(T, D), rows(T, D)
+        self.z = [rows(T, F) for _ in range(2 if mlp.gated else 1)]
+        self.da, self.dn = rows(T, F), [rows(T, D) for _ in range(2 if mlp.gated else 1)]
+        self.workspace = torch.empty(mlp.workspace_bytes(T), dtype=torch.uint8, device=device)
+
+
+class Q8Mlp:
+    """dim -> hidden -> dim with a root-mean-square norm before it; kind "gelu", or
+    "swiglu" with two inner products."""
+
+    def __init__(self, dim: int, hidden: int, kind: str = "gelu", eps: float = 1e-6,
+                 act_dt: str = "bf16"):
+        if kind not in q8.ACTIVATIONS:
+            raise ValueError(f"kind must be one of {sorted(q8.ACTIVATIONS)}, got {kind!r}")
+        if act_dt not in _DT:
+            raise ValueError(f"act_dt must be 'f32' or 'bf16', got {act_dt!r}")
+        if dim % 8 or hidden % 8:
+            raise ValueError("dim and hidden must be multiples of 8: the weights' rows lie one "
+                             "after the other in a replica's row, each on a 16-byte boundary")
+        self.dim, self.hidden, self.kind, self.eps = int(dim), int(hidden), kind, float(eps)
+        self.gated = kind == "swiglu"
+        self.act_dtype = _DT[act_dt]
+        shapes = [("norm", (dim,)), ("w1", (hidden, dim))]
+        if self.gated:
+            shapes.append(("w1u", (hidden, dim)))
+        shapes.append(("w2", (dim, hidden)))
+        self.tensors, at = {}, 0
+        for name, shape in shapes:
+            n = shape[0] * (shape[1] if len(shape) == 2 else 1)
+            self.tensors[name] = (at, shape)
+            at = round_up(at + n, 8)
+        self.numel = at
+
+    def view(self, row: torch.Tensor, name: str) -> torch.Tensor:
+        """A tensor of the layer in a replica's row of parameters or gradients."""
+        at, shape = self.tensors[name]
+        n = shape[0] * (shape[1] if len(shape) == 2 else 1)
+        return row[at:at + n].view(shape)
+
+    def init(self, generator: torch.Generator | None = None, device="cuda") -> torch.Tensor:
+        """Initial parameters, (numel,) fp32: the norm's weight 1, the others normal
+        with the variance 1 / inputs."""
+        row = torch.zeros(self.numel, device=device)
+        self.view(row, "norm").fill_(1.0)
+        for name, (_, shape) in self.tensors.items():
+            if len(shape) == 2:
+                self.view(row, name).normal_(0.0, shape[1] ** -0.5, generator=generator)
+        return row
+
+    def saved(self, T: int, device="cuda") -> Saved:
+        return Saved(self, int(T), device)
+
+    def workspace_bytes(self, T: int) -> int:
+        """The largest workspace of the layer's calls over T tokens."""
+        D, F, dt = self.dim, self.hidden, self.act_dtype
+        need = [q8.cpdp_q8_matmul_workspace(T, F, D), q8.cpdp_q8_matmul_workspace(T, D, F),
+                q8.cpdp_q8_norm_bwd_workspace(T, D)]
+        for N, K in ((F, D), (D, F)):
+            need.append(q8.cpdp_q8_grad_input_workspace(T, N, K, dt, dt))
+            need += [q8.cpdp_q8_grad_weight_workspace(T, N, K, dt, g) for g in _DT.values()]
+        return max(need + [16])
+
+    def forward(self, params, x, saved: Saved, residual=None, stream=None) -> torch.Tensor:
+        """saved.y <- the layer's output for x (T, dim); params is a replica's row.
+        With a residual saved.h is x + residual, the residual of what follows."""
+        s = saved
+        if residual is None:
+            q8.cpdp_q8_norm(x, self.view(params, "norm"), self.eps, q=s.n, scale=s.n_scale,
+                            rstd=s.rstd, stream=stream)
+            s.norm_of = x
+        else:
+            q8.cpdp_q8_norm(x, self.view(params, "norm"), self.eps, q=s.n, scale=s.n_scale,
+                            rstd=s.rstd, residual=residual, h=s.h, stream=stream)
+            s.norm_of = s.h
+        for name, (w, scale), z in zip(("w1", "w1u"), s.w1, s.z):
+            q8.cpdp_q8_rows(self.view(params, name), w, scale, stream=stream)
+            q8.cpdp_q8_matmul(s.n, s.n_scale, w, scale, z, workspace=s.workspace, stream=stream)
+        q8.cpdp_q8_act(self.kind, *s.z, q=s.a, scale=s.a_scale, cg=s.cg, sg=s.g_scale, cu=s.cu,
+                       su=s.u_scale, stream=stream)
+        q8.cpdp_q8_rows(self.view(params, "w2"), *s.w2, stream=stream)
+        q8.cpdp_q8_matmul(s.a, s.a_scale, *s.w2, s.y, workspace=s.workspace, stream=stream)
+        return s.y
+
+    def backward(self, params, dy, saved: Saved, grads, dres=None, stream=None) -> torch.Tensor:
+        """The gradients of the last forward pass over `saved`, of the parameters
+        into `grads` (a replica's row) and of the input, returned; dres is what
+        reaches x + residual past the layer."""
+        s = saved
+        kw = {"workspace": s.workspace, "stream": stream}
+        q8.cpdp_q8_grad_weight(dy, s.a, s.a_scale, self.view(grads, "w2"), **kw)
+        q8.cpdp_q8_grad_input(dy, *s.w2, s.da, **kw)
+        # z is done with: its gradient takes its place
+        q8.cpdp_q8_act_bwd(self.kind, s.da, s.cg, s.g_scale, s.z[0], cu=s.cu, su=s.u_scale,
+                           du=s.z[1] if self.gated else None, stream=stream)
+        for name, w, dz, dn in zip(("w1", "w1u"), s.w1, s.z, s.dn):
+            q8.cpdp_q8_grad_weight(dz, s.n, s.n_scale, self.view(grads, name), **kw)
+            q8.cpdp_q8_grad_input(dz, *w, dn, **kw)
+        dn = s.dn[0]
+        if self.gated:
+            with torch.cuda.stream(_torch_stream(stream)):
+                dn.add_(s.dn[1])
+        q8.cpdp_q8_norm_bwd(dn, s.norm_of, self.view(params, "norm"), s.rstd, s.dx,
+                            self.view(grads, "norm"), dres=dres, **kw)
+        return s.dx
+
+
+def _torch_stream(stream):
+    """A stream argument for torch's own operations (None: the current one)."""
+    return torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
