@@ -435,7 +435,7 @@ __global__ __launch_bounds__(256) void join_kernel(Target t, int64_t M, int64_t 
 // ---- which tile takes a product ----------------------------------------------------
 
 struct Shape {
-    int tile;    // 256, 128 or 64
+    int bm, bn;  // 256 x 256, 256 x 128, 128 x 128 or 64 x 64
     int slices;  // of K
 };
 
@@ -443,29 +443,35 @@ inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // The tile and the slices of K that should take the least time.  A step of a
 // tile's block takes `least` ns while its CU has few others, and the CU gets
-// through one such step in `each` ns when it has many (measured on products of
-// 64 to 8192 rows with 4096 columns and K = 4096, where the best choice is taken
-// or missed by less than a tenth).  A step with several parts of A takes them one
-// after the other (256), or together, with the loads of B once.  Slices are added up by a second launch: its
-// start, and each sum written and read again at 3 TB/s.
+// through one such step in `each` ns when it has many.  Measured on int8 products
+// with N = K = 4096, in us, and the best taken:
+//   rows     256 x 256   256 x 128   128 x 128   64 x 64
+//   256          47          31          28         15
+//   1024         48          33          30         32
+//   2048         49          39          44         55
+//   4096         61          74          83        105
+// A step with several parts of A takes them one after the other (256), or together,
+// with the loads of B once.  Slices are added up by a second launch: its start, and
+// each sum written and read again at 3 TB/s.
 inline Shape shape_of(int64_t M, int64_t N, int64_t steps, int parts = 1) {
     const struct {
-        int tile, least, each;
-    } tiles[] = {{256, parts * 1500, parts * 1850},
-                 {128, 700 + 200 * parts, 640 * parts},
-                 {64, 600 + 100 * parts, 115 + 115 * parts}};
-    Shape best = {256, 1};
+        int bm, bn, least, each;
+    } tiles[] = {{256, 256, parts * 1350, parts * 1800},
+                 {256, 128, parts * 920, parts * 1100},
+                 {128, 128, 580 + 200 * parts, 230 + 390 * parts},
+                 {64, 64, 250 + 100 * parts, 105 + 115 * parts}};
+    Shape best = {256, 256, 1};
     double least = -1;
     for (const auto& t : tiles) {
-        const int64_t n = up(M, t.tile) * up(N, t.tile);
+        const int64_t n = up(M, t.bm) * up(N, t.bn);
         for (int slices = 1; slices <= 64; slices *= 2) {
-            if (slices > 1 && (t.tile != 64 || n * slices > 2048 || steps < 4 * slices)) break;
+            if (slices > 1 && (t.bm != 64 || n * slices > 2048 || steps < 4 * slices)) break;
             const double each = (double)up(n * slices, 256) * t.each;
             const double time = (double)up(steps, slices) * (each > t.least ? each : t.least) +
                                 (slices > 1 ? 4500.0 + slices * (double)M * (double)N / 375.0 : 0);
             if (least < 0 || time < least) {
                 least = time;
-                best = {t.tile, slices};
+                best = {t.bm, t.bn, slices};
             }
         }
     }
@@ -492,7 +498,8 @@ int launch_tiles(const Operands& o, const Target& t, int slices, void* stream) {
         if (all_at_once(blocks, Gemm<Op, BM, BN, WM, WN, 4>::kBuffer * 4))
             return launch(gemm_kernel<Op, BM, BN, WM, WN, 4>, grid, 64 * WM * WN, stream, o, t, tm,
                           tn, slices);
-    return launch(gemm_kernel<Op, BM, BN, WM, WN, 2>, grid, 64 * WM * WN, stream, o, t, tm, tn,
+    constexpr int S = BM + BN == 384 ? 3 : 2;
+    return launch(gemm_kernel<Op, BM, BN, WM, WN, S>, grid, 64 * WM * WN, stream, o, t, tm, tn,
                   slices);
 }
 
@@ -509,8 +516,9 @@ int launch_gemm(const Operands& o, Target t, void* ws, void* stream) {
     t.ws = ws;
     t.ldws = slices_ld(o.N);
     t.slice = o.M * t.ldws;
-    if (s.tile == 256) return launch_tiles<Op, 256, 256, 2, 4>(o, t, 1, stream);
-    if (s.tile == 128) return launch_tiles<Op, 128, 128, 2, 2>(o, t, 1, stream);
+    if (s.bn == 256) return launch_tiles<Op, 256, 256, 2, 4>(o, t, 1, stream);
+    if (s.bm == 256) return launch_tiles<Op, 256, 128, 4, 2>(o, t, 1, stream);
+    if (s.bm == 128) return launch_tiles<Op, 128, 128, 2, 2>(o, t, 1, stream);
     if (int e = launch_tiles<Op, 64, 64, 2, 2>(o, t, s.slices, stream)) return e;
     if (s.slices == 1) return 0;
     return launch_join<Op>(t, o.M, o.N, s.slices, stream);

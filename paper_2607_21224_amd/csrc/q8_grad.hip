@@ -185,7 +185,8 @@ Layout layout(int64_t M, int64_t N, int64_t R, bool dy_bf16, bool out_bf16, bool
     return l;
 }
 int64_t workspace_of(const Layout& l, int64_t M, int64_t N) {
-    return l.dy_bytes + l.held_bytes + slices_bytes(M, N, l.Rp / kRound, l.parts);
+    return l.dy_bytes + l.held_bytes +
+           slices_bytes(M, N, l.Rp / kRound, l.held_as_is ? kDownParts : l.parts);
 }
 
 // c [M x N] = the sum over R of dy, which has its rows, and the 8-bit operand,

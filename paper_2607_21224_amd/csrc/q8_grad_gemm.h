@@ -44,6 +44,10 @@ struct GradOperands {
     int steps, parts;  // steps of one pass: R / 64, rounded up
 };
 
+// A step of an 8-bit operand that is converted on its way takes about as long as one
+// of three parts (shape_of).
+constexpr int kDownParts = 3;
+
 // What a lane reads for rows that are not there.
 __device__ __attribute__((aligned(16))) const uint32_t kNothing[4] = {0, 0, 0, 0};
 
@@ -376,21 +380,24 @@ int launch_grad_tiles(const GradOperands& o, const Target& t, int slices, void* 
         if (all_at_once(blocks, kDeep))
             return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, 4>, grid,
                           64 * WM * WN, stream, o, t, tm, tn, slices);
-    return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, 2>, grid, 64 * WM * WN, stream,
+    constexpr int S = BM + BN == 384 ? 3 : 2;
+    return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, S>, grid, 64 * WM * WN, stream,
                   o, t, tm, tn, slices);
 }
 
 template <bool ADOWN, bool BDOWN, int P>
 int launch_grad_gemm(const GradOperands& o, Target t, void* ws, void* stream) {
-    const Shape s = shape_of(o.M, o.N, o.steps, P);
+    const Shape s = shape_of(o.M, o.N, o.steps, BDOWN ? kDownParts : P);
     t.ws = ws;
     t.ldws = slices_ld(o.N);
     t.slice = o.M * t.ldws;
     // (as it is, the 8-bit operand of dx meets at most 128 rows: never this tile.
     // Its LDS holds one part.)
-    if constexpr (ADOWN || !BDOWN)
-        if (s.tile == 256) return launch_grad_tiles<256, 256, 2, 4, ADOWN, BDOWN, 1>(o, t, 1, stream);
-    if (s.tile >= 128) return launch_grad_tiles<128, 128, 2, 2, ADOWN, BDOWN, P>(o, t, 1, stream);
+    if constexpr (ADOWN || !BDOWN) {
+        if (s.bn == 256) return launch_grad_tiles<256, 256, 2, 4, ADOWN, BDOWN, 1>(o, t, 1, stream);
+        if (s.bm == 256) return launch_grad_tiles<256, 128, 4, 2, ADOWN, BDOWN, 1>(o, t, 1, stream);
+    }
+    if (s.bm >= 128) return launch_grad_tiles<128, 128, 2, 2, ADOWN, BDOWN, P>(o, t, 1, stream);
     // (a DOWN B is read 4 columns a lane: 64 a wavefront)
     constexpr int WM = BDOWN ? 4 : 2;
     if (int e = launch_grad_tiles<64, 64, WM, 4 / WM, ADOWN, BDOWN, P>(o, t, s.slices, stream))
