@@ -33,7 +33,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 struct Int8 {
     using Acc = i32x4;
     using Sum = int32_t;
-    static constexpr int kBytes = 1;
     static __device__ __forceinline__ Acc mfma(u32x4 a, u32x4 b, Acc c) {
         return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a),
                                                      __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
@@ -42,7 +41,6 @@ struct Int8 {
 struct Bf16 {
     using Acc = f32x4;
     using Sum = float;
-    static constexpr int kBytes = 2;
     static __device__ __forceinline__ Acc mfma(u32x4 a, u32x4 b, Acc c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
                                                        __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -103,9 +101,7 @@ __device__ __forceinline__ void barrier() {
 
 // 16 bytes at p, of which the first n exist (n may be negative) and `before` bytes
 // of the row come before p.  A piece that is cut short is read as the row's last
-// 16 bytes, shifted into place; a row shorter than that, element by element.
-
-template <int BYTES>
+// 16 bytes, shifted into place; a row shorter than that, byte by byte.
 __device__ __forceinline__ u32x4 load_tail(const char* p, int n, int before) {
     if (n >= 16) return *reinterpret_cast<const u32x4*>(p);
     u32x4 v = {0, 0, 0, 0};
@@ -116,13 +112,8 @@ __device__ __forceinline__ u32x4 load_tail(const char* p, int n, int before) {
         return __builtin_bit_cast(u32x4, all >> (8 * (16 - n)));
     }
 #pragma unroll
-    for (int i = 0; i < 16; i += BYTES)
-        if (i < n) {
-            uint32_t e;
-            if constexpr (BYTES == 1) e = *reinterpret_cast<const uint8_t*>(p + i);
-            else e = *reinterpret_cast<const uint16_t*>(p + i);
-            v[i / 4] |= e << (8 * (i % 4));
-        }
+    for (int i = 0; i < 16; ++i)
+        if (i < n) v[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i % 4));
     return v;
 }
 
@@ -223,24 +214,33 @@ struct Gemm {
     }
 
     // the last, short step of a row: through registers, zeros past the end
-    static __device__ __forceinline__ void fetch_tail(const char* a, const char* b, const Loads& l,
-                                                      char* lds, int wave, int lane, int bytes,
-                                                      int before) {
-        const int at = lane << 4;
+    struct Tail {
+        u32x4 a[kLoadsA], b[kLoadsB];
+    };
+    static __device__ __forceinline__ void load(Tail& t, const char* a, const char* b,
+                                                const Loads& l, int wave, int lane, int bytes,
+                                                int before) {
 #pragma unroll
         for (int j = 0; j < kLoadsA; ++j) {
             const int row = (j * kWaves + wave) * 8 + (lane >> 3);
             const int k = ((lane & 7) ^ place_a(row)) << 4;
-            *reinterpret_cast<u32x4*>(lds + (j * kWaves + wave) * 1024 + at) =
-                load_tail<Op::kBytes>(a + l.a[j], bytes - k, before + k);
+            t.a[j] = load_tail(a + l.a[j], bytes - k, before + k);
         }
 #pragma unroll
         for (int j = 0; j < kLoadsB; ++j) {
             const int row = (j * kWaves + wave) * 8 + (lane >> 3);
             const int k = ((lane & 7) ^ place_b(row)) << 4;
-            *reinterpret_cast<u32x4*>(lds + BM * kStep + (j * kWaves + wave) * 1024 + at) =
-                load_tail<Op::kBytes>(b + l.b[j], bytes - k, before + k);
+            t.b[j] = load_tail(b + l.b[j], bytes - k, before + k);
         }
+    }
+    static __device__ __forceinline__ void store(const Tail& t, char* lds, int wave, int lane) {
+#pragma unroll
+        for (int j = 0; j < kLoadsA; ++j)
+            *reinterpret_cast<u32x4*>(lds + (j * kWaves + wave) * 1024 + (lane << 4)) = t.a[j];
+#pragma unroll
+        for (int j = 0; j < kLoadsB; ++j)
+            *reinterpret_cast<u32x4*>(lds + BM * kStep + (j * kWaves + wave) * 1024 +
+                                      (lane << 4)) = t.b[j];
     }
 
     // the operands of half a step: 64 bytes of the wavefront's rows
@@ -303,6 +303,37 @@ struct Gemm {
         // buffer done with, one barrier, and the step S on is sent for into that
         // buffer while the second half is multiplied and the next step's first is
         // read.
+        // What the end needs, the short step and the scales, is sent for first where
+        // registers are to be had and a block's time short enough for it to show
+        // (2000 x 2000 x 2000 18.5 us, and 19.8 with both at the end; 1576 x 1153 x
+        // 385 8.1 and 8.4).
+        constexpr bool kEarly = BM <= 128;
+        constexpr int COLS = 4 * NT;
+        const int64_t n0 = tile.n + wn * NT * 16 + g * COLS;
+        const int n = (int)(o.N - n0 < COLS ? o.N - n0 : COLS);
+        const bool has_tail = tail != 0 && tile.slice == slices - 1;
+        Tail last;
+        float cs[COLS], rs[MT];
+        const auto scales = [&] {
+            if (slices > 1 || t.row_scale == nullptr) return;
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) {
+                const int64_t c = n0 + k;
+                cs[k] = t.col_scale[c < o.N ? c : o.N - 1];
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int64_t m = tile.m + (wm * MT + i) * 16 + r;
+                rs[i] = t.row_scale[m < o.M ? m : o.M - 1];
+            }
+        };
+        if constexpr (kEarly) {
+            if (has_tail)
+                load(last, a0 + (int64_t)steps * kStep, b0 + (int64_t)steps * kStep, l, wave, lane,
+                     tail, steps * kStep);
+            scales();
+        }
+
         const char* a_at = a0 + (int64_t)k0 * kStep;
         const char* b_at = b0 + (int64_t)k0 * kStep;
         const auto send = [&](int k) {
@@ -345,12 +376,14 @@ struct Gemm {
             if (k < k1 - 2) step(k++, Int<2>());
         if (k < k1 - 1) step(k++, Int<1>());
         if (k < k1) step(k, Int<0>());
-        if (tail != 0 && tile.slice == slices - 1) {
+        if (has_tail) {
             // no load is on its way, and all wavefronts are past their reads of every
             // buffer but the last step's
             char* now = lds + (k1 - k0) % S * kBuffer;
-            fetch_tail(a0 + (int64_t)steps * kStep, b0 + (int64_t)steps * kStep, l, now, wave, lane,
-                       tail, steps * kStep);
+            if constexpr (!kEarly)
+                load(last, a0 + (int64_t)steps * kStep, b0 + (int64_t)steps * kStep, l, wave, lane,
+                     tail, steps * kStep);
+            store(last, now, wave, lane);
             __syncthreads();
             read(h0, now + off_a, now + off_b, 0, swap);
             read(h1, now + off_a, now + off_b, 1, swap);
@@ -358,15 +391,8 @@ struct Gemm {
             multiply(h1, acc);
         }
 
-        constexpr int COLS = 4 * NT;
-        const int64_t n0 = tile.n + wn * NT * 16 + g * COLS;
-        const int n = (int)(o.N - n0 < COLS ? o.N - n0 : COLS);
         if (n <= 0) return;
-        float cs[COLS];
-        if (slices == 1 && t.col_scale != nullptr) {
-#pragma unroll
-            for (int k = 0; k < COLS; ++k) cs[k] = t.col_scale[n0 + (k < n ? k : 0)];
-        }
+        if constexpr (!kEarly) scales();
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int64_t m = tile.m + (wm * MT + i) * 16 + r;
@@ -385,9 +411,8 @@ struct Gemm {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[4 * j + k] = (float)acc[i][j][k];
             if (t.row_scale != nullptr) {
-                const float rs = t.row_scale[m];
 #pragma unroll
-                for (int k = 0; k < COLS; ++k) v[k] = v[k] * rs * cs[k];
+                for (int k = 0; k < COLS; ++k) v[k] = v[k] * rs[i] * cs[k];
             }
             store_cols<COLS>(t, m, n0, n, v);
         }
@@ -464,6 +489,8 @@ inline Shape shape_of(int64_t M, int64_t N, int64_t steps, int parts = 1) {
     double least = -1;
     for (const auto& t : tiles) {
         const int64_t n = up(M, t.bm) * up(N, t.bn);
+        // (a launch holds fewer than 2^32 work items, at most 512 a block)
+        if (t.bm < 256 && n >= (int64_t)1 << 23) continue;
         for (int slices = 1; slices <= 64; slices *= 2) {
             if (slices > 1 && (t.bm != 64 || n * slices > 2048 || steps < 4 * slices)) break;
             const double each = (double)up(n * slices, 256) * t.each;
@@ -491,7 +518,6 @@ inline bool all_at_once(int64_t blocks, int bytes) { return blocks <= 256 * (160
 template <class Op, int BM, int BN, int WM, int WN>
 int launch_tiles(const Operands& o, const Target& t, int slices, void* stream) {
     const int64_t tm = up(o.M, BM), tn = up(o.N, BN), blocks = tm * tn * slices;
-    // (work items of a launch stay below 2^32)
     if (blocks * 64 * WM * WN >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
     const dim3 grid((uint32_t)blocks);
     if constexpr (BM < 256)
@@ -512,7 +538,7 @@ int launch_join(const Target& t, int64_t M, int64_t N, int slices, void* stream)
 
 template <class Op>
 int launch_gemm(const Operands& o, Target t, void* ws, void* stream) {
-    const Shape s = shape_of(o.M, o.N, o.row / kStep);
+    const Shape s = shape_of(o.M, o.N, up(o.row, kStep));
     t.ws = ws;
     t.ldws = slices_ld(o.N);
     t.slice = o.M * t.ldws;

@@ -391,12 +391,13 @@ int launch_grad_gemm(const GradOperands& o, Target t, void* ws, void* stream) {
     t.ws = ws;
     t.ldws = slices_ld(o.N);
     t.slice = o.M * t.ldws;
-    // (as it is, the 8-bit operand of dx meets at most 128 rows: never this tile.
-    // Its LDS holds one part.)
-    if constexpr (ADOWN || !BDOWN) {
+    // (as it is, the 8-bit operand of dx meets at most 128 rows: never this tile,
+    // whose LDS holds one part)
+    if constexpr (ADOWN || !BDOWN)
         if (s.bn == 256) return launch_grad_tiles<256, 256, 2, 4, ADOWN, BDOWN, 1>(o, t, 1, stream);
-        if (s.bm == 256) return launch_grad_tiles<256, 128, 4, 2, ADOWN, BDOWN, 1>(o, t, 1, stream);
-    }
+    // (with more parts than one, two tiles of 128 x 128 take less than this one)
+    if constexpr (!BDOWN && P == 1)
+        if (s.bm == 256) return launch_grad_tiles<256, 128, 4, 2, false, false, 1>(o, t, 1, stream);
     if (s.bm >= 128) return launch_grad_tiles<128, 128, 2, 2, ADOWN, BDOWN, P>(o, t, 1, stream);
     // (a DOWN B is read 4 columns a lane: 64 a wavefront)
     constexpr int WM = BDOWN ? 4 : 2;

@@ -60,10 +60,10 @@ __global__ __launch_bounds__(1024) void few_kernel(const int8_t* a, int64_t lda,
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int n = K - (int)at - g * 32 - h * 16, before = (int)at + g * 32 + h * 16;
-            const u32x4 w = load_tail<1>(bp + at + h * 16, n, before);
+            const u32x4 w = load_tail(bp + at + h * 16, n, before);
 #pragma unroll
             for (int i = 0; i < MT; ++i)
-                acc[i] = Int8::mfma(w, load_tail<1>(ap[i] + at + h * 16, n, before), acc[i]);
+                acc[i] = Int8::mfma(w, load_tail(ap[i] + at + h * 16, n, before), acc[i]);
         }
     }
 #pragma unroll
@@ -106,7 +106,7 @@ int launch_few(Held a, Held b, int64_t M, int64_t N, int64_t K, const Target& t,
 }  // namespace
 
 int64_t matmul_workspace(int64_t M, int64_t N, int64_t K) {
-    return M <= kFewTokens ? 0 : slices_bytes(M, N, K / kStep);
+    return M <= kFewTokens ? 0 : slices_bytes(M, N, up(K, kStep));
 }
 
 int launch_matmul(Held a, Held b, int64_t M, int64_t N, int64_t K, Mat y, void* workspace,
