@@ -148,6 +148,94 @@ __device__ __forceinline__ void store_cols(const Target& t, int64_t m, int64_t n
     }
 }
 
+// A wavefront's 16 rows of C, as the matrix instructions leave them: lane (g, r) has
+// row r, and PIECES pieces of 16 bytes from PIECES g on.  A store of one piece a lane
+// would touch every row, and 16 bytes of every 32 or 64.  So the lanes r of 16
+// exchange pieces until piece i of a lane is of row row_of(i), its place there
+// place_of(): a store then covers whole rows.  Written as they are, 4096 x 4096 x 256
+// took 30 us (fp32) and 17 (bf16), and so 18 and 15.  Stores past the caches took 13
+// in bf16, but whoever reads the results then pays for it and more (8192 x 8192 x
+// 1024 and the rows made 8-bit: 127 us, and 115 so).
+template <int PIECES>
+struct Turn {
+    static_assert(PIECES == 1 || PIECES == 2 || PIECES == 4, "a power of two");
+    static __device__ __forceinline__ int row_of(int i, int r) {
+        return PIECES == 1 ? r : PIECES == 2 ? (r & 7) | i << 3 : (r & 3) | i << 2;
+    }
+    static __device__ __forceinline__ int place_of(int g, int r) {
+        return PIECES == 1 ? g : PIECES == 2 ? g << 1 | r >> 3 : g << 2 | r >> 2;
+    }
+    // gives the lower lane's b for the a of the one ACROSS (8 or 4) above it
+    template <int ACROSS>
+    static __device__ __forceinline__ void swap(u32x4& a, u32x4& b, int r) {
+        const bool upper = (r & ACROSS) != 0;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            uint32_t x = upper ? a[d] : b[d];
+            if constexpr (ACROSS == 8) {
+                x = __builtin_amdgcn_update_dpp(0, x, 0x128, 15, 15, true);  // row_ror:8
+            } else {
+                x = __builtin_amdgcn_update_dpp(0, x, 0x141, 15, 15, true);  // row_half_mirror
+                x = __builtin_amdgcn_update_dpp(0, x, 0x1b, 15, 15, true);   // quad_perm:[3,2,1,0]
+            }
+            a[d] = upper ? x : a[d];
+            b[d] = upper ? b[d] : x;
+        }
+    }
+    static __device__ __forceinline__ void run(u32x4 (&p)[PIECES], int r) {
+        if constexpr (PIECES == 2) {
+            swap<8>(p[0], p[1], r);
+        }
+        if constexpr (PIECES == 4) {
+            swap<8>(p[0], p[2], r);
+            swap<8>(p[1], p[3], r);
+            swap<4>(p[0], p[1], r);
+            swap<4>(p[2], p[3], r);
+        }
+    }
+};
+// Stores them to the rows at c, E as wide as an element; `rows` and `cols` are there.
+template <class E, int PIECES>
+__device__ __forceinline__ void store_turned(u32x4 (&p)[PIECES], E* c, int64_t ld, int64_t rows,
+                                             int64_t cols, int r, int g) {
+    using T = Turn<PIECES>;
+    constexpr int kEach = 16 / sizeof(E);
+    T::run(p, r);
+    const int col = T::place_of(g, r) * kEach;
+    const int n = cols - col < kEach ? (int)(cols - col) : kEach;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int row = T::row_of(i, r);
+        if (row >= rows) continue;
+        E* at = c + row * ld + col;
+        if (n == kEach) {
+            *reinterpret_cast<u32x4*>(at) = p[i];
+        } else {
+#pragma unroll
+            for (int k = 0; k < kEach - 1; ++k)
+                if (k < n)
+                    at[k] = (E)(p[i][k * sizeof(E) / 4] >> (sizeof(E) == 2 ? 16 * (k % 2) : 0));
+        }
+    }
+}
+
+// The same for numbers v of C: 4 NT consecutive columns of row m + r a lane.
+template <int NT>
+__device__ __forceinline__ void store_rows(const Target& t, int64_t m, int64_t n, int64_t rows,
+                                           int64_t cols, int r, int g, const float (&v)[4 * NT]) {
+    if (t.bf16) {
+        u32x4 p[NT / 2];
+#pragma unroll
+        for (int k = 0; k < 4 * NT; k += 2) p[k / 8][k % 8 / 2] = narrow2(v[k], v[k + 1]);
+        store_turned(p, static_cast<uint16_t*>(t.c) + m * t.ldc + n, t.ldc, rows, cols, r, g);
+    } else {
+        u32x4 p[NT];
+#pragma unroll
+        for (int k = 0; k < 4 * NT; ++k) p[k / 4][k % 4] = __float_as_uint(v[k]);
+        store_turned(p, static_cast<uint32_t*>(t.c) + m * t.ldc + n, t.ldc, rows, cols, r, g);
+    }
+}
+
 // The tile of a block.  Blocks are dealt to the 8 XCDs in turn; each XCD takes a
 // run of consecutive tiles, and those go down 8 rows of tiles before the next
 // column, so that the tiles an XCD works on share rows of A and B in its L2.
@@ -276,7 +364,7 @@ struct Gemm {
         }
     }
 
-    static __device__ void run(const Operands& o, const Target& t, int64_t tiles_m,
+    static __device__ __forceinline__ void run(const Operands& o, const Target& t, int64_t tiles_m,
                                int64_t tiles_n, int slices) {
         __shared__ __attribute__((aligned(1024))) char lds[S * kBuffer];
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -310,7 +398,6 @@ struct Gemm {
         constexpr bool kEarly = BM <= 128;
         constexpr int COLS = 4 * NT;
         const int64_t n0 = tile.n + wn * NT * 16 + g * COLS;
-        const int n = (int)(o.N - n0 < COLS ? o.N - n0 : COLS);
         const bool has_tail = tail != 0 && tile.slice == slices - 1;
         Tail last;
         float cs[COLS], rs[MT];
@@ -391,18 +478,19 @@ struct Gemm {
             multiply(h1, acc);
         }
 
-        if (n <= 0) return;
         if constexpr (!kEarly) scales();
+        const int64_t n_wave = tile.n + wn * NT * 16;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const int64_t m = tile.m + (wm * MT + i) * 16 + r;
-            if (m >= o.M) continue;
+            const int64_t m = tile.m + (wm * MT + i) * 16;
             if (slices > 1) {
-                auto* p = static_cast<typename Op::Sum*>(t.ws) + tile.slice * t.slice + m * t.ldws +
-                          n0;
+                u32x4 p[NT];
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
-                    *reinterpret_cast<typename Op::Acc*>(p + 4 * j) = acc[i][j];
+                for (int j = 0; j < NT; ++j) p[j] = __builtin_bit_cast(u32x4, acc[i][j]);
+                // (the workspace has rows of whole tiles)
+                store_turned(p, static_cast<uint32_t*>(t.ws) + tile.slice * t.slice + m * t.ldws +
+                                    n_wave,
+                             t.ldws, o.M - m, t.ldws - n_wave, r, g);
                 continue;
             }
             float v[COLS];
@@ -414,7 +502,7 @@ struct Gemm {
 #pragma unroll
                 for (int k = 0; k < COLS; ++k) v[k] = v[k] * rs[i] * cs[k];
             }
-            store_cols<COLS>(t, m, n0, n, v);
+            store_rows<NT>(t, m, n_wave, o.M - m, o.N - n_wave, r, g, v);
         }
     }
 };

@@ -258,7 +258,7 @@ struct GradGemm {
         }
     }
 
-    static __device__ void run(const GradOperands& o, const Target& t, int64_t tiles_m,
+    static __device__ __forceinline__ void run(const GradOperands& o, const Target& t, int64_t tiles_m,
                                int64_t tiles_n, int slices) {
         __shared__ __attribute__((aligned(1024))) char lds[S * kBuffer];
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -338,26 +338,24 @@ struct GradGemm {
         if (k < k1) step(k, Int<0>());
 
         // lane: 4 NT columns of MT rows
-        constexpr int COLS = 4 * NT;
         const int wm = wave / WN, wn = wave % WN, r = lane & 15, g = lane >> 4;
-        const int64_t n0 = tile.n + wn * NT * 16 + g * COLS;
-        const int n = (int)(o.N - n0 < COLS ? o.N - n0 : COLS);
-        if (n <= 0) return;
+        const int64_t n = tile.n + wn * NT * 16;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const int64_t m = tile.m + (wm * MT + i) * 16 + r;
-            if (m >= o.M) continue;
-            float v[COLS];
+            const int64_t m = tile.m + (wm * MT + i) * 16;
+            float v[4 * NT];
 #pragma unroll
-            for (int c = 0; c < COLS; ++c)
+            for (int c = 0; c < 4 * NT; ++c)
                 v[c] = BDOWN ? acc[i][c % 4][c / 4] : acc[i][c / 4][c % 4];
             if (slices > 1) {
-                float* p = static_cast<float*>(t.ws) + tile.slice * t.slice + m * t.ldws + n0;
+                u32x4 p[NT];
 #pragma unroll
-                for (int c = 0; c < COLS; c += 4)
-                    *reinterpret_cast<f32x4*>(p + c) = f32x4{v[c], v[c + 1], v[c + 2], v[c + 3]};
+                for (int c = 0; c < 4 * NT; ++c) p[c / 4][c % 4] = __float_as_uint(v[c]);
+                // (the workspace has rows of whole tiles)
+                store_turned(p, static_cast<uint32_t*>(t.ws) + tile.slice * t.slice + m * t.ldws + n,
+                             t.ldws, o.M - m, t.ldws - n, r, g);
             } else {
-                store_cols<COLS>(t, m, n0, n, v);
+                store_rows<NT>(t, m, n, o.M - m, o.N - n, r, g, v);
             }
         }
     }
