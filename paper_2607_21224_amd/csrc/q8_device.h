@@ -28,6 +28,9 @@ struct F32 {
 struct BF16 {
     using T = uint16_t;
 };
+struct I8 {
+    using T = int8_t;
+};
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -144,6 +147,15 @@ struct Raw<F32> {
     float v[kPiece];
     __device__ __forceinline__ void load(const float* p, int n, int c) { load8(p, n, c, v); }
     __device__ __forceinline__ float operator[](int k) const { return v[k]; }
+};
+
+template <>
+struct Raw<I8> {
+    u32x2 v;
+    __device__ __forceinline__ void load(const int8_t* p, int n, int c) { v = bits8(p, n, c); }
+    __device__ __forceinline__ float operator[](int k) const {
+        return (float)(int8_t)(v[k / 4] >> (8 * (k % 4)));
+    }
 };
 
 // Results leave as they are made, nontemporal: what a launch leaves in an XCD's

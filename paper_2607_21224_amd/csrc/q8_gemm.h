@@ -550,6 +550,7 @@ __global__ __launch_bounds__(256) void join_kernel(Target t, int64_t M, int64_t 
 struct Shape {
     int bm, bn;  // 256 x 256, 256 x 128, 128 x 128 or 64 x 64
     int slices;  // of K
+    double ns;   // it should take
 };
 
 inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -566,15 +567,12 @@ inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // A step with several parts of A takes them one after the other (256), or together,
 // with the loads of B once.  Slices are added up by a second launch: its start, and
 // each sum written and read again at 3 TB/s.
-inline Shape shape_of(int64_t M, int64_t N, int64_t steps, int parts = 1) {
-    const struct {
-        int bm, bn, least, each;
-    } tiles[] = {{256, 256, parts * 1350, parts * 1800},
-                 {256, 128, parts * 920, parts * 1100},
-                 {128, 128, 580 + 200 * parts, 230 + 390 * parts},
-                 {64, 64, 250 + 100 * parts, 105 + 115 * parts}};
-    Shape best = {256, 256, 1};
-    double least = -1;
+struct TileCost {
+    int bm, bn, least, each;
+};
+template <int TILES>
+inline Shape least_of(const TileCost (&tiles)[TILES], int64_t M, int64_t N, int64_t steps) {
+    Shape best = {256, 256, 1, -1};
     for (const auto& t : tiles) {
         const int64_t n = up(M, t.bm) * up(N, t.bn);
         // (a launch holds fewer than 2^32 work items, at most 512 a block)
@@ -584,19 +582,22 @@ inline Shape shape_of(int64_t M, int64_t N, int64_t steps, int parts = 1) {
             const double each = (double)up(n * slices, 256) * t.each;
             const double time = (double)up(steps, slices) * (each > t.least ? each : t.least) +
                                 (slices > 1 ? 4500.0 + slices * (double)M * (double)N / 375.0 : 0);
-            if (least < 0 || time < least) {
-                least = time;
-                best = {t.bm, t.bn, slices};
-            }
+            if (best.ns < 0 || time < best.ns) best = {t.bm, t.bn, slices, time};
         }
     }
     return best;
 }
+inline Shape shape_of(int64_t M, int64_t N, int64_t steps, int parts = 1) {
+    const TileCost tiles[] = {{256, 256, parts * 1350, parts * 1800},
+                              {256, 128, parts * 920, parts * 1100},
+                              {128, 128, 580 + 200 * parts, 230 + 390 * parts},
+                              {64, 64, 250 + 100 * parts, 105 + 115 * parts}};
+    return least_of(tiles, M, N, steps);
+}
 
 // Workspace of a product's slices.
 inline int64_t slices_ld(int64_t N) { return up(N, 64) * 64; }
-inline int64_t slices_bytes(int64_t M, int64_t N, int64_t steps, int parts = 1) {
-    const Shape s = shape_of(M, N, steps, parts);
+inline int64_t slices_bytes(int64_t M, int64_t N, const Shape& s) {
     return s.slices == 1 ? 0 : s.slices * M * slices_ld(N) * 4;
 }
 

@@ -31,6 +31,9 @@ namespace {
 // A sum of at most so many values (one step) is taken with all parts.
 constexpr int64_t kFew = 64;
 
+// What a lane reads for what is not there.
+__device__ __attribute__((aligned(16))) const uint32_t kNothing[4] = {0, 0, 0, 0};
+
 // Parts of the scaled gradient in a sum of R values.
 inline int parts_of(int64_t R, bool dy_bf16, bool out_bf16) {
     return out_bf16 && R > kFew ? 1 : dy_bf16 ? 2 : 3;

@@ -8,6 +8,7 @@
 // applied; the product kernel then reads them from memory straight into LDS.  The
 // extra traffic is that of the operands, small beside the product's 2 T N K
 // operations.
+#include "q8_grad_f32.h"
 #include "q8_grad_gemm.h"
 
 namespace cpdp {
@@ -40,43 +41,53 @@ constexpr int tile_cols() {
 template <int P, int COLS>
 using Tile = uint32_t[P][COLS][33];
 
-// 8 columns of two rows, each scaled, as pairs in P parts
-template <class In, int P, int COLS>
-__device__ __forceinline__ void turn8(const Source& s, int64_t r, int64_t c, int col, int pair,
-                                      Tile<P, COLS>& tile) {
-    float x[2][kPiece] = {};
-    const int n = s.C - c < kPiece ? (int)(s.C - c) : kPiece;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        if (r + h < s.R && n > 0) {
-            load8(static_cast<const In*>(s.p) + (r + h) * s.ld + c, n, (int)(c < 8 ? c : 8), x[h]);
-            if (s.scale != nullptr) {
-                const float f = s.scale[r + h];
-#pragma unroll
-                for (int k = 0; k < kPiece; ++k) x[h][k] = k < n ? x[h][k] * f : 0.0f;
-            }
-        }
-#pragma unroll
-    for (int k = 0; k < kPiece; ++k) {
-        uint16_t lo[P], hi[P];
-        split<P>(x[0][k], lo);
-        split<P>(x[1][k], hi);
-#pragma unroll
-        for (int p = 0; p < P; ++p) tile[p][col + k][pair] = (uint32_t)lo[p] | (uint32_t)hi[p] << 16;
-    }
-}
-
 // in [R x C] -> out [P][C][pad], scaled by row, zeros from R to pad.  A block takes
-// 64 rows through LDS, two neighbouring ones a thread.
-template <class In, int P>
-__device__ void transpose(const Source& s, uint32_t block, Tile<P, tile_cols<In>()>& tile) {
-    constexpr int COLS = tile_cols<In>();
+// 64 rows through LDS, two neighbouring ones a thread.  All that a thread reads is
+// sent for before any of it is used (WHOLE: and without a branch, as all of the
+// block's rows and columns are there): one after the other, its rows and their scales
+// were 8 waits for memory, and the layout of 1576 x 1536 fp32 took 11 us.
+template <class E, int P, bool WHOLE>
+__device__ __forceinline__ void turn(const Source& s, int64_t r0, int64_t c0,
+                                     Tile<P, tile_cols<typename E::T>()>& tile) {
+    constexpr int H = tile_cols<typename E::T>() / 64;
+    const int pair = (int)threadIdx.x / 8, col = (int)threadIdx.x % 8 * kPiece;
+    const int64_t r = r0 + 2 * pair;
+    Raw<E> x[H][2] = {};
+    float f[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool there = WHOLE || r + i < s.R;
+        // (rows that are not there are zeros, whatever the scales)
+        f[i] = !there ? 0.0f : s.scale == nullptr ? 1.0f : s.scale[r + i];
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            const int64_t c = c0 + h * 64 + col;
+            const int n = WHOLE || s.C - c > kPiece ? kPiece : (int)(s.C - c);
+            if (there && n > 0)
+                x[h][i].load(static_cast<const typename E::T*>(s.p) + (r + i) * s.ld + c, n,
+                             (int)(c < 8 ? c : 8));
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) {
+            uint16_t lo[P], hi[P];
+            split<P>(x[h][0][k] * f[0], lo);
+            split<P>(x[h][1][k] * f[1], hi);
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                tile[p][h * 64 + col + k][pair] = (uint32_t)lo[p] | (uint32_t)hi[p] << 16;
+        }
+}
+template <class E, int P>
+__device__ void transpose(const Source& s, uint32_t block,
+                          Tile<P, tile_cols<typename E::T>()>& tile) {
+    constexpr int COLS = tile_cols<typename E::T>();
     const uint32_t tiles_r = (uint32_t)(s.pad / 64);
     const int64_t r0 = (int64_t)(block % tiles_r) * 64, c0 = (int64_t)(block / tiles_r) * COLS;
-    const int pair = (int)threadIdx.x / 8, col = (int)threadIdx.x % 8 * kPiece;
-#pragma unroll
-    for (int h = 0; h < COLS; h += 64)
-        turn8<In, P, COLS>(s, r0 + 2 * pair, c0 + h + col, h + col, pair, tile);
+    if (r0 + 64 <= s.R && c0 + COLS <= s.C) turn<E, P, true>(s, r0, c0, tile);
+    else turn<E, P, false>(s, r0, c0, tile);
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < P; ++p)
@@ -91,27 +102,22 @@ __device__ void transpose(const Source& s, uint32_t block, Tile<P, tile_cols<In>
 }
 
 // in [R x C] -> out [P][R][pad], scaled by column, zeros from C to pad
-template <class In, int P>
+template <class E, int P>
 __device__ void spread(const Source& s, uint32_t block) {
     // (a launch holds fewer than 2^32 work items)
     const uint32_t across = (uint32_t)(s.pad / kPiece), i = block * 256u + threadIdx.x;
     const int64_t r = i / across, c = (int64_t)(i % across) * kPiece;
     if (r >= s.R) return;
-    float x[kPiece] = {};
-    const int n = s.C - c < kPiece ? (int)(s.C - c) : kPiece;
+    Raw<E> x = {};
+    Raw<F32> f = {};
+    const int n = s.C - c < kPiece ? (int)(s.C - c) : kPiece, before = (int)(c < 8 ? c : 8);
     if (n > 0) {
-        const int before = (int)(c < 8 ? c : 8);
-        load8(static_cast<const In*>(s.p) + r * s.ld + c, n, before, x);
-        if (s.scale != nullptr) {
-            float f[kPiece];
-            load8(s.scale + c, n, before, f);
-#pragma unroll
-            for (int k = 0; k < kPiece; ++k) x[k] = k < n ? x[k] * f[k] : 0.0f;
-        }
+        x.load(static_cast<const typename E::T*>(s.p) + r * s.ld + c, n, before);
+        if (s.scale != nullptr) f.load(s.scale + c, n, before);
     }
     uint16_t part[kPiece][P];
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) split<P>(x[k], part[k]);
+    for (int k = 0; k < kPiece; ++k) split<P>(s.scale != nullptr ? x[k] * f[k] : x[k], part[k]);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         u32x4 v;
@@ -124,18 +130,18 @@ __device__ void spread(const Source& s, uint32_t block) {
 
 // One launch lays out what has to be: the first blocks the 8-bit operand, the
 // others dy.
-template <class In, int P, bool ALONG>
+template <class E, int P, bool ALONG>
 __global__ __launch_bounds__(256) void layout_kernel(Source held, Source dy) {
     __shared__ union {
         Tile<1, tile_cols<int8_t>()> held;
-        Tile<ALONG ? 1 : P, tile_cols<In>()> dy;
+        Tile<ALONG ? 1 : P, tile_cols<typename E::T>()> dy;
     } tile;
     if (blockIdx.x < held.blocks)
-        transpose<int8_t, 1>(held, blockIdx.x, tile.held);
+        transpose<I8, 1>(held, blockIdx.x, tile.held);
     else if constexpr (ALONG)
-        spread<In, P>(dy, blockIdx.x - (uint32_t)held.blocks);
+        spread<E, P>(dy, blockIdx.x - (uint32_t)held.blocks);
     else
-        transpose<In, P>(dy, blockIdx.x - (uint32_t)held.blocks, tile.dy);
+        transpose<E, P>(dy, blockIdx.x - (uint32_t)held.blocks, tile.dy);
 }
 
 __global__ __launch_bounds__(256) void zero_rows_kernel(char* p, int64_t ld, int64_t R,
@@ -161,7 +167,10 @@ struct Layout {
     int parts;
     bool held_scaled;
     bool dy_as_is, held_as_is;
-    int64_t Rp;  // summed size, padded to whole steps
+    bool f32;  // fp32 dy as it is, taken apart on its way (q8_grad_f32.h)
+    int64_t Rp;  // summed size, padded to whole steps,
+    int64_t steps;
+    Shape shape;  // of the product
     int64_t dy_bytes, held_bytes;
 };
 
@@ -172,21 +181,32 @@ struct Layout {
 // 2048 (2048 x 2048) 40 and 48.
 constexpr int64_t kHeldInput = 128, kHeldWeight = 1024;
 
+// fp32 dy in three parts: written at about 2.2 TB/s where that is much of the time
+// there is.  dx laid out, and taken apart on its way: 1576 x 1536 x 384 26 and 20 us,
+// 1000^3 18.8 and 17.1, 4000 x 600 x 600 33 and 24, 2048^3 57 and 69.
+constexpr double kLayoutNs = 6 / 2200.0;
+
 Layout layout(int64_t M, int64_t N, int64_t R, bool dy_bf16, bool out_bf16, bool along) {
-    Layout l;
+    Layout l{};
     l.parts = parts_of(R, dy_bf16, out_bf16);
     l.held_scaled = l.parts == 1 && dy_bf16;
     l.Rp = up(R, kRound) * kRound;
+    l.steps = l.Rp / kRound;
     l.held_as_is = l.held_scaled && (along ? M <= kHeldInput : R <= kHeldWeight);
+    l.shape = shape_of(M, N, l.steps, l.held_as_is ? kDownParts : l.parts);
+    if (l.parts == 3) {
+        const Shape s = f32_shape(M, N, l.steps);
+        l.f32 = s.ns >= 0 && s.ns < l.shape.ns + (double)M * (double)l.Rp * kLayoutNs;
+        if (l.f32) l.shape = s;
+    }
     // a step of dx reads 128 bytes of a row of dy, which have to be there
-    l.dy_as_is = along ? l.held_scaled && l.Rp == R : l.held_as_is;
+    l.dy_as_is = l.f32 || (along ? l.held_scaled && l.Rp == R : l.held_as_is);
     l.dy_bytes = l.dy_as_is ? 0 : l.parts * M * l.Rp * 2;
     l.held_bytes = l.held_as_is ? 0 : N * l.Rp * 2;
     return l;
 }
 int64_t workspace_of(const Layout& l, int64_t M, int64_t N) {
-    return l.dy_bytes + l.held_bytes +
-           slices_bytes(M, N, l.Rp / kRound, l.held_as_is ? kDownParts : l.parts);
+    return l.dy_bytes + l.held_bytes + slices_bytes(M, N, l.shape);
 }
 
 // c [M x N] = the sum over R of dy, which has its rows, and the 8-bit operand,
@@ -207,11 +227,21 @@ int gradient(Mat dy, Held held, int64_t R, int64_t M, int64_t N, Mat c, void* wo
         const dim3 grid((uint32_t)(h.blocks + d.blocks));
         const int e =
             dy.bf16
-                ? l.parts == 1 ? launch(layout_kernel<uint16_t, 1, ALONG>, grid, 256, stream, h, d)
-                               : launch(layout_kernel<uint16_t, 2, ALONG>, grid, 256, stream, h, d)
-            : l.parts == 1 ? launch(layout_kernel<float, 1, ALONG>, grid, 256, stream, h, d)
-                           : launch(layout_kernel<float, 3, ALONG>, grid, 256, stream, h, d);
+                ? l.parts == 1 ? launch(layout_kernel<BF16, 1, ALONG>, grid, 256, stream, h, d)
+                               : launch(layout_kernel<BF16, 2, ALONG>, grid, 256, stream, h, d)
+            : l.parts == 1 ? launch(layout_kernel<F32, 1, ALONG>, grid, 256, stream, h, d)
+                           : launch(layout_kernel<F32, 3, ALONG>, grid, 256, stream, h, d);
         if (e) return e;
+    }
+    Target t{};
+    t.c = c.p;
+    t.ldc = c.ld;
+    t.bf16 = c.bf16;
+    void* slices = ws + l.dy_bytes + l.held_bytes;
+    if (l.f32) {
+        const F32Operands o{static_cast<const char*>(dy.p), dy.ld * 4, ws, l.Rp * 2,
+                            held.scale, R, M, N, (int)l.steps};
+        return launch_grad_f32<!ALONG>(o, t, l.shape.slices, slices, stream);
     }
     GradOperands o{};
     o.a = l.dy_as_is ? static_cast<const char*>(dy.p) : ws;
@@ -223,17 +253,12 @@ int gradient(Mat dy, Held held, int64_t R, int64_t M, int64_t N, Mat c, void* wo
     o.R = R;
     o.M = M;
     o.N = N;
-    o.steps = (int)(l.Rp / kRound);
+    o.steps = (int)l.steps;
     o.parts = l.parts;
-    Target t{};
-    t.c = c.p;
-    t.ldc = c.ld;
-    t.bf16 = c.bf16;
-    void* slices = ws + l.dy_bytes + l.held_bytes;
-    if (l.held_as_is) return launch_grad_gemm<!ALONG, true, 1>(o, t, slices, stream);
-    if (l.parts == 1) return launch_grad_gemm<false, false, 1>(o, t, slices, stream);
-    return l.parts == 2 ? launch_grad_gemm<false, false, 2>(o, t, slices, stream)
-                        : launch_grad_gemm<false, false, 3>(o, t, slices, stream);
+    if (l.held_as_is) return launch_grad_gemm<!ALONG, true, 1>(o, t, l.shape, slices, stream);
+    if (l.parts == 1) return launch_grad_gemm<false, false, 1>(o, t, l.shape, slices, stream);
+    return l.parts == 2 ? launch_grad_gemm<false, false, 2>(o, t, l.shape, slices, stream)
+                        : launch_grad_gemm<false, false, 3>(o, t, l.shape, slices, stream);
 }
 
 }  // namespace

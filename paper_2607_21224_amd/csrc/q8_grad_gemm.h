@@ -48,9 +48,6 @@ struct GradOperands {
 // of three parts (shape_of).
 constexpr int kDownParts = 3;
 
-// What a lane reads for rows that are not there.
-__device__ __attribute__((aligned(16))) const uint32_t kNothing[4] = {0, 0, 0, 0};
-
 template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P, int S>
 struct GradGemm {
     using G = Gemm<Bf16, BM, BN, WM, WN, 2>;
@@ -384,8 +381,7 @@ int launch_grad_tiles(const GradOperands& o, const Target& t, int slices, void* 
 }
 
 template <bool ADOWN, bool BDOWN, int P>
-int launch_grad_gemm(const GradOperands& o, Target t, void* ws, void* stream) {
-    const Shape s = shape_of(o.M, o.N, o.steps, BDOWN ? kDownParts : P);
+int launch_grad_gemm(const GradOperands& o, Target t, const Shape& s, void* ws, void* stream) {
     t.ws = ws;
     t.ldws = slices_ld(o.N);
     t.slice = o.M * t.ldws;

@@ -106,7 +106,7 @@ int launch_few(Held a, Held b, int64_t M, int64_t N, int64_t K, const Target& t,
 }  // namespace
 
 int64_t matmul_workspace(int64_t M, int64_t N, int64_t K) {
-    return M <= kFewTokens ? 0 : slices_bytes(M, N, up(K, kStep));
+    return M <= kFewTokens ? 0 : slices_bytes(M, N, shape_of(M, N, up(K, kStep)));
 }
 
 int launch_matmul(Held a, Held b, int64_t M, int64_t N, int64_t K, Mat y, void* workspace,
