@@ -148,6 +148,9 @@ class Call {
 
 constexpr at::ScalarType kEither = at::kByte;
 
+// torch.OutOfMemoryError
+PyObject* out_of_memory = nullptr;
+
 // Runs f(arguments), with n arguments expected; no exception leaves it.
 template <class F>
 PyObject* entry(PyObject* const* a, Py_ssize_t got, Py_ssize_t n, F f) {
@@ -160,6 +163,8 @@ PyObject* entry(PyObject* const* a, Py_ssize_t got, Py_ssize_t n, F f) {
     } catch (const Raised&) {
     } catch (const std::invalid_argument& e) {
         PyErr_SetString(PyExc_ValueError, e.what());
+    } catch (const c10::OutOfMemoryError& e) {
+        PyErr_SetString(out_of_memory, e.what_without_backtrace());
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
     }
@@ -260,8 +265,10 @@ void same_stride(const Mat& m, const Mat& as, const char* name, const char* othe
 }
 
 int kind_of(PyObject* o) {
-    const long k = PyLong_AsLong(o);
+    int over = 0;
+    const long k = PyLong_AsLongAndOverflow(o, &over);
     if (k == -1 && PyErr_Occurred()) throw Raised();
+    if (over != 0 || k != (int)k) refuse("kind", "no activation has that number");
     return (int)k;
 }
 
@@ -364,4 +371,10 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q8", nullptr, -1, methods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__q8() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__q8() {
+    PyObject* torch = PyImport_ImportModule("torch");
+    if (torch == nullptr) return nullptr;
+    out_of_memory = PyObject_GetAttrString(torch, "OutOfMemoryError");
+    Py_DECREF(torch);
+    return out_of_memory == nullptr ? nullptr : PyModule_Create(&module);
+}

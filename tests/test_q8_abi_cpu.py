@@ -188,3 +188,13 @@ def test_python_checks_come_first():
         q8.cpdp_q8_rows(x, q, s)
     with pytest.raises(ValueError, match="float32 or torch.bfloat16"):
         q8.cpdp_q8_rows(x.half(), q, s)
+
+
+@pytest.mark.parametrize("kind", [1 << 32, -(1 << 40) + 1, 1 << 80])
+def test_python_refuses_numbers_no_activation_has(kind):
+    x = torch.zeros(4, 32)
+    q, s = torch.zeros(4, 32, dtype=torch.int8), torch.zeros(4)
+    with pytest.raises(ValueError, match="kind"):
+        q8.cpdp_q8_act(kind, x, q=q, scale=s)
+    with pytest.raises(ValueError, match="kind"):
+        q8.cpdp_q8_act_bwd(kind, x, q, s, x)
