@@ -18,12 +18,18 @@ def test_no_memory_for_a_workspace():
     torch.cuda.synchronize()
     torch.cuda.empty_cache()
     total = torch.cuda.get_device_properties(0).total_memory
+    held = []
     try:
         torch.cuda.set_per_process_memory_fraction(
             (torch.cuda.memory_reserved() + (8 << 20)) / total)
+        # what the allocator has kept of earlier tests
+        with pytest.raises(torch.OutOfMemoryError):
+            while True:
+                held.append(torch.empty(48 << 20, dtype=torch.uint8, device="cuda"))
         with pytest.raises(torch.OutOfMemoryError):
             q8.cpdp_q8_grad_input(dy, b, s, dx)
     finally:
+        held.clear()
         torch.cuda.set_per_process_memory_fraction(1.0)
     assert bool((dx == 1).all())
     q8.cpdp_q8_grad_input(dy, b, s, dx)
