@@ -255,9 +255,35 @@ __device__ __forceinline__ TileAt tile_at(int64_t tiles_m, int64_t tiles_n, int 
     return {(band * 8 + in % high) * BM, in / high * BN, (int)slice};
 }
 
-template <class Op, int BM, int BN, int WM, int WN, int S>
+// Two groups of WAVES wavefronts have sums of the same rows of C over the two halves of
+// the steps: each gives the other its sums of half the rows, and adds what it gets.
+template <int WAVES, class Acc, int MT, int NT>
+__device__ __forceinline__ void join_halves(const Acc (&acc)[MT][NT], Acc (&sum)[MT / 2][NT],
+                                            char* lds, int wave, int lane) {
+    const bool second = wave >= WAVES;
+    auto* room = reinterpret_cast<Acc(*)[MT / 2][NT][64]>(lds);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MT / 2; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            room[wave][i][j][lane] = second ? acc[i][j] : acc[MT / 2 + i][j];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MT / 2; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            sum[i][j] = (second ? acc[MT / 2 + i][j] : acc[i][j]) + room[wave ^ WAVES][i][j][lane];
+}
+
+// KS == 2: the wavefronts are two groups, each with one half of every step.  With one
+// block a CU a wavefront has a SIMD to itself and waits for what it has sent for; two
+// share it, and each reads half as much of LDS for a step (1024 x 4096 x 4096 25 -> 20
+// us, 2000^3 16.7 -> 14.8, 256 x 4096 x 4096 11.6 -> 10; with several blocks a CU it
+// costs: 1576 x 1536 x 384 5.9 -> 8.4).
+template <class Op, int BM, int BN, int WM, int WN, int S, int KS = 1>
 struct Gemm {
-    static constexpr int kWaves = WM * WN;
+    static constexpr int kWaves = WM * WN * KS;
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
     static constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;
@@ -381,7 +407,9 @@ struct Gemm {
         const int k1 = (int)((int64_t)steps * (tile.slice + 1) / slices);
 
         typename Op::Acc acc[MT][NT] = {};
-        const int wm = wave / WN, wn = wave % WN, r = lane & 15, g = lane >> 4;
+        // KS == 2: which half of a step the wavefront takes, and then of its rows of C
+        const int wk = KS == 1 ? 0 : wave / (WM * WN);
+        const int wm = wave / WN % WM, wn = wave % WN, r = lane & 15, g = lane >> 4;
         const int off_a = (wm * MT * 16 + r) * kStep;
         const int off_b = BM * kStep + (wn * NT * 16 + (r >> 2) * 4 * NT + (r & 3)) * kStep;
         const int swap = (g ^ (r >> 1)) << 4;
@@ -396,11 +424,11 @@ struct Gemm {
         // (2000 x 2000 x 2000 18.5 us, and 19.8 with both at the end; 1576 x 1153 x
         // 385 8.1 and 8.4).
         constexpr bool kEarly = BM <= 128;
-        constexpr int COLS = 4 * NT;
+        constexpr int COLS = 4 * NT, MO = MT / KS;
         const int64_t n0 = tile.n + wn * NT * 16 + g * COLS;
         const bool has_tail = tail != 0 && tile.slice == slices - 1;
         Tail last;
-        float cs[COLS], rs[MT];
+        float cs[COLS], rs[MO];
         const auto scales = [&] {
             if (slices > 1 || t.row_scale == nullptr) return;
 #pragma unroll
@@ -409,8 +437,8 @@ struct Gemm {
                 cs[k] = t.col_scale[c < o.N ? c : o.N - 1];
             }
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int64_t m = tile.m + (wm * MT + i) * 16 + r;
+            for (int i = 0; i < MO; ++i) {
+                const int64_t m = tile.m + (wm * MT + wk * MO + i) * 16 + r;
                 rs[i] = t.row_scale[m < o.M ? m : o.M - 1];
             }
         };
@@ -436,21 +464,32 @@ struct Gemm {
             // the first step has come, later ones may be on their way
             wait_steps<S - 1, kLoadsA + kLoadsB>(k1 - k0 - 1);
             barrier();
-            read(h0, lds + off_a, lds + off_b, 0, swap);
+            read(h0, lds + off_a, lds + off_b, wk, swap);
         }
         // one step; `ahead` steps (S: or more) come after it
         const auto step = [&](int k, auto ahead) {
             constexpr int kAhead = ahead;
             char* now = lds + (k - k0) % S * kBuffer;
             char* then = lds + (k - k0 + 1) % S * kBuffer;
-            read(h1, now + off_a, now + off_b, 1, swap);
-            multiply(h0, acc);
-            spread<0>();
+            if constexpr (KS == 1) {
+                read(h1, now + off_a, now + off_b, 1, swap);
+                multiply(h0, acc);
+                spread<0>();
+            }
             // the next step has come, and `now` has been read
             wait_loads<(kAhead >= S ? S - 2 : kAhead >= 2 ? kAhead - 1 : 0) *
                        (kLoadsA + kLoadsB)>();
             barrier();
             if constexpr (kAhead >= S) send(k + S);
+            if constexpr (KS == 2) {
+                if constexpr (kAhead >= 1) read(h1, then + off_a, then + off_b, wk, swap);
+                multiply(h0, acc);
+                if constexpr (kAhead >= 1) {
+                    spread<kAhead >= S ? kLoadsA + kLoadsB : 0>();
+                    h0 = h1;
+                }
+                return;
+            }
             if constexpr (kAhead >= 1) read(h0, then + off_a, then + off_b, 0, swap);
             multiply(h1, acc);
             if constexpr (kAhead >= 1) spread<kAhead >= S ? kLoadsA + kLoadsB : 0>();
@@ -472,21 +511,31 @@ struct Gemm {
                      tail, steps * kStep);
             store(last, now, wave, lane);
             __syncthreads();
-            read(h0, now + off_a, now + off_b, 0, swap);
-            read(h1, now + off_a, now + off_b, 1, swap);
+            read(h0, now + off_a, now + off_b, wk, swap);
+            if constexpr (KS == 1) read(h1, now + off_a, now + off_b, 1, swap);
             multiply(h0, acc);
-            multiply(h1, acc);
+            if constexpr (KS == 1) multiply(h1, acc);
+        }
+        typename Op::Acc sum[MO][NT];
+        if constexpr (KS == 1) {
+#pragma unroll
+            for (int i = 0; i < MO; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) sum[i][j] = acc[i][j];
+        } else {
+            static_assert(kWaves * MO * NT * 1024 <= S * kBuffer, "the sums' room");
+            join_halves<WM * WN>(acc, sum, lds, wave, lane);
         }
 
         if constexpr (!kEarly) scales();
         const int64_t n_wave = tile.n + wn * NT * 16;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int64_t m = tile.m + (wm * MT + i) * 16;
+        for (int i = 0; i < MO; ++i) {
+            const int64_t m = tile.m + (wm * MT + wk * MO + i) * 16;
             if (slices > 1) {
                 u32x4 p[NT];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) p[j] = __builtin_bit_cast(u32x4, acc[i][j]);
+                for (int j = 0; j < NT; ++j) p[j] = __builtin_bit_cast(u32x4, sum[i][j]);
                 // (the workspace has rows of whole tiles)
                 store_turned(p, static_cast<uint32_t*>(t.ws) + tile.slice * t.slice + m * t.ldws +
                                     n_wave,
@@ -497,7 +546,7 @@ struct Gemm {
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[4 * j + k] = (float)acc[i][j][k];
+                for (int k = 0; k < 4; ++k) v[4 * j + k] = (float)sum[i][j][k];
             if (t.row_scale != nullptr) {
 #pragma unroll
                 for (int k = 0; k < COLS; ++k) v[k] = v[k] * rs[i] * cs[k];
@@ -507,10 +556,11 @@ struct Gemm {
     }
 };
 
-template <class Op, int BM, int BN, int WM, int WN, int S>
-__global__ __launch_bounds__(64 * WM * WN) void gemm_kernel(Operands o, Target t, int64_t tiles_m,
-                                                            int64_t tiles_n, int slices) {
-    Gemm<Op, BM, BN, WM, WN, S>::run(o, t, tiles_m, tiles_n, slices);
+template <class Op, int BM, int BN, int WM, int WN, int S, int KS>
+__global__ __launch_bounds__(64 * WM * WN * KS) void gemm_kernel(Operands o, Target t,
+                                                                 int64_t tiles_m, int64_t tiles_n,
+                                                                 int slices) {
+    Gemm<Op, BM, BN, WM, WN, S, KS>::run(o, t, tiles_m, tiles_n, slices);
 }
 
 // Joins the slices of a product in their order: 4 columns a thread.
@@ -555,20 +605,22 @@ struct Shape {
 
 inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The tile and the slices of K that should take the least time.  A step of a
-// tile's block takes `least` ns while its CU has few others, and the CU gets
-// through one such step in `each` ns when it has many.  Measured on int8 products
-// with N = K = 4096, in us, and the best taken:
+// The tile and the slices of K that should take the least time.  A step of a tile's
+// block takes `alone` ns while its CU has no other (and `first` before the first and
+// after the last), and the CU gets through one such step in `each` ns when it has
+// several.  Measured on int8 products with N = K = 4096,
+// in us, and the best taken:
 //   rows     256 x 256   256 x 128   128 x 128   64 x 64
-//   256          47          31          28         15
-//   1024         48          33          30         32
-//   2048         49          39          44         55
-//   4096         61          74          83        105
-// A step with several parts of A takes them one after the other (256), or together,
-// with the loads of B once.  Slices are added up by a second launch: its start, and
-// each sum written and read again at 3 TB/s.
+//   256          43          28          18         10
+//   1024         45          29          23         30
+//   2048         48          35          40         55
+//   4096         57          69          76        104
+// Slices are added up by a second launch: its start, and each sum written and read
+// again at 3 TB/s.
+constexpr int64_t kCus = 256;
+
 struct TileCost {
-    int bm, bn, least, each;
+    int bm, bn, alone, each, first;
 };
 template <int TILES>
 inline Shape least_of(const TileCost (&tiles)[TILES], int64_t M, int64_t N, int64_t steps) {
@@ -579,19 +631,20 @@ inline Shape least_of(const TileCost (&tiles)[TILES], int64_t M, int64_t N, int6
         if (t.bm < 256 && n >= (int64_t)1 << 23) continue;
         for (int slices = 1; slices <= 64; slices *= 2) {
             if (slices > 1 && (t.bm != 64 || n * slices > 2048 || steps < 4 * slices)) break;
-            const double each = (double)up(n * slices, 256) * t.each;
-            const double time = (double)up(steps, slices) * (each > t.least ? each : t.least) +
+            const bool alone = n * slices <= kCus;
+            const double step = alone ? t.alone : (double)up(n * slices, kCus) * t.each;
+            const double time = (double)up(steps, slices) * step + (alone ? t.first : 0) +
                                 (slices > 1 ? 4500.0 + slices * (double)M * (double)N / 375.0 : 0);
             if (best.ns < 0 || time < best.ns) best = {t.bm, t.bn, slices, time};
         }
     }
     return best;
 }
-inline Shape shape_of(int64_t M, int64_t N, int64_t steps, int parts = 1) {
-    const TileCost tiles[] = {{256, 256, parts * 1350, parts * 1800},
-                              {256, 128, parts * 920, parts * 1100},
-                              {128, 128, 580 + 200 * parts, 230 + 390 * parts},
-                              {64, 64, 250 + 100 * parts, 105 + 115 * parts}};
+inline Shape shape_of(int64_t M, int64_t N, int64_t steps) {
+    const TileCost tiles[] = {{256, 256, 1800, 1800, 0},
+                              {256, 128, 1100, 1100, 0},
+                              {128, 128, 540, 620, 800},
+                              {64, 64, 280, 220, 0}};
     return least_of(tiles, M, N, steps);
 }
 
@@ -602,20 +655,26 @@ inline int64_t slices_bytes(int64_t M, int64_t N, const Shape& s) {
 }
 
 // Whether all blocks of a launch are on the card at once, each with `bytes` of LDS.
-inline bool all_at_once(int64_t blocks, int bytes) { return blocks <= 256 * (160 * 1024 / bytes); }
+inline bool all_at_once(int64_t blocks, int bytes) { return blocks <= kCus * (160 * 1024 / bytes); }
 
+template <class Op, int BM, int BN, int WM, int WN, int S, int KS>
+int launch_kernel(const Operands& o, const Target& t, int slices, void* stream) {
+    const int64_t tm = up(o.M, BM), tn = up(o.N, BN), blocks = tm * tn * slices;
+    constexpr int kThreads = 64 * WM * WN * KS;
+    if (blocks * kThreads >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
+    return launch(gemm_kernel<Op, BM, BN, WM, WN, S, KS>, dim3((uint32_t)blocks), kThreads, stream,
+                  o, t, tm, tn, slices);
+}
 template <class Op, int BM, int BN, int WM, int WN>
 int launch_tiles(const Operands& o, const Target& t, int slices, void* stream) {
-    const int64_t tm = up(o.M, BM), tn = up(o.N, BN), blocks = tm * tn * slices;
-    if (blocks * 64 * WM * WN >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
-    const dim3 grid((uint32_t)blocks);
-    if constexpr (BM < 256)
+    const int64_t blocks = up(o.M, BM) * up(o.N, BN) * slices;
+    if constexpr (BM < 256) {
+        if (blocks <= kCus) return launch_kernel<Op, BM, BN, WM, WN, 4, 2>(o, t, slices, stream);
         if (all_at_once(blocks, Gemm<Op, BM, BN, WM, WN, 4>::kBuffer * 4))
-            return launch(gemm_kernel<Op, BM, BN, WM, WN, 4>, grid, 64 * WM * WN, stream, o, t, tm,
-                          tn, slices);
+            return launch_kernel<Op, BM, BN, WM, WN, 4, 1>(o, t, slices, stream);
+    }
     constexpr int S = BM + BN == 384 ? 3 : 2;
-    return launch(gemm_kernel<Op, BM, BN, WM, WN, S>, grid, 64 * WM * WN, stream, o, t, tm, tn,
-                  slices);
+    return launch_kernel<Op, BM, BN, WM, WN, S, 1>(o, t, slices, stream);
 }
 
 template <class Op>

@@ -193,7 +193,7 @@ Layout layout(int64_t M, int64_t N, int64_t R, bool dy_bf16, bool out_bf16, bool
     l.Rp = up(R, kRound) * kRound;
     l.steps = l.Rp / kRound;
     l.held_as_is = l.held_scaled && (along ? M <= kHeldInput : R <= kHeldWeight);
-    l.shape = shape_of(M, N, l.steps, l.held_as_is ? kDownParts : l.parts);
+    l.shape = grad_shape(M, N, l.steps, l.parts, l.held_as_is);
     if (l.parts == 3) {
         const Shape s = f32_shape(M, N, l.steps);
         l.f32 = s.ns >= 0 && s.ns < l.shape.ns + (double)M * (double)l.Rp * kLayoutNs;

@@ -274,7 +274,7 @@ __global__ __launch_bounds__(512) void grad_f32_kernel(F32Operands o, Target t, 
 // Its slices, and its time beside that of shape_of: ns a step with a block a CU, and
 // with several.
 inline Shape f32_shape(int64_t M, int64_t N, int64_t steps) {
-    const TileCost tile[] = {{64, 64, 700, 560}};
+    const TileCost tile[] = {{64, 64, 700, 560, 0}};
     return least_of(tile, M, N, steps);
 }
 

@@ -44,18 +44,29 @@ struct GradOperands {
     int steps, parts;  // steps of one pass: R / 64, rounded up
 };
 
-// A step of an 8-bit operand that is converted on its way takes about as long as one
-// of three parts (shape_of).
-constexpr int kDownParts = 3;
+// The tile of such a product (see shape_of).  A step with several parts of A takes them
+// one after the other (256), or together, with the loads of B once; one whose 8-bit
+// operand is converted on its way takes about as long as one of three parts, by the
+// kernels with a wavefront a SIMD.
+inline Shape grad_shape(int64_t M, int64_t N, int64_t steps, int parts, bool down) {
+    const int p = down ? 3 : parts, each = 230 + 390 * p;
+    const TileCost tiles[] = {
+        {256, 256, p * 1800, p * 1800, 0},
+        {256, 128, p * 1100, p * 1100, 0},
+        {128, 128, down ? each : 310 + 290 * p, each, down ? 0 : 800},
+        {64, 64, 250 + 100 * p, 105 + 115 * p, 0}};
+    return least_of(tiles, M, N, steps);
+}
 
-template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P, int S>
+template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P, int S, int KS = 1>
 struct GradGemm {
     using G = Gemm<Bf16, BM, BN, WM, WN, 2>;
-    static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+    static constexpr int kWaves = WM * WN * KS;
     static constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
     static_assert(!BDOWN || NT == 4, "4 columns of B a lane");
     static_assert(BDOWN || !ADOWN, "as it is, A meets B as it is");
     static_assert(P == 1 || !BDOWN, "parts are laid out");
+    static_assert(KS == 1 || !BDOWN, "halves of laid out steps");
     static constexpr int kRows = kStep / 2;  // of a step
     static constexpr int kPart = BM * kStep, kA = P * kPart, kB = BDOWN ? kRows * BN : BN * kStep;
     static constexpr int kBuffer = kA + kB + (BDOWN ? 256 : 0);
@@ -163,7 +174,7 @@ struct GradGemm {
     };
     static __device__ __forceinline__ At at(int wave, int lane) {
         At t;
-        const int wm = wave / WN, wn = wave % WN, r = lane & 15, g = lane >> 4;
+        const int wm = wave / WN % WM, wn = wave % WN, r = lane & 15, g = lane >> 4;
         t.swap = (g ^ (r >> 1)) << 4;
         if constexpr (ADOWN) {
             // row 8 g + r / 4, columns 4 (r % 4) on
@@ -282,6 +293,7 @@ struct GradGemm {
         };
 
         const At at_ = at(wave, lane);
+        const int wk = KS == 1 ? 0 : wave / (WM * WN);  // (see Gemm)
         f32x4 acc[MT][NT] = {};
         Half h0, h1;
         // loads of a step; the first wavefront has the scales too
@@ -297,7 +309,7 @@ struct GradGemm {
             if (BDOWN && wave == 0) wait_steps<S - 1, kLoads + 1>(k1 - k0 - 1);
             else wait_steps<S - 1, kLoads>(k1 - k0 - 1);
             barrier();
-            read(h0, lds, at_, 0);
+            read(h0, lds, at_, wk);
             convert(h0);
         }
         // one step; `ahead` steps (S: or more) come after it, S + 1: the step S on may
@@ -306,13 +318,24 @@ struct GradGemm {
             constexpr int kAhead = ahead;
             char* now = lds + (k - k0) % S * kBuffer;
             char* then = lds + (k - k0 + 1) % S * kBuffer;
-            read(h1, now, at_, 1);
-            multiply(h0, acc);
-            spread<0>();
-            convert(h1);
+            if constexpr (KS == 1) {
+                read(h1, now, at_, 1);
+                multiply(h0, acc);
+                spread<0>();
+                convert(h1);
+            }
             wait(Int<(kAhead >= S ? S - 2 : kAhead >= 2 ? kAhead - 1 : 0)>());
             barrier();
             if constexpr (kAhead >= S) send(now, std::integral_constant<bool, (kAhead > S)>());
+            if constexpr (KS == 2) {
+                if constexpr (kAhead >= 1) read(h1, then, at_, wk);
+                multiply(h0, acc);
+                if constexpr (kAhead >= 1) {
+                    spread<kAhead >= S ? kLoads : 0>();
+                    h0 = h1;
+                }
+                return;
+            }
             if constexpr (kAhead >= 1) read(h0, then, at_, 0);
             multiply(h1, acc);
             if constexpr (kAhead >= 1) {
@@ -334,16 +357,28 @@ struct GradGemm {
         if (k < k1 - 1) step(k++, Int<1>());
         if (k < k1) step(k, Int<0>());
 
-        // lane: 4 NT columns of MT rows
-        const int wm = wave / WN, wn = wave % WN, r = lane & 15, g = lane >> 4;
+        constexpr int MO = MT / KS;
+        f32x4 sum[MO][NT];
+        if constexpr (KS == 1) {
+#pragma unroll
+            for (int i = 0; i < MO; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) sum[i][j] = acc[i][j];
+        } else {
+            static_assert(kWaves * MO * NT * 1024 <= S * kBuffer, "the sums' room");
+            join_halves<WM * WN>(acc, sum, lds, wave, lane);
+        }
+
+        // lane: 4 NT columns of MO rows
+        const int wm = wave / WN % WM, wn = wave % WN, r = lane & 15, g = lane >> 4;
         const int64_t n = tile.n + wn * NT * 16;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int64_t m = tile.m + (wm * MT + i) * 16;
+        for (int i = 0; i < MO; ++i) {
+            const int64_t m = tile.m + (wm * MT + wk * MO + i) * 16;
             float v[4 * NT];
 #pragma unroll
             for (int c = 0; c < 4 * NT; ++c)
-                v[c] = BDOWN ? acc[i][c % 4][c / 4] : acc[i][c / 4][c % 4];
+                v[c] = BDOWN ? sum[i][c % 4][c / 4] : sum[i][c / 4][c % 4];
             if (slices > 1) {
                 u32x4 p[NT];
 #pragma unroll
@@ -358,26 +393,36 @@ struct GradGemm {
     }
 };
 
-template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P, int S>
-__global__ __launch_bounds__(64 * WM * WN) void grad_gemm_kernel(GradOperands o, Target t,
-                                                                 int64_t tiles_m, int64_t tiles_n,
-                                                                 int slices) {
-    GradGemm<BM, BN, WM, WN, ADOWN, BDOWN, P, S>::run(o, t, tiles_m, tiles_n, slices);
+template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P, int S, int KS>
+__global__ __launch_bounds__(64 * WM * WN * KS) void grad_gemm_kernel(GradOperands o, Target t,
+                                                                      int64_t tiles_m,
+                                                                      int64_t tiles_n,
+                                                                      int slices) {
+    GradGemm<BM, BN, WM, WN, ADOWN, BDOWN, P, S, KS>::run(o, t, tiles_m, tiles_n, slices);
 }
 
+template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P, int S, int KS>
+int launch_grad_kernel(const GradOperands& o, const Target& t, int slices, void* stream) {
+    const int64_t tm = up(o.M, BM), tn = up(o.N, BN), blocks = tm * tn * slices;
+    constexpr int kThreads = 64 * WM * WN * KS;
+    if (blocks * kThreads >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
+    return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, S, KS>, dim3((uint32_t)blocks),
+                  kThreads, stream, o, t, tm, tn, slices);
+}
 template <int BM, int BN, int WM, int WN, bool ADOWN, bool BDOWN, int P>
 int launch_grad_tiles(const GradOperands& o, const Target& t, int slices, void* stream) {
-    const int64_t tm = up(o.M, BM), tn = up(o.N, BN), blocks = tm * tn * slices;
-    if (blocks * 64 * WM * WN >= ((int64_t)1 << 32)) return (int)hipErrorInvalidValue;
-    const dim3 grid((uint32_t)blocks);
+    const int64_t blocks = up(o.M, BM) * up(o.N, BN) * slices;
     constexpr int kDeep = 4 * GradGemm<BM, BN, WM, WN, ADOWN, BDOWN, P, 4>::kBuffer;
+    // (64 x 64 tiles gain nothing by it)
+    if constexpr (BM == 128 && !BDOWN)
+        if (blocks <= kCus)
+            return launch_grad_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P,
+                                      kDeep <= 160 * 1024 ? 4 : 2, 2>(o, t, slices, stream);
     if constexpr (BM < 256 && kDeep <= 160 * 1024)
         if (all_at_once(blocks, kDeep))
-            return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, 4>, grid,
-                          64 * WM * WN, stream, o, t, tm, tn, slices);
+            return launch_grad_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, 4, 1>(o, t, slices, stream);
     constexpr int S = BM + BN == 384 ? 3 : 2;
-    return launch(grad_gemm_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, S>, grid, 64 * WM * WN, stream,
-                  o, t, tm, tn, slices);
+    return launch_grad_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, S, 1>(o, t, slices, stream);
 }
 
 template <bool ADOWN, bool BDOWN, int P>
