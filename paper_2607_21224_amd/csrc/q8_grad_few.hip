@@ -17,26 +17,20 @@ namespace {
 
 constexpr int kSum = 32;  // values of the sum that one instruction takes
 
-// 8 rows of int8, W columns (4 or 8) a lane: rows that are past the last one repeat
-// it (their partners are zeros), columns past the last one are zeros.
+// 8 rows of int8, W columns (4 or 8) a lane.  Rows that are past the last one repeat
+// it (their partners are zeros), and so do columns past the last piece (what they come
+// to is not stored): no load is behind a branch, and all are on their way together.
 template <int W>
 struct Octet {
     uint32_t w[8][W / 4];
     __device__ __forceinline__ void load(const int8_t* p, int64_t ld, int64_t row, int64_t rows,
                                          int64_t col, int64_t cols) {
+        const int64_t last = (cols - 1) / W * W, c = col < last ? col : last;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int8_t* q = p + (row + i < rows ? row + i : rows - 1) * ld + col;
-            if (cols - col >= W) {
+            const int8_t* q = p + (row + i < rows ? row + i : rows - 1) * ld + c;
 #pragma unroll
-                for (int k = 0; k < W / 4; ++k) w[i][k] = reinterpret_cast<const uint32_t*>(q)[k];
-                continue;
-            }
-#pragma unroll
-            for (int k = 0; k < W / 4; ++k) w[i][k] = 0;
-#pragma unroll
-            for (int k = 0; k < W - 1; ++k)
-                if (k < cols - col) w[i][k / 4] |= (uint32_t)(uint8_t)q[k] << (8 * (k % 4));
+            for (int k = 0; k < W / 4; ++k) w[i][k] = reinterpret_cast<const uint32_t*>(q)[k];
         }
     }
     // column c of the 8 rows (exact: a number of 8 bits has no bits past a bf16's)
@@ -172,6 +166,44 @@ int few_input_rows(Mat dy, Held b, int64_t T, int64_t N, int64_t K, const Target
     return few_input<E, P, 2>(dy, b, T, N, K, t, slices, stream);
 }
 
+// Stores 16 rows of COLS columns that lie in LDS to rows m0, m0 + apart, .. of C.
+template <class E, int COLS>
+__device__ __forceinline__ void store_tile(const float (&tile)[16][COLS + 4], const Target& t,
+                                           int64_t m0, int apart, int64_t M, int64_t k0, int64_t K,
+                                           int lane) {
+    constexpr int kEach = 16 / sizeof(E);
+    constexpr int kLanes = COLS / kEach, kRows = 64 / kLanes;  // of one store
+#pragma unroll
+    for (int i = 0; i < 16; i += kRows) {
+        const int row = i + lane / kLanes, col = lane % kLanes * kEach;
+        float v[kEach];
+#pragma unroll
+        for (int h = 0; h < kEach; h += 4) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(&tile[row][col + h]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[h + k] = x[k];
+        }
+        const int64_t m = m0 + row * apart, c = k0 + col;
+        if (m >= M || c >= K) continue;
+        E* at = static_cast<E*>(t.c) + m * t.ldc + c;
+        if (K - c >= kEach) {
+            u32x4 p;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (sizeof(E) == 2) p[k] = narrow2(v[2 * k], v[2 * k + 1]);
+                else p[k] = __float_as_uint(v[k]);
+            }
+            // past the caches: the weights' gradients are read when a step is due, long
+            // after (4096 x 4096 fp32 of 64 tokens 27.5 us otherwise, and 22 so)
+            __builtin_nontemporal_store(p, reinterpret_cast<u32x4*>(at));
+        } else {
+#pragma unroll
+            for (int k = 0; k < kEach - 1; ++k)
+                if (k < K - c) narrow(v[k], at + k);
+        }
+    }
+}
+
 // dw [N x K], a sum over at most 64 tokens.  A wavefront takes 16 WN rows and 16 WK
 // columns: each lane WN columns of dy and WK of a.
 template <class E, int P, int WN, int WK>
@@ -185,30 +217,29 @@ __global__ __launch_bounds__(256) void few_weight_kernel(const typename E::T* dy
     const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n0 = at / across * 16 * WN, k0 = at % across * kCols;
     if (n0 >= N) return;
-    const int64_t n = n0 + r * WN;
+    // columns of dy past the last piece repeat it (what they come to is not stored)
+    const int64_t last = (N - 1) / WN * WN, n = n0 + r * WN, n_there = n < last ? n : last;
     f32x4 acc[WK][WN] = {};
     for (int t0 = 0; t0 < T; t0 += kSum) {
         const int row = t0 + g * 8;
         Octet<WK> w;
         w.load(a, lda, row, T, k0 + r * WK, K);
         float x[8][WN];
+        // (as with a: no branch; a token that is not there is zeros, whatever the last one
+        // holds)
+        typename E::T e[8][WN];
+        float f[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const bool there = row + i < T && n < N;
-            const typename E::T* p = dy + (there ? row + i : 0) * lddy + (there ? n : 0);
-            const float f = there ? scale[row + i] : 0.0f;
-            if (there && N - n >= WN) {
-                typename E::T e[WN];
-                __builtin_memcpy(e, __builtin_assume_aligned(p, sizeof(e)), sizeof(e));
-#pragma unroll
-                for (int k = 0; k < WN; ++k) x[i][k] = widen(e[k]) * f;
-            } else {
-                // (a scale that is not finite reaches the columns that are there)
-#pragma unroll
-                for (int k = 0; k < WN; ++k)
-                    x[i][k] = there && k < N - n ? widen(p[k]) * f : 0.0f;
-            }
+            const int t = row + i < T ? row + i : T - 1;
+            const typename E::T* p = dy + t * lddy + n_there;
+            __builtin_memcpy(e[i], __builtin_assume_aligned(p, sizeof(e[i])), sizeof(e[i]));
+            f[i] = scale[t];
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int k = 0; k < WN; ++k) x[i][k] = row + i < T ? widen(e[i][k]) * f[i] : 0.0f;
         u32x4 d[WN][P];
 #pragma unroll
         for (int c = 0; c < WN; ++c) {
@@ -228,10 +259,9 @@ __global__ __launch_bounds__(256) void few_weight_kernel(const typename E::T* dy
     }
     // A lane holds rows WN r to WN r + WN - 1, columns 4 WK g to 4 WK g + 4 WK - 1.
     // Its wavefront turns them over in LDS, 16 rows at a time, so that a store
-    // covers whole rows of the tile: straight from the registers, 16 bytes here and
-    // there, 4096 x 4096 took 23 to 33 us and not 13 to 18.
+    // covers whole rows of the tile, 16 bytes a lane: straight from the registers, 16
+    // bytes here and there, 4096 x 4096 took 10 to 15 us more.
     float(*mine)[16][kCols + 4] = &turn[threadIdx.x >> 6];
-    constexpr int kLanes = kCols / 8, kRows = 64 / kLanes;  // of one store
 #pragma unroll
     for (int j = 0; j < WN; ++j) {
 #pragma unroll
@@ -242,19 +272,8 @@ __global__ __launch_bounds__(256) void few_weight_kernel(const typename E::T* dy
                     f32x4{acc[c][j][i], acc[c + 1][j][i], acc[c + 2][j][i], acc[c + 3][j][i]};
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int i = 0; i < 16; i += kRows) {
-            const int row = i + lane / kLanes, col = lane % kLanes * 8;
-            float v[8];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const f32x4 x = *reinterpret_cast<const f32x4*>(&(*mine)[row][col + h * 4]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[h * 4 + k] = x[k];
-            }
-            const int64_t m = n0 + row * WN + j, c0 = k0 + col;
-            if (m < N && c0 < K) store_cols<8>(t, m, c0, least(K - c0, 8), v);
-        }
+        if (t.bf16) store_tile<uint16_t, kCols>(*mine, t, n0 + j, WN, N, k0, K, lane);
+        else store_tile<float, kCols>(*mine, t, n0 + j, WN, N, k0, K, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
@@ -270,14 +289,14 @@ int few_weight_tiles(Mat dy, Held a, int64_t T, int64_t N, int64_t K, const Targ
                   across, t);
 }
 
-// Wider tiles store whole 256-byte rows and take a's columns once for more rows,
-// where there are enough of them for two wavefronts a SIMD (bf16, T = 1 and 64,
-// 4096 x 4096: 12 and 18 us, narrow ones 14 and 24); narrow ones are done sooner
-// (f32, 500 x 300: 9 us, wide ones 15).
+// Wider tiles take a's columns once for more of dw, where there are enough of them for
+// most SIMDs (bf16, T = 1 and 64, 4096 x 4096: 9 and 12.4 us, narrow ones 11 and 16.7;
+// 40 x 2000 x 2000 6.8 and 7.4); narrow ones are done sooner (fp32, 1536 x 384: 4.2 us,
+// wide ones 5.2).
 template <class E, int P>
 int few_weight(Mat dy, Held a, int64_t T, int64_t N, int64_t K, const Target& t, void* stream) {
-    return up(N, 32) * up(K, 128) >= 2048 ? few_weight_tiles<E, P, 2, 8>(dy, a, T, N, K, t, stream)
-                                          : few_weight_tiles<E, P, 2, 4>(dy, a, T, N, K, t, stream);
+    return up(N, 32) * up(K, 128) >= 768 ? few_weight_tiles<E, P, 2, 8>(dy, a, T, N, K, t, stream)
+                                         : few_weight_tiles<E, P, 2, 4>(dy, a, T, N, K, t, stream);
 }
 
 }  // namespace
