@@ -598,7 +598,7 @@ __global__ __launch_bounds__(256) void join_kernel(Target t, int64_t M, int64_t 
 // ---- which tile takes a product ----------------------------------------------------
 
 struct Shape {
-    int bm, bn;  // 256 x 256, 256 x 128, 128 x 128 or 64 x 64
+    int bm, bn;  // 256 x 256, 256 x 128, 128 x 128, 128 x 64 or 64 x 64
     int slices;  // of K
     double ns;   // it should take
 };
@@ -608,8 +608,9 @@ inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // The tile and the slices of K that should take the least time.  A step of a tile's
 // block takes `alone` ns while its CU has no other (and `first` before the first and
 // after the last), and the CU gets through one such step in `each` ns when it has
-// several.  Measured on int8 products with N = K = 4096,
-// in us, and the best taken:
+// several (0: not taken then; a tile of 128 x 64 is for up to twice as many tiles of
+// 64 x 64 as there are CUs: 512 x 4096 x 4096 14.5 -> 12.8 us).  Measured on int8
+// products with N = K = 4096, in us, and the best taken:
 //   rows     256 x 256   256 x 128   128 x 128   64 x 64
 //   256          43          28          18         10
 //   1024         45          29          23         30
@@ -632,6 +633,7 @@ inline Shape least_of(const TileCost (&tiles)[TILES], int64_t M, int64_t N, int6
         for (int slices = 1; slices <= 64; slices *= 2) {
             if (slices > 1 && (t.bm != 64 || n * slices > 2048 || steps < 4 * slices)) break;
             const bool alone = n * slices <= kCus;
+            if (!alone && t.each == 0) break;
             const double step = alone ? t.alone : (double)up(n * slices, kCus) * t.each;
             const double time = (double)up(steps, slices) * step + (alone ? t.first : 0) +
                                 (slices > 1 ? 4500.0 + slices * (double)M * (double)N / 375.0 : 0);
@@ -644,6 +646,7 @@ inline Shape shape_of(int64_t M, int64_t N, int64_t steps) {
     const TileCost tiles[] = {{256, 256, 1800, 1800, 0},
                               {256, 128, 1100, 1100, 0},
                               {128, 128, 540, 620, 800},
+                              {128, 64, 350, 0, 500},
                               {64, 64, 280, 220, 0}};
     return least_of(tiles, M, N, steps);
 }
@@ -692,7 +695,8 @@ int launch_gemm(const Operands& o, Target t, void* ws, void* stream) {
     t.slice = o.M * t.ldws;
     if (s.bn == 256) return launch_tiles<Op, 256, 256, 2, 4>(o, t, 1, stream);
     if (s.bm == 256) return launch_tiles<Op, 256, 128, 4, 2>(o, t, 1, stream);
-    if (s.bm == 128) return launch_tiles<Op, 128, 128, 2, 2>(o, t, 1, stream);
+    if (s.bn == 128) return launch_tiles<Op, 128, 128, 2, 2>(o, t, 1, stream);
+    if (s.bm == 128) return launch_kernel<Op, 128, 64, 2, 2, 4, 2>(o, t, 1, stream);
     if (int e = launch_tiles<Op, 64, 64, 2, 2>(o, t, s.slices, stream)) return e;
     if (s.slices == 1) return 0;
     return launch_join<Op>(t, o.M, o.N, s.slices, stream);

@@ -36,6 +36,21 @@ def test_product(q8, M, N, K):  # noqa: F811
     untouched(half)
 
 
+@pytest.mark.parametrize("M,N,K", [(500, 4001, 1031), (512, 4096, 1024), (1700, 1100, 2000),
+                                   (130, 8190, 1500), (1750, 901, 816)])
+def test_product_of_tiles_of_128_x_64(q8, M, N, K):  # noqa: F811
+    g = gen(M + 2 * N + K)
+    a, b = put(ints(g, M, K), torch.int8, 20), put(ints(g, N, K), torch.int8, 3)
+    sa, sb = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+    y, half = blank(M, N, torch.float32, 5), blank(M, N, torch.bfloat16, 5)
+    q8.cpdp_q8_matmul(a, sa, b, sb, y)
+    q8.cpdp_q8_matmul(a, sa, b, sb, half)
+    want = torch.mm(a.double(), b.double().t().contiguous()) * torch.outer(sa.double(), sb.double())
+    assert bool(((y.double() - want).abs() <= 3 * U * want.abs()).all())
+    assert torch.equal(half, y.to(torch.bfloat16))
+    untouched(y, half)
+
+
 def test_product_of_extremes(q8):  # noqa: F811
     M, N, K = 1025, 2100, 1111
     one_m, one_n = torch.ones(M, device="cuda"), torch.ones(N, device="cuda")
