@@ -144,9 +144,9 @@ int norm_typed(Mat x, Mat res, const void* w, bool w_bf16, float eps, int64_t T,
 // dw = sum over rows of dy n.  A block takes every G-th row and keeps its
 // columns' part of dw in registers (where a wavefront holds a row, the block's four
 // meet in LDS); the G parts go to the workspace and are added in their order by a
-// second launch, so the result does not depend on which block ran first.  Joining the
-// wavefronts' own parts, four times as many, made 1576 x 384 fp32
-// 9.4 us and 16384 x 512 bf16 22, now 7.7 and 16.
+// second launch, so the result does not depend on which block ran first (few and short
+// rows: norm_bwd_one_kernel).  Joining the wavefronts' own parts, four times as many,
+// made 1576 x 384 fp32 9.4 us and 16384 x 512 bf16 22, now 7.7 and 16.
 
 // Floats from part to part: whole 16-byte pieces.
 __host__ __device__ constexpr int64_t parts_ld(int64_t D) { return (D + 3) / 4 * 4; }
@@ -241,6 +241,95 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_bwd_kernel(
     for (int j = 0; j < CH; ++j) {
         const int c = (j * TPR + lane) * kPiece;
         if (c < D) store8(part + c, D - c, acc[j]);
+    }
+}
+
+// Both in one launch, for few and short rows: the first blocks take 8 columns of dw
+// each, over all rows, the others a row of dx (four, where a wavefront holds one).  dy
+// and h are read twice, by the first blocks a piece here and there, which costs less
+// than a second launch as long as they are small (bwd_one).
+template <class E, int TPR, int CH>
+__global__ __launch_bounds__(block_of(TPR)) void norm_bwd_one_kernel(
+    const typename E::T* dy, int64_t lddy, const typename E::T* h, int64_t ldh,
+    const typename E::T* dres, int64_t lddres, const void* w, bool w_bf16, const float* rstd,
+    int T, int D, typename E::T* dx, int64_t lddx, void* dw, bool dw_bf16, int dw_blocks) {
+    constexpr int kThreads = block_of(TPR), kWaves = kThreads / 64;
+    if ((int)blockIdx.x < dw_blocks) {
+        __shared__ float sums[kWaves][kPiece];
+        const int c = (int)blockIdx.x * kPiece;
+        float acc[kPiece] = {};
+        constexpr int U = 4;  // rows on their way
+        for (int row = (int)threadIdx.x; row < T; row += U * kThreads) {
+            Raw<E> g[U], n[U];
+            float rs[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = row + u * kThreads < T ? row + u * kThreads : row;
+                g[u].load(dy + at * lddy + c, D - c, c);
+                n[u].load(h + at * ldh + c, D - c, c);
+                rs[u] = rstd[at];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool there = row + u * kThreads < T;
+#pragma unroll
+                for (int k = 0; k < kPiece; ++k)
+                    acc[k] = there ? fmaf(g[u][k], n[u][k] * rs[u], acc[k]) : acc[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) acc[k] = wave_reduce(acc[k], Add());
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < kPiece; ++k) sums[threadIdx.x >> 6][k] = acc[k];
+        }
+        __syncthreads();
+        const int k = (int)threadIdx.x;
+        if (k >= kPiece || c + k >= D) return;
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) s += sums[i][k];
+        if (dw_bf16) narrow(s, static_cast<uint16_t*>(dw) + c + k);
+        else static_cast<float*>(dw)[c + k] = s;
+        return;
+    }
+    __shared__ RowWords<TPR, 0> words;
+    const int row =
+        ((int)blockIdx.x - dw_blocks) * rows_of(TPR) + (int)threadIdx.x / TPR;
+    const int lane = (int)threadIdx.x % TPR;
+    if (row >= T) return;  // a whole wavefront, in the one-wavefront form only
+    const float rs = rstd[row];
+    float sum = 0.0f, gw[CH][kPiece], nv[CH][kPiece], r[CH][kPiece] = {};
+    uint32_t none[1];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int c = (j * TPR + lane) * kPiece;
+        if (c < D) {
+            float wv[kPiece];
+            load8(dy + row * lddy + c, D - c, c, gw[j]);
+            load8(h + row * ldh + c, D - c, c, nv[j]);
+            load_w(w, w_bf16, c, D - c, wv);
+            if (dres != nullptr) load8(dres + row * lddres + c, D - c, c, r[j]);
+#pragma unroll
+            for (int k = 0; k < kPiece; ++k) {
+                nv[j][k] *= rs;
+                gw[j][k] *= wv[k];
+                sum = fmaf(gw[j][k], nv[j][k], sum);
+            }
+        }
+    }
+    row_reduce<TPR, true, 0>(sum, none, words);
+    const float mean = sum / (float)D;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int c = (j * TPR + lane) * kPiece;
+        if (c < D) {
+            float d[kPiece];
+#pragma unroll
+            for (int k = 0; k < kPiece; ++k)
+                d[k] = fmaf(fmaf(-nv[j][k], mean, gw[j][k]), rs, r[j][k]);
+            store8(dx + row * lddx + c, D - c, d);
+        }
     }
 }
 
@@ -351,6 +440,15 @@ int64_t bwd_blocks(int64_t T, int rows) {
     return blocks < 1 ? 1 : blocks > 1024 ? 1024 : blocks;
 }
 
+// Whether one launch takes both: as long as a thread has two turns of four rows, a
+// block's 256 threads suffice for a row, and dy is so small that reading it and h again
+// is nothing.  In us, two launches and one: 256 x 384 fp32 7.3 and 5.0, 1576 x 384 bf16
+// 7.4 and 5.5, 64 x 7264 7.6 and 6.2; but 1576 x 384 fp32 (2.4 MB) 7.3 and 9.7, 3000 x 96
+// 7.3 and 8.5, 5 x 8191 7.7 and 8.7.
+bool bwd_one(int64_t T, int64_t D, int64_t element) {
+    return T <= 2048 && D <= 4096 && T * D * element <= 3 << 19;
+}
+
 template <class E>
 int norm_bwd_typed(Mat dy, Mat h, Mat dres, const void* w, bool w_bf16, const float* rstd,
                    int64_t T, int D, Mat dx, void* dw, bool dw_bf16, float* parts, void* stream) {
@@ -359,6 +457,7 @@ int norm_bwd_typed(Mat dy, Mat h, Mat dres, const void* w, bool w_bf16, const fl
              *rp = static_cast<const ET*>(dres.p);
     ET* dxp = static_cast<ET*>(dx.p);
     int groups = 0;
+    bool done = false;
     int e = with_bwd_shape(D, [&](auto tpr, auto ch) {
         if constexpr (tpr == 0) {
             groups = (int)bwd_blocks(T, 4);
@@ -374,13 +473,21 @@ int norm_bwd_typed(Mat dy, Mat h, Mat dres, const void* w, bool w_bf16, const fl
                                (uint32_t)groups),
                           256, stream, dyp, dy.ld, hp, h.ld, rstd, T, D, parts);
         } else {
+            if (bwd_one(T, D, sizeof(ET))) {
+                done = true;
+                const int dw_blocks = (D + kPiece - 1) / kPiece;
+                const int64_t rows = (T + rows_of(tpr) - 1) / rows_of(tpr);
+                return launch(norm_bwd_one_kernel<E, tpr, ch>, dim3((uint32_t)(dw_blocks + rows)),
+                              block_of(tpr), stream, dyp, dy.ld, hp, h.ld, rp, dres.ld, w, w_bf16,
+                              rstd, (int)T, D, dxp, dx.ld, dw, dw_bf16, dw_blocks);
+            }
             groups = (int)bwd_blocks(T, rows_of(tpr));
             return launch(norm_bwd_kernel<E, tpr, ch>, dim3((uint32_t)groups), block_of(tpr),
                           stream, dyp, dy.ld, hp, h.ld, rp, dres.ld, w, w_bf16, rstd, T, D, dxp,
                           dx.ld, parts);
         }
     });
-    if (e) return e;
+    if (e || done) return e;
     const dim3 grid((uint32_t)((D + 31) / 32));
     return dw_bf16 ? launch(norm_dw_join_kernel<BF16>, grid, 1024, stream, parts, groups, D,
                             static_cast<uint16_t*>(dw))
