@@ -80,8 +80,10 @@ __global__ __launch_bounds__(64 * WAVES) void few_input_kernel(
         const int64_t n = s * kSum + g * 8;
         Octet<8> w;
         w.load(b, ldb, n, N, k0 + r * 8, K);
+        // (past the last row the last piece of the scales, as with b: not used)
+        const int64_t n_there = n < N ? n : (N - 1) / 8 * 8;
         float f[8];
-        load8(scale + (n < N ? n : 0), n < N ? least(N - n, 8) : 0, n < 8 ? (int)n : 8, f);
+        load8(scale + n_there, least(N - n_there, 8), least(n_there, 8), f);
         u32x4 d[MT][P];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
