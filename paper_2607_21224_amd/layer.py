@@ -22,6 +22,8 @@ quarter of fp32 and half of bf16, for each of the replicas on the GPU::
 Forward, with `8(.)` for rounding to 8-bit rows (cpdp_q8.h):
     h = x + residual;  n = 8(norm(h) * w);  z = n 8(W1)^T;  a = 8(act(z))
     y = a 8(W2)^T
+The gated kind's two inner products are one, of twice the channels: their weights follow
+each other in a row, and g and u are the halves of z.
 Backward passes gradients through the roundings unchanged, and uses the rounded
 operands.
 """
@@ -47,6 +49,7 @@ class Saved:
             return torch.empty(n, device=device)
 
         D, F, i8 = mlp.dim, mlp.hidden, torch.int8
+        halves = range(0, mlp.inner, F)
         self.T = T
         # one byte an activation: the norm's output, the activation's inputs and
         # output, and the weights as they were used
@@ -54,12 +57,14 @@ class Saved:
         self.cg, self.g_scale = rows(T, F, i8), vec(T)
         self.cu, self.u_scale = (rows(T, F, i8), vec(T)) if mlp.gated else (None, None)
         self.a, self.a_scale = rows(T, F, i8), vec(T)
-        self.w1 = [(rows(F, D, i8), vec(F)) for _ in range(2 if mlp.gated else 1)]
+        q, scale = self.w_in = rows(mlp.inner, D, i8), vec(mlp.inner)
+        self.w1 = [(q[i:i + F], scale[i:i + F]) for i in halves]
         self.w2 = rows(D, F, i8), vec(D)
         # the sum that the norm is taken of, the result, and what lives for a while
         self.h, self.y, self.dx = rows(T, D), rows(T, D), rows(T, D)
-        self.z = [rows(T, F) for _ in range(2 if mlp.gated else 1)]
-        self.da, self.dn = rows(T, F), [rows(T, D) for _ in range(2 if mlp.gated else 1)]
+        self.z_all = rows(T, mlp.inner)
+        self.z = [self.z_all[:, i:i + F] for i in halves]
+        self.da, self.dn = rows(T, F), rows(T, D)
         self.workspace = torch.empty(mlp.workspace_bytes(T), dtype=torch.uint8, device=device)
 
 
@@ -78,6 +83,7 @@ class Q8Mlp:
                              "after the other in a replica's row, each on a 16-byte boundary")
         self.dim, self.hidden, self.kind, self.eps = int(dim), int(hidden), kind, float(eps)
         self.gated = kind == "swiglu"
+        self.inner = self.hidden * (2 if self.gated else 1)  # channels of z
         self.act_dtype = _DT[act_dt]
         shapes = [("norm", (dim,)), ("w1", (hidden, dim))]
         if self.gated:
@@ -96,6 +102,11 @@ class Q8Mlp:
         n = shape[0] * (shape[1] if len(shape) == 2 else 1)
         return row[at:at + n].view(shape)
 
+    def _w_in(self, row: torch.Tensor) -> torch.Tensor:
+        """The inner product's weights, (inner, dim): w1, and w1u after it."""
+        at, _ = self.tensors["w1"]
+        return row[at:at + self.inner * self.dim].view(self.inner, self.dim)
+
     def init(self, generator: torch.Generator | None = None, device="cuda") -> torch.Tensor:
         """Initial parameters, (numel,) fp32: the norm's weight 1, the others normal
         with the variance 1 / inputs."""
@@ -111,10 +122,10 @@ class Q8Mlp:
 
     def workspace_bytes(self, T: int) -> int:
         """The largest workspace of the layer's calls over T tokens."""
-        D, F, dt = self.dim, self.hidden, self.act_dtype
-        need = [q8.cpdp_q8_matmul_workspace(T, F, D), q8.cpdp_q8_matmul_workspace(T, D, F),
+        D, F, I, dt = self.dim, self.hidden, self.inner, self.act_dtype
+        need = [q8.cpdp_q8_matmul_workspace(T, I, D), q8.cpdp_q8_matmul_workspace(T, D, F),
                 q8.cpdp_q8_norm_bwd_workspace(T, D)]
-        for N, K in ((F, D), (D, F)):
+        for N, K in ((I, D), (D, F)):
             need.append(q8.cpdp_q8_grad_input_workspace(T, N, K, dt, dt))
             need += [q8.cpdp_q8_grad_weight_workspace(T, N, K, dt, g) for g in _DT.values()]
         return max(need + [16])
@@ -131,9 +142,8 @@ class Q8Mlp:
             q8.cpdp_q8_norm(x, self.view(params, "norm"), self.eps, q=s.n, scale=s.n_scale,
                             rstd=s.rstd, residual=residual, h=s.h, stream=stream)
             s.norm_of = s.h
-        for name, (w, scale), z in zip(("w1", "w1u"), s.w1, s.z):
-            q8.cpdp_q8_rows(self.view(params, name), w, scale, stream=stream)
-            q8.cpdp_q8_matmul(s.n, s.n_scale, w, scale, z, workspace=s.workspace, stream=stream)
+        q8.cpdp_q8_rows(self._w_in(params), *s.w_in, stream=stream)
+        q8.cpdp_q8_matmul(s.n, s.n_scale, *s.w_in, s.z_all, workspace=s.workspace, stream=stream)
         q8.cpdp_q8_act(self.kind, *s.z, q=s.a, scale=s.a_scale, cg=s.cg, sg=s.g_scale, cu=s.cu,
                        su=s.u_scale, stream=stream)
         q8.cpdp_q8_rows(self.view(params, "w2"), *s.w2, stream=stream)
@@ -151,18 +161,8 @@ class Q8Mlp:
         # z is done with: its gradient takes its place
         q8.cpdp_q8_act_bwd(self.kind, s.da, s.cg, s.g_scale, s.z[0], cu=s.cu, su=s.u_scale,
                            du=s.z[1] if self.gated else None, stream=stream)
-        for name, w, dz, dn in zip(("w1", "w1u"), s.w1, s.z, s.dn):
-            q8.cpdp_q8_grad_weight(dz, s.n, s.n_scale, self.view(grads, name), **kw)
-            q8.cpdp_q8_grad_input(dz, *w, dn, **kw)
-        dn = s.dn[0]
-        if self.gated:
-            with torch.cuda.stream(_torch_stream(stream)):
-                dn.add_(s.dn[1])
-        q8.cpdp_q8_norm_bwd(dn, s.norm_of, self.view(params, "norm"), s.rstd, s.dx,
+        q8.cpdp_q8_grad_weight(s.z_all, s.n, s.n_scale, self._w_in(grads), **kw)
+        q8.cpdp_q8_grad_input(s.z_all, *s.w_in, s.dn, **kw)
+        q8.cpdp_q8_norm_bwd(s.dn, s.norm_of, self.view(params, "norm"), s.rstd, s.dx,
                             self.view(grads, "norm"), dres=dres, **kw)
         return s.dx
-
-
-def _torch_stream(stream):
-    """A stream argument for torch's own operations (None: the current one)."""
-    return torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
