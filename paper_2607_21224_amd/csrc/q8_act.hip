@@ -27,6 +27,18 @@ __device__ __forceinline__ float activation(float g, float u) {
     else return g * reciprocal(1.0f + expf(-g)) * u;
 }
 
+// 1 + erf cancels for negative g: far below zero its error, about |g| 2^-25, is no longer
+// small beside g Phi(g).  A row whose largest result is large does not show it.  One whose
+// results are all small and come from there (known by the two maxima) is computed again
+// with the upper tail's function below -2; other rows do not pay for that function, the
+// vector instructions being what bounds the fp32 forward pass.
+__device__ __forceinline__ bool all_small(uint32_t top_a, uint32_t top_g) {
+    return top_a < 0x3e800000u && top_g >= 0x40000000u;  // |a| < 1/4, |g| from 2 on
+}
+__device__ __forceinline__ float small_gelu(float g, float a) {
+    return g < -2.0f ? 0.5f * g * erfcf(-g * kSqrtHalf) : a;
+}
+
 // The backward pass has no such steps.  e^x and 1 / x are the hardware's
 // instructions, each good to one unit in the last place; e^x also takes the rounding
 // of x log2(e), |x| 2^-24 relative.
@@ -90,6 +102,24 @@ __global__ __launch_bounds__(block_of(TPR)) void act_kernel(
         }
     }
     row_reduce<TPR, false, kTops>(none, top, words);
+    if constexpr (K == Act::GELU) {
+        if (all_small(top[0], top[1])) {  // (all threads of the row)
+            __shared__ RowWords<TPR, 1> again;
+            uint32_t small[1] = {0};
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                if ((j * TPR + lane) * kPiece < F) {
+#pragma unroll
+                    for (int k = 0; k < kPiece; ++k) {
+                        a[j][k] = small_gelu(gv[j][k], a[j][k]);
+                        small[0] = max(small[0], magnitude(a[j][k]));
+                    }
+                }
+            }
+            row_reduce<TPR, false, 1>(none, small, again);
+            top[0] = small[0];
+        }
+    }
     RowScale r[kTops];
 #pragma unroll
     for (int i = 0; i < kTops; ++i) r[i] = row_scale(__uint_as_float(top[i]));
@@ -135,6 +165,19 @@ __global__ __launch_bounds__(1024) void act_long_kernel(
         }
     }
     row_reduce<1024, false, 3>(none, top, words);
+    const bool small = K == Act::GELU && all_small(top[0], top[1]);
+    if (small) {
+        __shared__ RowWords<1024, 1> again;
+        uint32_t most[1] = {0};
+        for (int c = (int)threadIdx.x * kPiece; c < F; c += 1024 * kPiece) {
+            load8(g + row * ldg + c, F - c, c, gv);
+#pragma unroll
+            for (int k = 0; k < kPiece; ++k)
+                most[0] = max(most[0], magnitude(small_gelu(gv[k], activation<K>(gv[k], 0.0f))));
+        }
+        row_reduce<1024, false, 1>(none, most, again);
+        top[0] = most[0];
+    }
     RowScale r[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) r[i] = row_scale(__uint_as_float(top[i]));
@@ -147,7 +190,10 @@ __global__ __launch_bounds__(1024) void act_long_kernel(
         load8(g + row * ldg + c, F - c, c, gv);
         if constexpr (kGated) load8(u + row * ldg + c, F - c, c, uv);
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) a[k] = activation<K>(gv[k], uv[k]);
+        for (int k = 0; k < kPiece; ++k) {
+            a[k] = activation<K>(gv[k], uv[k]);
+            if (small) a[k] = small_gelu(gv[k], a[k]);
+        }
         write_piece<Y>(a, r[0], q + row * ldq + c, y == nullptr ? y : y + row * ldy + c, F - c);
         if (cg != nullptr) write_piece<F32>(gv, r[1], cg + row * ldc + c, nullptr, F - c);
         if (kGated && cu != nullptr)
