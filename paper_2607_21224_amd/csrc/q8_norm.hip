@@ -391,7 +391,8 @@ __global__ __launch_bounds__(1024) void norm_dw_join_kernel(const float* parts, 
                                                             typename W::T* dw) {
     __shared__ float sums[32][33];
     const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + lane, ld = parts_ld(D);
+    const int64_t c0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 32;
+    const int64_t c = c0 + lane, ld = parts_ld(D);
     float s = 0.0f;
     if (c < D) {
         const float* p = parts + part * ld + c;
@@ -417,7 +418,7 @@ __global__ __launch_bounds__(1024) void norm_dw_join_kernel(const float* parts, 
     s = sums[lane][part];
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) s += __shfl_xor(s, off);
-    const int64_t col = (int64_t)blockIdx.x * 32 + part;
+    const int64_t col = c0 + part;
     if (lane == 0 && col < D) narrow(s, dw + col);
 }
 
@@ -488,7 +489,9 @@ int norm_bwd_typed(Mat dy, Mat h, Mat dres, const void* w, bool w_bf16, const fl
         }
     });
     if (e || done) return e;
-    const dim3 grid((uint32_t)((D + 31) / 32));
+    // (fewer than 2^32 work items in a direction of the grid)
+    const int64_t across = ((int64_t)D + 31) / 32, most = 1 << 21;
+    const dim3 grid((uint32_t)(across < most ? across : most), (uint32_t)((across + most - 1) / most));
     return dw_bf16 ? launch(norm_dw_join_kernel<BF16>, grid, 1024, stream, parts, groups, D,
                             static_cast<uint16_t*>(dw))
                    : launch(norm_dw_join_kernel<F32>, grid, 1024, stream, parts, groups, D,

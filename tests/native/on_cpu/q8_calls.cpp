@@ -32,7 +32,7 @@ class Memory {
         }
     }
     char* take(size_t bytes) {
-        if (!running) return reinterpret_cast<char*>(next_ += (uintptr_t)1 << 40);
+        if (!running) return reinterpret_cast<char*>(next_ += (uintptr_t)1 << 44);
         // (AddressSanitizer keeps 16 bytes or more around it)
         void* p = nullptr;
         if (posix_memalign(&p, 16, bytes == 0 ? 1 : bytes) != 0) abort();
