@@ -26,7 +26,8 @@
  * contiguous; w and dw start on a 16-byte boundary, scales and rstd on a 4-byte
  * one.  Storage types are CPDP_F32 or CPDP_BF16 of cpdp.h; arithmetic is fp32
  * (sums of 8-bit products: 32-bit integers), each value rounded to nearest-even
- * once, when it is written.
+ * once, when it is written; but the gradients of a product may round what they sum,
+ * as it says there.
  *
  * All pointers are device pointers owned by the caller; the library never
  * allocates, frees or keeps them.  Every argument is checked on the host before
@@ -149,11 +150,16 @@ int cpdp_q8_act_bwd(int kind, const void* da, int64_t ldda, int act_dt, const in
  *   cpdp_q8_grad_input   dx[t, k] = sum_n dy[t, n] * b_scale[n] * b[n, k]
  *   cpdp_q8_grad_weight  dw[n, k] = sum_t dy[t, n] * a_scale[t] * a[t, k]
  * dx [T x K], dw [N x K] in out_dt.  Products run on the bfloat16 matrix cores
- * with fp32 sums.  With a bf16 result and a sum of more than 64 values the scaled
- * 8-bit operand (bf16 dy) or the scaled gradient (fp32 dy) is rounded to one
- * bfloat16 number a value; else the scaled gradient is taken as two (bf16 dy,
- * exact for scales of 8 significant bits) or three (fp32 dy), so that nothing
- * short of fp32's precision is lost.
+ * with fp32 sums; what they sum is held in bfloat16 numbers:
+ *   fp32 result, or a sum of at most 64 values
+ *     fp32 dy   three for each scaled value of dy: all of its 24 bits
+ *     bf16 dy   two: all of its bits where the scale has 8 significant ones, as those
+ *               that this library writes; with other scales within 2^-16 of it
+ *   bf16 result of a sum of more than 64 values
+ *     one, for each scaled value of dy (fp32 dy) or of the 8-bit operand (bf16 dy):
+ *     within 2^-8 of it, as one rounding of the result is.  These errors are
+ *     independent and average out over a sum, but not against one that cancels: whoever
+ *     needs that takes an fp32 result.
  */
 int64_t cpdp_q8_grad_input_workspace(int64_t T, int64_t N, int64_t K, int dy_dt, int out_dt);
 int cpdp_q8_grad_input(const void* dy, int64_t lddy, int dy_dt, const int8_t* b, int64_t ldb,

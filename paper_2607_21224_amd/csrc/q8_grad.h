@@ -5,7 +5,9 @@
 // of what the ones before it left, and the product runs over them as over a
 // longer sum.  It is the gradient that is scaled and taken apart, q being exact in
 // one part: an infinity in it is one part's and meets each q once.
-//   bf16 dy   dy * s has 16 significant bits: two parts, exactly
+//   bf16 dy   dy * s has 16 significant bits where s has 8, as every scale has that is
+//             written here: two parts, exactly (other scales: within 2^-16; a third part
+//             would be half as much work again for every caller)
 //   fp32 dy   dy * s has 24: three parts
 // With bf16 results one part is kept where the sum is long: its relative error, up
 // to 2^-8 a value and independent from value to value, averages out to that of
