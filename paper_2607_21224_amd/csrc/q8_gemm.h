@@ -671,11 +671,12 @@ int launch_kernel(const Operands& o, const Target& t, int slices, void* stream) 
 template <class Op, int BM, int BN, int WM, int WN>
 int launch_tiles(const Operands& o, const Target& t, int slices, void* stream) {
     const int64_t blocks = up(o.M, BM) * up(o.N, BN) * slices;
-    if constexpr (BM < 256) {
+    if constexpr (BM < 256)
         if (blocks <= kCus) return launch_kernel<Op, BM, BN, WM, WN, 4, 2>(o, t, slices, stream);
+    // (four buffers of larger tiles leave a CU room for one block)
+    if constexpr (BM == 64)
         if (all_at_once(blocks, Gemm<Op, BM, BN, WM, WN, 4>::kBuffer * 4))
             return launch_kernel<Op, BM, BN, WM, WN, 4, 1>(o, t, slices, stream);
-    }
     constexpr int S = BM + BN == 384 ? 3 : 2;
     return launch_kernel<Op, BM, BN, WM, WN, S, 1>(o, t, slices, stream);
 }

@@ -418,7 +418,7 @@ int launch_grad_tiles(const GradOperands& o, const Target& t, int slices, void* 
         if (blocks <= kCus)
             return launch_grad_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P,
                                       kDeep <= 160 * 1024 ? 4 : 2, 2>(o, t, slices, stream);
-    if constexpr (BM < 256 && kDeep <= 160 * 1024)
+    if constexpr ((BM == 64 || (BM == 128 && BDOWN)) && kDeep <= 160 * 1024)
         if (all_at_once(blocks, kDeep))
             return launch_grad_kernel<BM, BN, WM, WN, ADOWN, BDOWN, P, 4, 1>(o, t, slices, stream);
     constexpr int S = BM + BN == 384 ? 3 : 2;

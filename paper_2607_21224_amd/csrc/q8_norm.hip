@@ -474,13 +474,16 @@ int norm_bwd_typed(Mat dy, Mat h, Mat dres, const void* w, bool w_bf16, const fl
                                (uint32_t)groups),
                           256, stream, dyp, dy.ld, hp, h.ld, rstd, T, D, parts);
         } else {
-            if (bwd_one(T, D, sizeof(ET))) {
-                done = true;
-                const int dw_blocks = (D + kPiece - 1) / kPiece;
-                const int64_t rows = (T + rows_of(tpr) - 1) / rows_of(tpr);
-                return launch(norm_bwd_one_kernel<E, tpr, ch>, dim3((uint32_t)(dw_blocks + rows)),
-                              block_of(tpr), stream, dyp, dy.ld, hp, h.ld, rp, dres.ld, w, w_bf16,
-                              rstd, (int)T, D, dxp, dx.ld, dw, dw_bf16, dw_blocks);
+            if constexpr (tpr <= 256) {  // (rows of up to 4096)
+                if (bwd_one(T, D, sizeof(ET))) {
+                    done = true;
+                    const int dw_blocks = (D + kPiece - 1) / kPiece;
+                    const int64_t rows = (T + rows_of(tpr) - 1) / rows_of(tpr);
+                    return launch(norm_bwd_one_kernel<E, tpr, ch>,
+                                  dim3((uint32_t)(dw_blocks + rows)), block_of(tpr), stream, dyp,
+                                  dy.ld, hp, h.ld, rp, dres.ld, w, w_bf16, rstd, (int)T, D, dxp,
+                                  dx.ld, dw, dw_bf16, dw_blocks);
+                }
             }
             groups = (int)bwd_blocks(T, rows_of(tpr));
             return launch(norm_bwd_kernel<E, tpr, ch>, dim3((uint32_t)groups), block_of(tpr),
@@ -491,7 +494,8 @@ int norm_bwd_typed(Mat dy, Mat h, Mat dres, const void* w, bool w_bf16, const fl
     if (e || done) return e;
     // (fewer than 2^32 work items in a direction of the grid)
     const int64_t across = ((int64_t)D + 31) / 32, most = 1 << 21;
-    const dim3 grid((uint32_t)(across < most ? across : most), (uint32_t)((across + most - 1) / most));
+    const dim3 grid((uint32_t)(across < most ? across : most),
+                    (uint32_t)((across + most - 1) / most));
     return dw_bf16 ? launch(norm_dw_join_kernel<BF16>, grid, 1024, stream, parts, groups, D,
                             static_cast<uint16_t*>(dw))
                    : launch(norm_dw_join_kernel<F32>, grid, 1024, stream, parts, groups, D,
