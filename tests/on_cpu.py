@@ -8,8 +8,7 @@ from paper_2607_21224_amd import build
 
 NATIVE = os.path.join(build.ROOT, "tests", "native")
 CLANG = os.path.join(os.path.dirname(os.path.dirname(build.HIPCC)), "llvm", "bin", "clang++")
-# (without optimisation: a load whose result nothing uses is made all the same)
-FLAGS = ["-std=c++17", "-O0", "-g1", "-fno-pie", "-fno-omit-frame-pointer",
+FLAGS = ["-std=c++17", "-g1", "-fno-pie", "-fno-omit-frame-pointer",
          "-fsanitize=address,alignment", "-fno-sanitize-recover=all"]
 
 
@@ -17,8 +16,9 @@ def available():
     return shutil.which(CLANG) is not None
 
 
-def compile_calls(folder):
-    """The program, built in `folder`."""
+def compile_calls(folder, optimise="-O0"):
+    """The program, built in `folder`; as it is, a load whose result nothing uses is made all
+    the same, optimised, calls of some size run in a second."""
     csrc = os.path.join(build.PKG, "csrc")
     sources = [os.path.join(csrc, s) for s in build.Q8_SOURCES]
     sources.append(os.path.join(NATIVE, "on_cpu", "q8_calls.cpp"))
@@ -27,7 +27,7 @@ def compile_calls(folder):
     jobs, objects = [], []
     for s in sources:
         objects.append(os.path.join(folder, os.path.basename(s) + ".o"))
-        jobs.append(subprocess.Popen([CLANG, *FLAGS, *include, "-x", "c++", "-c", s, "-o",
+        jobs.append(subprocess.Popen([CLANG, *FLAGS, optimise, *include, "-x", "c++", "-c", s, "-o",
                                       objects[-1]], stdout=subprocess.PIPE,
                                      stderr=subprocess.STDOUT, text=True))
     for j in jobs:

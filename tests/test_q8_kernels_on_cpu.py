@@ -1,7 +1,9 @@
 """Which kernels of the 8-bit path the calls of q8_sizes.py take: each that is compiled into
-it runs, so that the GPU tests compare it and none is kept that no call reaches."""
+it runs, so that the GPU tests compare it and none is kept that no call reaches; and that
+all they read and write in these calls is in range."""
 import re
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 import pytest
 
@@ -44,3 +46,14 @@ def launched(tmp_path_factory):
 def test_every_kernel_is_reached(launched):
     left = sorted(n for n, calls in launched.items() if not calls)
     assert not left, "\n".join(left)
+
+
+def test_all_that_they_touch_is_in_range(tmp_path):
+    """(test_q8_reads_on_cpu.py goes through more sizes, smaller ones)"""
+    exe = on_cpu.compile_calls(str(tmp_path), "-O1")
+    calls = [" ".join(map(str, c)) for c in q8_sizes.calls()]
+    with ThreadPoolExecutor(8) as pool:
+        parts = [calls[i::32] for i in range(32)]
+        for part, answers in zip(parts, pool.map(lambda p: on_cpu.run(exe, "run", p), parts)):
+            for call, (status, kernels) in zip(part, answers):
+                assert status == 0 and "large" not in kernels, call
