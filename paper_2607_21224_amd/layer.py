@@ -3,9 +3,11 @@ CPDP steps.
 
 ``Q8Mlp`` holds no weights: they are slices of a replica's row of
 ``CpdpState.params``, and its gradients go into the same slices of a row of
-gradients, so one model of any number of such layers is one row.  A layer's
-forward pass keeps one byte an activation for its backward pass (``Saved``), a
-quarter of fp32 and half of bf16, for each of the replicas on the GPU::
+gradients, so one model of any number of such layers is one row.  What a layer's
+forward pass keeps for its backward pass (``Saved``) is one byte an activation, a
+quarter of fp32 and half of bf16, but for the sum that the norm is taken of; what
+passes need for a while (``Scratch``), layers whose passes run one after the
+other share::
 
     mlp = Q8Mlp(dim=384, hidden=1536)
     st = CpdpState(W=8, P=mlp.numel, K=4)
@@ -18,6 +20,11 @@ quarter of fp32 and half of bf16, for each of the replicas on the GPU::
             dy = ...                                   # the loss' gradient of saved.y
             mlp.backward(st.params[i], dy, saved, grads[i])
         st.step(t, grads, hyper, T)
+
+For dim 384, hidden 1536, GELU and bf16, bytes a token: n, z and a in 8 bits 3456, their
+scales and rstd 16, h 768, and the results y and dx 768 each, once a layer; z, da and dn
+6912, once for all that share them.  (h, n, z and a in bf16 are 7680.)  Replicas that run
+one after the other, as here, need one ``Saved`` a layer, not one each.
 
 Forward, with `8(.)` for rounding to 8-bit rows (cpdp_q8.h):
     h = x + residual;  n = 8(norm(h) * w);  z = n 8(W1)^T;  a = 8(act(z))
@@ -37,17 +44,36 @@ from .state import round_up
 _DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
-class Saved:
-    """What a forward pass over `T` tokens leaves for its backward pass, and the
-    tensors both write; it serves one replica after another."""
+class Scratch:
+    """What passes over `T` tokens need for a while: the inner product's result and its
+    gradient (z), the gradients of the activation (da) and of the norm (dn), and the
+    operators' workspace.  Nothing of it outlives a pass, so layers of one shape may share
+    one where no two of their passes run at the same time (one stream)."""
 
     def __init__(self, mlp: "Q8Mlp", T: int, device="cuda"):
+        self.T, self.shape = T, mlp.shape
+        self.z_all = q8.empty_rows(T, mlp.inner, mlp.act_dtype, device)
+        self.da = q8.empty_rows(T, mlp.hidden, mlp.act_dtype, device)
+        self.dn = q8.empty_rows(T, mlp.dim, mlp.act_dtype, device)
+        self.workspace = torch.empty(mlp.workspace_bytes(T), dtype=torch.uint8, device=device)
+
+
+class Saved:
+    """What a forward pass over `T` tokens leaves for its backward pass, and the results of
+    both; it serves one replica after another.  `scratch`: a Scratch to share."""
+
+    def __init__(self, mlp: "Q8Mlp", T: int, device="cuda", scratch: Scratch | None = None):
         def rows(r, c, dt=mlp.act_dtype):
             return q8.empty_rows(r, c, dt, device)
 
         def vec(n):
             return torch.empty(n, device=device)
 
+        if scratch is None:
+            scratch = Scratch(mlp, T, device)
+        elif (scratch.T, scratch.shape) != (T, mlp.shape):
+            raise ValueError(f"scratch: made for {scratch.T} tokens of a layer {scratch.shape}, "
+                             f"this one is for {T} of {mlp.shape}")
         D, F, i8 = mlp.dim, mlp.hidden, torch.int8
         halves = range(0, mlp.inner, F)
         self.T = T
@@ -60,12 +86,11 @@ class Saved:
         q, scale = self.w_in = rows(mlp.inner, D, i8), vec(mlp.inner)
         self.w1 = [(q[i:i + F], scale[i:i + F]) for i in halves]
         self.w2 = rows(D, F, i8), vec(D)
-        # the sum that the norm is taken of, the result, and what lives for a while
+        # the sum that the norm is taken of, and the results
         self.h, self.y, self.dx = rows(T, D), rows(T, D), rows(T, D)
-        self.z_all = rows(T, mlp.inner)
+        self.z_all, self.da, self.dn = scratch.z_all, scratch.da, scratch.dn
         self.z = [self.z_all[:, i:i + F] for i in halves]
-        self.da, self.dn = rows(T, F), rows(T, D)
-        self.workspace = torch.empty(mlp.workspace_bytes(T), dtype=torch.uint8, device=device)
+        self.workspace = scratch.workspace
 
 
 class Q8Mlp:
@@ -84,6 +109,7 @@ class Q8Mlp:
         self.dim, self.hidden, self.kind, self.eps = int(dim), int(hidden), kind, float(eps)
         self.gated = kind == "swiglu"
         self.inner = self.hidden * (2 if self.gated else 1)  # channels of z
+        self.shape = (self.dim, self.hidden, kind, act_dt)
         self.act_dtype = _DT[act_dt]
         shapes = [("norm", (dim,)), ("w1", (hidden, dim))]
         if self.gated:
@@ -117,8 +143,11 @@ class Q8Mlp:
                 self.view(row, name).normal_(0.0, shape[1] ** -0.5, generator=generator)
         return row
 
-    def saved(self, T: int, device="cuda") -> Saved:
-        return Saved(self, int(T), device)
+    def saved(self, T: int, device="cuda", scratch: Scratch | None = None) -> Saved:
+        return Saved(self, int(T), device, scratch)
+
+    def scratch(self, T: int, device="cuda") -> Scratch:
+        return Scratch(self, int(T), device)
 
     def workspace_bytes(self, T: int) -> int:
         """The largest workspace of the layer's calls over T tokens."""
@@ -132,7 +161,8 @@ class Q8Mlp:
 
     def forward(self, params, x, saved: Saved, residual=None, stream=None) -> torch.Tensor:
         """saved.y <- the layer's output for x (T, dim); params is a replica's row.
-        With a residual saved.h is x + residual, the residual of what follows."""
+        With a residual saved.h is x + residual, the residual of what follows; without one
+        the backward pass reads x again, which has to stay as it is until then."""
         s = saved
         if residual is None:
             q8.cpdp_q8_norm(x, self.view(params, "norm"), self.eps, q=s.n, scale=s.n_scale,
