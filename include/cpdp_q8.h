@@ -34,17 +34,20 @@
  * any GPU work: a count below 0 or an inner size out of range is
  * CPDP_ERR_INVALID_ARG, a missing pointer CPDP_ERR_NULL, an unknown storage
  * type CPDP_ERR_DTYPE; the ranges of different arguments must not overlap
- * (CPDP_ERR_OVERLAP) but where it says so.  Calls return once their kernels are
- * enqueued on `stream` (a hipStream_t, NULL for the null stream); they copy,
- * clear and allocate nothing through the runtime, so they may be captured in a
- * graph.  Zero rows are a valid no-op (a gradient summed over zero rows is 0).
- * Results are bitwise reproducible: sums run in an order that is fixed by the
- * sizes.
+ * (CPDP_ERR_OVERLAP) but where it says so.  Row strides are at most 2^28 elements;
+ * those of the matrices that a product or its gradients read at most 2^23 - 16 (dy:
+ * 2^22 - 8), and a gradient sums over at most 2^22 - 72 values (CPDP_ERR_TOO_LARGE).
+ * Calls return once their kernels are enqueued on `stream` (a hipStream_t, NULL for
+ * the null stream); they copy, clear and allocate nothing through the runtime, so
+ * they may be captured in a graph.  Zero rows are a valid no-op (a gradient summed
+ * over zero rows is 0).  Results are bitwise reproducible: sums run in an order that
+ * is fixed by the sizes.
  *
  * Workspaces.  Calls with a `workspace` need the bytes that the matching
  * *_workspace function returns for the same sizes (0: it may be NULL), on a
- * 16-byte boundary; less is CPDP_ERR_INVALID_ARG.  The content is not kept from
- * one call to the next; two calls that may run at the same time need two.
+ * 16-byte boundary; less is CPDP_ERR_INVALID_ARG (also from calls of these sizes
+ * whose storage types let a kernel do without).  The content is not kept from one
+ * call to the next; two calls that may run at the same time need two.
  */
 #ifndef CPDP_Q8_H
 #define CPDP_Q8_H
@@ -81,7 +84,8 @@ int cpdp_q8_values(const int8_t* q, int64_t ldq, const float* scale, int64_t T, 
  *   q, scale <- v as an 8-bit row;  y <- s * q (y_dt), if y is not NULL
  * x, residual, h in act_dt; w [D] in w_dt; rstd [T] fp32 or NULL.  residual and
  * h are both given or both NULL; h may be the same rows as x or as residual.
- * eps >= 0.
+ * eps >= 0.  The sum of squares is fp32, as the other arithmetic: one that passes
+ * fp32's largest number (|h| about 2^64) makes rstd and the row 0.
  */
 int cpdp_q8_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, int act_dt,
                  const void* w, int w_dt, float eps, int64_t T, int64_t D, void* h, int64_t ldh,

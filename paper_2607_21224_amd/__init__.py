@@ -7,8 +7,9 @@ Submodules
   state  HBM-resident replica state (flat layout), the host cadence driving
          it, step tables and HIP-graph capture, checkpoint/resume
   multi  the same for a model held as separate tensors (multi-tensor plans)
-  q8     ctypes binding of include/cpdp_q8.h (libcpdp_q8.so): norm, products and
-         activations on rows of 8-bit numbers, and their backward passes
+  q8     binding of include/cpdp_q8.h (libcpdp_q8.so, through the extension module
+         _q8): norm, products and activations on rows of 8-bit numbers, and their
+         backward passes
   layer  the MLP half of a transformer block on that path, with its weights and
          gradients in replica rows
   build  hipcc build of the shared libraries

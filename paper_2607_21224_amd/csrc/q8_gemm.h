@@ -609,13 +609,15 @@ inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // block takes `alone` ns while its CU has no other (and `first` before the first and
 // after the last), and the CU gets through one such step in `each` ns when it has
 // several (0: not taken then; a tile of 128 x 64 is for up to twice as many tiles of
-// 64 x 64 as there are CUs: 512 x 4096 x 4096 14.5 -> 12.8 us).  Measured on int8
-// products with N = K = 4096, in us, and the best taken:
-//   rows     256 x 256   256 x 128   128 x 128   64 x 64
-//   256          43          28          18         10
-//   1024         45          29          23         30
-//   2048         48          35          40         55
-//   4096         57          69          76        104
+// 64 x 64 as there are CUs).  Measured on int8 products with N = K = 4096 and bf16
+// results, calls that follow each other on one card, in us:
+//   rows     256 x 256   256 x 128   128 x 128   128 x 64   64 x 64
+//   256          43          28          19         13         11
+//   512          44          29          20         14         16
+//   1024         45          29          21         26         29
+//   2048         46          34          38         49         53
+//   4096         55          64          72         98        101
+// and the rule takes the best of every row.
 // Slices are added up by a second launch: its start, and each sum written and read
 // again at 3 TB/s.
 constexpr int64_t kCus = 256;

@@ -146,7 +146,8 @@ int norm_typed(Mat x, Mat res, const void* w, bool w_bf16, float eps, int64_t T,
 // meet in LDS); the G parts go to the workspace and are added in their order by a
 // second launch, so the result does not depend on which block ran first (few and short
 // rows: norm_bwd_one_kernel).  Joining the wavefronts' own parts, four times as many,
-// made 1576 x 384 fp32 9.4 us and 16384 x 512 bf16 22, now 7.7 and 16.
+// made 1576 x 384 fp32 9.4 us and 16384 x 512 bf16 22, now 7.1 and 15.5 (calls that
+// follow each other, as in the figures below).
 
 // Floats from part to part: whole 16-byte pieces.
 __host__ __device__ constexpr int64_t parts_ld(int64_t D) { return (D + 3) / 4 * 4; }
@@ -444,8 +445,9 @@ int64_t bwd_blocks(int64_t T, int rows) {
 // Whether one launch takes both: as long as a thread has two turns of four rows, a
 // block's 256 threads suffice for a row, and dy is so small that reading it and h again
 // is nothing.  In us, two launches and one: 256 x 384 fp32 7.3 and 5.0, 1576 x 384 bf16
-// 7.4 and 5.5, 64 x 7264 7.6 and 6.2; but 1576 x 384 fp32 (2.4 MB) 7.3 and 9.7, 3000 x 96
-// 7.3 and 8.5, 5 x 8191 7.7 and 8.7.
+// 7.4 and 5.5; but 1576 x 384 fp32 (2.4 MB) 7.3 and 9.7, 3000 x 96 7.3 and 8.5.  Rows
+// past 4096 columns, for which a block has 512 threads and dw's blocks most of them idle,
+// go either way (64 x 7264 bf16 7.6 and 6.2, 5 x 8191 fp32 7.7 and 8.7) and take two.
 bool bwd_one(int64_t T, int64_t D, int64_t element) {
     return T <= 2048 && D <= 4096 && T * D * element <= 3 << 19;
 }
