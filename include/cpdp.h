@@ -451,6 +451,46 @@ int cpdp_count_unsynced(const void* params, const float* anchor, int W,
                         int64_t P, int64_t ld, int param_dt, uint64_t* count,
                         void* stream);
 
+/* ------------------------------------------------------------------------
+ * Gradient norm and clipping, between the backward pass and a step.  For every
+ * replica i,
+ *   norm_i = sqrt(sum over p < P of grad_i[p]^2)
+ *   grad_i <- c_i * grad_i,  c_i = min(1, max_norm / (norm_i + 1e-6))
+ * or, with CPDP_NORM_MEAN, for the gradient that a synchronisation step uses (or a
+ * DDP step), one norm for all replicas:
+ *   norm   = sqrt(sum over p < P of gbar[p]^2),  gbar = (1/W) * sum_i grad_i
+ *   grad_i <- c * grad_i for every i             (so that gbar is c times gbar)
+ * Squares and their sum are fp64 (gbar fp32, in the order i = 0..W-1), norm and c
+ * fp32; a scaled bf16 gradient is rounded to nearest-even.  Replicas with c = 1 are
+ * left as they are.  A norm that is infinite or NaN follows the formula: c is 0 or
+ * NaN.  Results are bitwise reproducible.
+ *   grads [W x ld] in grad_dt: read only by cpdp_grad_norm, updated in place by
+ *     cpdp_clip_grads; the plan calls take the plan's gradient tensors
+ *   norm [W] fp32, or with CPDP_NORM_MEAN [1]: written (before clipping; the norm
+ *     of no coordinates is 0), on a 4-byte boundary
+ *   workspace: the bytes that the matching *_workspace function returns for the same
+ *     W and P or plan (0 from it: an invalid argument), on a 16-byte boundary; its
+ *     content is not kept, and two calls that may run at the same time need two
+ * 1 <= W <= 2^23; max_norm > 0 and finite.  Nothing is copied or cleared by the
+ * runtime: the calls may be captured in a graph.
+ * ------------------------------------------------------------------------ */
+enum { CPDP_NORM_MEAN = 1 };
+
+int64_t cpdp_grad_norm_workspace(int W, int64_t P);
+int cpdp_grad_norm(const void* grads, int W, int64_t P, int64_t ld, int grad_dt,
+                   unsigned flags, float* norm, void* workspace,
+                   int64_t workspace_bytes, void* stream);
+int cpdp_clip_grads(void* grads, int W, int64_t P, int64_t ld, int grad_dt,
+                    float max_norm, unsigned flags, float* norm, void* workspace,
+                    int64_t workspace_bytes, void* stream);
+
+int64_t cpdp_grad_norm_plan_workspace(const cpdp_plan* plan);
+int cpdp_grad_norm_plan(const cpdp_plan* plan, unsigned flags, float* norm,
+                        void* workspace, int64_t workspace_bytes, void* stream);
+int cpdp_clip_grads_plan(const cpdp_plan* plan, float max_norm, unsigned flags,
+                         float* norm, void* workspace, int64_t workspace_bytes,
+                         void* stream);
+
 /*
  * Synchronisation indicator (Sec. 3.2) with the forced synchronisation at the
  * end of an epoch (Sec. 3.1, Sec. 4.2).  Host only, no GPU work.

@@ -39,6 +39,8 @@ KERNEL_HEADERS = ("cpdp_device.h", "cpdp_sync_impl.h", "cpdp_split.h", "cpdp_dis
 HOST_SOURCES = ("cpdp_api.cpp",)
 # the library's own device memory (no kernels): the static plan table
 SCRATCH_SOURCES = ("plan_scratch.hip",)
+# gradient norms and clipping (part of libcpdp.so; no kernel of a step)
+CLIP_SOURCES = ("kernels_clip.hip", "clip_api.cpp")
 # libcpdp_q8.so: kernel translation units and the host validation layer
 Q8_SOURCES = ("q8_rows.hip", "q8_norm.hip", "q8_act.hip", "q8_matmul.hip", "q8_grad.hip",
               "q8_grad_few.hip", "q8_api.cpp")
@@ -52,7 +54,7 @@ def _run(cmd):
 
 
 def build_cpdp(out: str = LIB_CPDP, extra=(),
-               sources=KERNEL_SOURCES + HOST_SOURCES + SCRATCH_SOURCES) -> str:
+               sources=KERNEL_SOURCES + HOST_SOURCES + SCRATCH_SOURCES + CLIP_SOURCES) -> str:
     from concurrent.futures import ThreadPoolExecutor
     csrc = os.path.join(PKG, "csrc")
     objdir = os.path.join(OBJ_ROOT, os.path.basename(out) + ".objs")

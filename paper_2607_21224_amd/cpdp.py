@@ -45,6 +45,8 @@ EXPORTS = ("cpdp_state_init", "cpdp_local_step", "cpdp_reconcile",
            "cpdp_sync_step_table", "cpdp_local_steps_table", "cpdp_sync_step_table_ahead",
            "cpdp_step_table_advance_by", "cpdp_local_step_plan_table",
            "cpdp_sync_step_plan_table",
+           "cpdp_grad_norm_workspace", "cpdp_grad_norm", "cpdp_clip_grads",
+           "cpdp_grad_norm_plan_workspace", "cpdp_grad_norm_plan", "cpdp_clip_grads_plan",
            "cpdp_count_unsynced", "cpdp_status_str")
 
 CPDP_OPT_SGD = 0
@@ -56,6 +58,7 @@ SYNC_KINDS = {"cpdp": CPDP_SYNC_CPDP, "localsgd": CPDP_SYNC_LOCALSGD,
               "ddp": CPDP_SYNC_DDP}
 CPDP_SYNC_WRITE_GRAD_MEAN = 1
 CPDP_SYNC_AVERAGE_OPT_STATE = 2
+CPDP_NORM_MEAN = 1
 
 
 class cpdp_plan(ctypes.Structure):
@@ -151,6 +154,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cpdp_local_step_plan_table.restype = i
     lib.cpdp_sync_step_plan_table.argtypes = [i, pp, i, tp, ctypes.c_uint, vp]
     lib.cpdp_sync_step_plan_table.restype = i
+    lib.cpdp_grad_norm_workspace.argtypes = [i, i64]
+    lib.cpdp_grad_norm_plan_workspace.argtypes = [pp]
+    u = ctypes.c_uint
+    lib.cpdp_grad_norm.argtypes = [vp, i, i64, i64, i, u, vp, vp, i64, vp]
+    lib.cpdp_clip_grads.argtypes = [vp, i, i64, i64, i, f, u, vp, vp, i64, vp]
+    lib.cpdp_grad_norm_plan.argtypes = [pp, u, vp, vp, i64, vp]
+    lib.cpdp_clip_grads_plan.argtypes = [pp, f, u, vp, vp, i64, vp]
+    for name in ("cpdp_grad_norm", "cpdp_clip_grads", "cpdp_grad_norm_plan",
+                 "cpdp_clip_grads_plan"):
+        getattr(lib, name).restype = i
+        getattr(lib, name.replace("clip_grads", "grad_norm") + "_workspace").restype = i64
     lib.cpdp_count_unsynced.argtypes = [vp, vp, i, i64, i64, i, vp, vp]
     lib.cpdp_count_unsynced.restype = i
     lib.cpdp_is_sync_step.argtypes = [i64, i, i64]
@@ -610,6 +624,61 @@ def cpdp_count_unsynced(params, anchor, W, P, ld, count, param_dt=CPDP_F32, stre
                                 _vec(anchor, P, "anchor"), int(W), int(P), int(ld),
                                 _dt(param_dt), _addr(count), _stream(stream))
     return _done(s, "cpdp_count_unsynced", check)
+
+
+def cpdp_grad_norm_workspace(W, P) -> int:
+    return int(lib.cpdp_grad_norm_workspace(int(W), int(P)))
+
+
+def cpdp_grad_norm_plan_workspace(plan: cpdp_plan) -> int:
+    return int(lib.cpdp_grad_norm_plan_workspace(ctypes.byref(plan)))
+
+
+def _workspace(x) -> tuple:
+    """Address and bytes of a workspace argument, a contiguous device tensor of any
+    type."""
+    if x is None:
+        return None, 0
+    return _addr(x), x.nbytes
+
+
+def _norms(norm, W, flags):
+    return _vec(norm, 1 if int(flags) & CPDP_NORM_MEAN else W, "norm")
+
+
+def cpdp_grad_norm(grads, W, P, ld, norm, workspace, grad_dt=CPDP_F32, flags=0, stream=None,
+                   check=True):
+    """norm <- the norm of every replica's gradient, or with CPDP_NORM_MEAN of their
+    mean.  workspace: a tensor of cpdp_grad_norm_workspace(W, P) bytes."""
+    s = lib.cpdp_grad_norm(_rows(grads, W, P, ld, grad_dt, "grads"), int(W), int(P), int(ld),
+                           _dt(grad_dt), int(flags), _norms(norm, W, flags),
+                           *_workspace(workspace), _stream(stream))
+    return _done(s, "cpdp_grad_norm", check)
+
+
+def cpdp_clip_grads(grads, W, P, ld, max_norm, norm, workspace, grad_dt=CPDP_F32, flags=0,
+                    stream=None, check=True):
+    """cpdp_grad_norm, and grads scaled in place to at most max_norm."""
+    s = lib.cpdp_clip_grads(_rows(grads, W, P, ld, grad_dt, "grads"), int(W), int(P), int(ld),
+                            _dt(grad_dt), float(max_norm), int(flags), _norms(norm, W, flags),
+                            *_workspace(workspace), _stream(stream))
+    return _done(s, "cpdp_clip_grads", check)
+
+
+def cpdp_grad_norm_plan(plan: cpdp_plan, norm, workspace, flags=0, stream=None, check=True):
+    """cpdp_grad_norm over the gradient tensors of a plan."""
+    s = lib.cpdp_grad_norm_plan(ctypes.byref(plan), int(flags), _norms(norm, plan.W, flags),
+                                *_workspace(workspace), _stream(stream))
+    return _done(s, "cpdp_grad_norm_plan", check)
+
+
+def cpdp_clip_grads_plan(plan: cpdp_plan, max_norm, norm, workspace, flags=0, stream=None,
+                         check=True):
+    """cpdp_clip_grads over the gradient tensors of a plan."""
+    s = lib.cpdp_clip_grads_plan(ctypes.byref(plan), float(max_norm), int(flags),
+                                 _norms(norm, plan.W, flags), *_workspace(workspace),
+                                 _stream(stream))
+    return _done(s, "cpdp_clip_grads_plan", check)
 
 
 def cpdp_local_step_plan_table(plan: cpdp_plan, K, t: cpdp_step_table, stream=None, check=True):

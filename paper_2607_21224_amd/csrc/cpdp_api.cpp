@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "cpdp_launch.h"
+#include "plan_check.h"
 #include "plan_scratch.h"
 
 namespace {
@@ -893,3 +894,8 @@ const char* cpdp_status_str(int status) {
 }
 
 }  // extern "C"
+
+int cpdp::check_plan_handle(const cpdp_plan* plan) {
+    if (int s = check_plan(plan)) return s;
+    return check_seal(plan);
+}

@@ -1,0 +1,329 @@
+// The global norm of a replica's gradient, and clipping by it.
+//   norm_i = sqrt(sum over p of g_i[p]^2), or of the replicas' mean gradient;
+//   c_i = min(1, max_norm / (norm_i + 1e-6));  g_i <- c_i g_i
+//
+// Both are bound by HBM.  A first launch gives each block a run of chunks of one
+// replica (of all replicas for the mean) and leaves one sum for each; a second one
+// adds a replica's sums up, every block of it by itself and in the same order, and
+// scales.  Squares and sums are fp64: they cannot overflow or lose small values, and
+// cost nothing beside the memory (2 instructions a coordinate of 4 bytes).  There
+// are no atomics; the order of a sum is fixed by the sizes.
+#include "cpdp_device.h"
+
+#include "clip_launch.h"
+
+namespace cpdp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int64_t kCoords = (int64_t)kBlock * kVec;  // of a chunk
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+// 16 bytes of gradients as they lie in memory
+struct F32Piece {
+    using T = float;
+    static constexpr int N = 4;
+    u32x4 v;
+    __device__ __forceinline__ float get(int k) const { return __uint_as_float(v[k]); }
+    __device__ __forceinline__ void set(const float (&x)[N]) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = __float_as_uint(x[k]);
+    }
+    static __device__ __forceinline__ float one(T x) { return x; }
+    static __device__ __forceinline__ T narrow(float x) { return x; }
+};
+struct BF16Piece {
+    using T = uint16_t;
+    static constexpr int N = 8;
+    u32x4 v;
+    __device__ __forceinline__ float get(int k) const {
+        return __uint_as_float(k % 2 == 0 ? v[k / 2] << 16 : v[k / 2] & 0xFFFF0000u);
+    }
+    __device__ __forceinline__ void set(const float (&x)[N]) {
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k)
+            v[k] = bf16_bits(x[2 * k]) | (bf16_bits(x[2 * k + 1]) << 16);
+    }
+    static __device__ __forceinline__ float one(T x) { return bf16_value(x); }
+    static __device__ __forceinline__ T narrow(float x) { return (T)bf16_bits(x); }
+};
+
+// Where replica i's coordinates lie.  runs(c0, c1, f) calls f(t, e, count) for each run
+// of `count` coordinates, from e on, of a tensor t that chunks c0 to c1 cover.
+template <class G>
+struct FlatRows {
+    typename G::T* base;
+    int64_t ld, P;
+    __device__ __forceinline__ typename G::T* row(int64_t i, int64_t) const {
+        return base + i * ld;
+    }
+    template <class F>
+    __device__ __forceinline__ void runs(int64_t c0, int64_t c1, F f) const {
+        const int64_t e = c0 * kCoords;
+        f((int64_t)0, e, min(c1 * kCoords, P) - e);
+    }
+};
+struct PlanRows {
+    const int64_t* plan;
+    int W, n;
+    __device__ __forceinline__ float* row(int64_t i, int64_t t) const {
+        return global_ptr<float>(plan_view(plan, W, n).grads[i * n + t]);
+    }
+    template <class F>
+    __device__ __forceinline__ void runs(int64_t c0, int64_t c1, F f) const {
+        const PlanView v = plan_view(plan, W, n);
+        int64_t t = plan_tensor_scalar(v, n, c0);
+        for (int64_t c = c0; c < c1; ++t) {
+            const int64_t start = v.chunk_start[t], end = min(v.chunk_start[t + 1], c1);
+            if (end <= c) continue;  // an empty tensor
+            const int64_t e = (c - start) * kCoords;
+            f(t, e, min((end - start) * kCoords, v.numel[t]) - e);
+            c = end;
+        }
+    }
+};
+
+// body(at, first) for the thread's pieces of `count` coordinates, U of them at a
+// time: a piece is read at `at`, and its coordinates from `first` on are the
+// thread's.  (A piece that the end cuts short is read as the last N coordinates,
+// wherever they start.)  count >= N.
+template <int N, int U, class Body>
+__device__ __forceinline__ void pieces(int64_t count, Body body) {
+    constexpr int64_t kRound = (int64_t)kThreads * N;
+    const int64_t lane = (int64_t)threadIdx.x * N;
+    int64_t at[U];
+    int first[U];
+    int64_t r = 0;
+    for (; r + U * kRound <= count; r += U * kRound) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) at[u] = r + u * kRound + lane, first[u] = 0;
+        body(at, first);
+    }
+    for (; r < count; r += U * kRound) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = r + u * kRound + lane, last = count - N;
+            at[u] = i < last ? i : last;
+            first[u] = (int)min(i - at[u], (int64_t)N);
+        }
+        body(at, first);
+    }
+}
+
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+    return x;
+}
+// the sum over the block's threads, in every thread
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double x) {
+    __shared__ double words[THREADS / 64];
+    x = wave_sum(x);
+    if (threadIdx.x % 64 == 0) words[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = words[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) x += words[w];
+    return x;
+}
+
+// A part of the sum of squares of a row, or (MEAN) of the mean of W rows: the rows'
+// coordinates are added up in fp32, in their order, as a synchronisation step does.
+template <class G, bool MEAN, class Src>
+__device__ __forceinline__ double part_sum(const Src& src, int64_t row, int W, float inv_w,
+                                           int64_t c0, int64_t c1) {
+    using T = typename G::T;
+    constexpr int N = G::N, U = MEAN ? 1 : 4;
+    double acc[4] = {0.0, 0.0, 0.0, 0.0};
+    src.runs(c0, c1, [&](int64_t t, int64_t e, int64_t count) {
+        if (count < N) {
+            if ((int64_t)threadIdx.x >= count) return;
+            const int64_t at = e + threadIdx.x;
+            float x;
+            if constexpr (MEAN) {
+                x = 0.0f;
+                for (int i = 0; i < W; ++i) x += G::one(src.row(i, t)[at]);
+                x *= inv_w;
+            } else {
+                x = G::one(src.row(row, t)[at]);
+            }
+            acc[0] = fma((double)x, (double)x, acc[0]);
+            return;
+        }
+        const auto load = [&](int64_t i, int64_t at) {
+            G g;
+            g.v = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(src.row(i, t)) + e +
+                                                      at);
+            return g;
+        };
+        pieces<N, U>(count, [&](const int64_t (&at)[U], const int (&first)[U]) {
+            if constexpr (MEAN) {
+                float s[N] = {};
+                const auto add = [&](int i, auto rows) {
+                    G g[rows];
+#pragma unroll
+                    for (int j = 0; j < rows; ++j) g[j] = load(i + j, at[0]);
+#pragma unroll
+                    for (int j = 0; j < rows; ++j)
+#pragma unroll
+                        for (int k = 0; k < N; ++k) s[k] += g[j].get(k);
+                };
+                int i = 0;
+                for (; i + 8 <= W; i += 8) add(i, std::integral_constant<int, 8>());
+                for (; i + 2 <= W; i += 2) add(i, std::integral_constant<int, 2>());
+                if (i < W) add(i, std::integral_constant<int, 1>());
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const float x = k < first[0] ? 0.0f : s[k] * inv_w;
+                    acc[k % 4] = fma((double)x, (double)x, acc[k % 4]);
+                }
+            } else {
+                G g[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) g[u] = load(row, at[u]);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        const float x = k < first[u] ? 0.0f : g[u].get(k);
+                        acc[k % 4] = fma((double)x, (double)x, acc[k % 4]);
+                    }
+            }
+        });
+    });
+    return (acc[0] + acc[1]) + (acc[2] + acc[3]);
+}
+
+// first chunk of part k of `parts`
+__device__ __forceinline__ int64_t part_start(int64_t chunks, int64_t parts, int64_t k) {
+    return chunks / parts * k + min(chunks % parts, k);
+}
+
+template <class G, bool MEAN, class Src>
+__global__ __launch_bounds__(kThreads) void norm_part_kernel(Src src, int W, float inv_w,
+                                                             int64_t chunks, int parts,
+                                                             double* sums) {
+    const int64_t row = blockIdx.x / parts, k = blockIdx.x % parts;
+    const double s = block_sum<kThreads>(part_sum<G, MEAN>(src, row, W, inv_w,
+                                                           part_start(chunks, parts, k),
+                                                           part_start(chunks, parts, k + 1)));
+    if (threadIdx.x == 0) sums[blockIdx.x] = s;
+}
+
+// the norm of a row from its parts, in every thread
+__device__ __forceinline__ float row_norm(const double* sums, int parts) {
+    double s = 0.0;
+    for (int k = threadIdx.x; k < parts; k += kThreads) s += sums[k];
+    return (float)sqrt(block_sum<kThreads>(s));
+}
+
+__global__ __launch_bounds__(kThreads) void norm_join_kernel(const double* sums, int parts,
+                                                             float* norm) {
+    const float x = row_norm(sums + (int64_t)blockIdx.x * parts, parts);
+    if (threadIdx.x == 0) norm[blockIdx.x] = x;
+}
+
+// 1 where the norm is not longer; a NaN stays one
+__device__ __forceinline__ float clip_scale(float norm, float max_norm) {
+    const float c = max_norm / (norm + 1e-6f);
+    return c >= 1.0f ? 1.0f : c;
+}
+
+// Part k of `parts` of a row, whose norm is the sum of `of_sums` parts (mean: every
+// row's is the first's).  Rows that are not longer than max_norm are not read.
+template <class G, class Src>
+__global__ __launch_bounds__(kThreads) void clip_kernel(Src src, int64_t chunks, int parts,
+                                                        const double* sums, int of_sums, int mean,
+                                                        float max_norm, float* norm) {
+    using T = typename G::T;
+    constexpr int N = G::N, U = 4;
+    const int64_t row = blockIdx.x / parts, k = blockIdx.x % parts, of = mean ? 0 : row;
+    const float x = row_norm(sums + of * of_sums, of_sums);
+    if (k == 0 && row == of && threadIdx.x == 0) norm[of] = x;
+    const float c = clip_scale(x, max_norm);
+    if (c == 1.0f) return;
+    src.runs(part_start(chunks, parts, k), part_start(chunks, parts, k + 1),
+             [&](int64_t t, int64_t e, int64_t count) {
+        T* const p = src.row(row, t) + e;
+        if (count < N) {
+            if ((int64_t)threadIdx.x < count)
+                p[threadIdx.x] = G::narrow(G::one(p[threadIdx.x]) * c);
+            return;
+        }
+        pieces<N, U>(count, [&](const int64_t (&at)[U], const int (&first)[U]) {
+            G g[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) g[u].v = *reinterpret_cast<const u32x4_any*>(p + at[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float y[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) y[j] = g[u].get(j) * c;
+                if (first[u] == 0) {
+                    g[u].set(y);
+                    *reinterpret_cast<u32x4_any*>(p + at[u]) = g[u].v;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (j >= first[u]) p[at[u] + j] = G::narrow(y[j]);
+                }
+            }
+        });
+    });
+}
+
+template <class... Args>
+int launch_blocks(void (*kernel)(Args...), int64_t blocks, void* stream,
+                  typename same_type<Args>::type... args) {
+    void* argv[] = {static_cast<void*>(&args)...};
+    return (int)hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((uint32_t)blocks),
+                                dim3(kThreads), argv, 0, static_cast<hipStream_t>(stream));
+}
+
+template <class G, class Src>
+int norm_parts_of(const Gradients& g, Src src, bool mean, int parts, double* sums, void* stream) {
+    const float inv_w = 1.0f / (float)g.W;
+    return mean ? launch_blocks(norm_part_kernel<G, true, Src>, parts, stream, src, g.W, inv_w,
+                                g.chunks, parts, sums)
+                : launch_blocks(norm_part_kernel<G, false, Src>, (int64_t)parts * g.W, stream, src,
+                                g.W, inv_w, g.chunks, parts, sums);
+}
+
+// f(piece type, source)
+template <class F>
+int with_source(const Gradients& g, F f) {
+    if (g.plan != nullptr) return f(F32Piece(), PlanRows{g.plan, g.W, g.n});
+    if (g.bf16)
+        return f(BF16Piece(), FlatRows<BF16Piece>{static_cast<uint16_t*>(g.base), g.ld, g.P});
+    return f(F32Piece(), FlatRows<F32Piece>{static_cast<float*>(g.base), g.ld, g.P});
+}
+
+}  // namespace
+
+int launch_grad_norm(const Gradients& g, bool mean, float* norm, void* workspace, void* stream) {
+    return with_source(g, [&](auto piece, auto src) {
+        using G = decltype(piece);
+        const int rows = mean ? 1 : g.W, parts = (int)norm_parts(rows, g.chunks);
+        auto* sums = static_cast<double*>(workspace);
+        if (int e = norm_parts_of<G>(g, src, mean, parts, sums, stream)) return e;
+        return launch_blocks(norm_join_kernel, rows, stream, sums, parts, norm);
+    });
+}
+
+int launch_clip_grads(const Gradients& g, bool mean, float max_norm, float* norm, void* workspace,
+                      void* stream) {
+    return with_source(g, [&](auto piece, auto src) {
+        using G = decltype(piece);
+        const int of_sums = (int)norm_parts(mean ? 1 : g.W, g.chunks);
+        const int parts = (int)norm_parts(g.W, g.chunks);
+        auto* sums = static_cast<double*>(workspace);
+        if (int e = norm_parts_of<G>(g, src, mean, of_sums, sums, stream)) return e;
+        return launch_blocks(clip_kernel<G, decltype(src)>, (int64_t)parts * g.W, stream, src,
+                             g.chunks, parts, sums, of_sums, (int)mean, max_norm, norm);
+    });
+}
+
+}  // namespace cpdp

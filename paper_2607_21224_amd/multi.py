@@ -6,7 +6,7 @@ from __future__ import annotations
 import torch
 
 from . import cpdp
-from .state import Hyper, Optimizer, _on, check_exact, load_exact
+from .state import Hyper, Norms, Optimizer, _on, check_exact, load_exact
 
 
 class CpdpMultiState:
@@ -37,6 +37,7 @@ class CpdpMultiState:
                              flat(self.mom), flat(self.mom2) if adamw else None,
                              flat(self.grads), self.slow_mom, self.anchor, param_dt)
         self.opt_step = 0
+        self._norms = Norms(self.W, self.table.device)
 
     def init(self, theta0_list, stream=None) -> None:
         """Algorithm 1 initialisation from per-tensor initial values.  The
@@ -53,6 +54,22 @@ class CpdpMultiState:
         torch.cuda.synchronize()
         cpdp.cpdp_state_init_plan(self.plan, _on(stream))
         self.opt_step = 0
+
+    def grad_norm(self, mean: bool = False, norm=None, stream=None) -> torch.Tensor:
+        """The norms of the gradients in self.grads (see CpdpState.grad_norm)."""
+        norm, ws = self._norms(cpdp.cpdp_grad_norm_plan_workspace(self.plan), mean, norm, stream)
+        cpdp.cpdp_grad_norm_plan(self.plan, norm, ws, cpdp.CPDP_NORM_MEAN if mean else 0,
+                                 _on(stream))
+        return norm
+
+    def clip_grads(self, max_norm: float, mean: bool = False, norm=None,
+                   stream=None) -> torch.Tensor:
+        """Clip the gradients in self.grads by their norms, over all of a replica's tensors
+        together (see CpdpState.clip_grads)."""
+        norm, ws = self._norms(cpdp.cpdp_grad_norm_plan_workspace(self.plan), mean, norm, stream)
+        cpdp.cpdp_clip_grads_plan(self.plan, max_norm, norm, ws,
+                                  cpdp.CPDP_NORM_MEAN if mean else 0, _on(stream))
+        return norm
 
     def step(self, t: int, opt: Optimizer, beta: float = 0.0, alpha: float = 1.0, T: int = 0,
              stream=None, method: str = "cpdp", flags: int = 0) -> str:

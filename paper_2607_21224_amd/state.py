@@ -58,6 +58,25 @@ def _on(stream):
     return torch.cuda.current_stream()
 
 
+class Norms:
+    """The workspace of a state's gradient norms, and the tensors that they go to.  One
+    workspace a state: its calls, and replays of graphs that hold them, do not run at the
+    same time."""
+
+    def __init__(self, W: int, device):
+        self.W, self.device, self.workspace = W, device, None
+
+    def __call__(self, nbytes: int, mean: bool, norm, stream) -> tuple:
+        if norm is None:
+            # torch ties a new tensor to its current stream
+            if stream is not None:
+                raise ValueError("norm: needed where a stream is given")
+            norm = torch.empty(1 if mean else self.W, dtype=torch.float32, device=self.device)
+        if self.workspace is None:
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return norm, self.workspace
+
+
 @dataclass(frozen=True)
 class Hyper:
     """Hyperparameters as the fp32 values the kernels use."""
@@ -157,6 +176,7 @@ class CpdpState:
         self.mom2 = torch.empty_like(self.mom) if adamw else None
         self.opt_step = 0         # optimizer updates applied (AdamW bias correction)
         self._count = None        # device word of count_unsynced
+        self._norms = Norms(self.W, self.params.device)
 
     @property
     def torch_param_dtype(self):
@@ -242,6 +262,32 @@ class CpdpState:
             kind = "local"
         self.opt_step += 1
         return kind
+
+    # ---- gradient norm and clipping, before a step ------------------------------
+
+    def grad_norm(self, grads: torch.Tensor, mean: bool = False, norm=None,
+                  stream=None) -> torch.Tensor:
+        """The norm of every replica's gradient, (W,) fp32, or with ``mean`` that of
+        their mean, (1,): of the gradient a synchronisation step uses.  It goes to the
+        tensor ``norm``, or a new one (on torch's current stream only)."""
+        self._check_grads(grads)
+        norm, ws = self._norms(cpdp.cpdp_grad_norm_workspace(self.W, self.P), mean, norm, stream)
+        cpdp.cpdp_grad_norm(grads, self.W, self.P, self.ld, norm, ws, self.grad_dt,
+                            cpdp.CPDP_NORM_MEAN if mean else 0, _on(stream))
+        return norm
+
+    def clip_grads(self, grads: torch.Tensor, max_norm: float, mean: bool = False, norm=None,
+                   stream=None) -> torch.Tensor:
+        """Scale every replica's gradient, in place, to a norm of at most ``max_norm``;
+        with ``mean`` all of them alike, so that their mean's is.  Returns the norms
+        there were, as grad_norm.  ``mean`` goes with the steps that use the mean
+        gradient (CPDP synchronisation and DDP steps), each replica's own with local and
+        LocalSGD steps."""
+        self._check_grads(grads)
+        norm, ws = self._norms(cpdp.cpdp_grad_norm_workspace(self.W, self.P), mean, norm, stream)
+        cpdp.cpdp_clip_grads(grads, self.W, self.P, self.ld, max_norm, norm, ws, self.grad_dt,
+                             cpdp.CPDP_NORM_MEAN if mean else 0, _on(stream))
+        return norm
 
     def step(self, t: int, grads: torch.Tensor, h: Hyper, T: int = 0,
              stream=None, method: str = "cpdp") -> str:
