@@ -19,8 +19,8 @@
  *
  * Layout.  A matrix argument of R rows and C columns has its element (r, c) at
  * base[r * ld + c].  Elements past a row's end are never written, and not used:
- * the gradients of a product read their operands in whole 16-byte pieces, up to 15
- * bytes past a row's end, the other calls read nothing there.
+ * the gradients of a product, and of the loss, read their operands in whole 16-byte
+ * pieces, up to 15 bytes past a row's end, the other calls read nothing there.
  * Every matrix starts on a 16-byte boundary and ld * sizeof(element) is a
  * multiple of 16 (CPDP_ERR_MISALIGNED); ld >= C.  Vectors (scales, w, dw) are
  * contiguous; w and dw start on a 16-byte boundary, scales and rstd on a 4-byte
@@ -175,6 +175,42 @@ int cpdp_q8_grad_weight(const void* dy, int64_t lddy, int dy_dt, const int8_t* a
                         const float* a_scale, int64_t T, int64_t N, int64_t K, void* dw,
                         int64_t lddw, int out_dt, void* workspace, int64_t workspace_bytes,
                         void* stream);
+
+/*
+ * Softmax cross entropy over V classes, of the logits
+ *   z[t, v] = x_scale[t] * w_scale[v] * sum_k x[t, k] * w[v, k]
+ * which are never held as a whole: the classes are taken in pieces.
+ *   cpdp_q8_xent      lse[t]  = log sum_v exp z[t, v]
+ *                     loss[t] = lse[t] - z[t, target[t]]
+ *   cpdp_q8_xent_bwd  d[t, v] = g[t] * (exp(z[t, v] - lse[t]) - (v == target[t] ? 1 : 0))
+ *                     dx[t, k] = sum_v d[t, v] * w_scale[v] * w[v, k]
+ *                     dw[v, k] = sum_t d[t, v] * x_scale[t] * x[t, k]
+ * x [T x K] with a scale for each row (token), w [V x K] with a scale for each row
+ * (class); target [T] int64 on an 8-byte boundary; loss, lse and g [T] fp32, lse as
+ * cpdp_q8_xent left it, g the gradient that reaches loss.  A token whose target is
+ * negative does not count: its loss and its row of dx are 0 and it adds nothing to dw,
+ * whatever its x and g hold.  One whose target is V or more has a NaN for its loss, its
+ * row of dx and all of dw.  dx [T x K] in dx_dt, dw [V x K] in dw_dt; either may be NULL
+ * and is then not computed.
+ * 0 <= T <= CPDP_Q8_MAX_T, 1 <= K <= CPDP_Q8_MAX_K.  Logits are exact sums, scaled in
+ * fp32, and everything that is taken of them is fp32.  The gradients' products run on
+ * the bfloat16 matrix cores with fp32 sums; each d[t, v], scaled, is held in three
+ * bfloat16 numbers for an fp32 result (all of its 24 bits, down to 2^-126, below which
+ * the matrix cores take a bfloat16 number as 0), in one for a bf16 result, as in the
+ * gradients of a product from fp32 dy.
+ */
+#define CPDP_Q8_MAX_T 4194232 /* 2^22 - 72: what a gradient sums over */
+
+int64_t cpdp_q8_xent_workspace(int64_t T, int64_t V, int64_t K);
+int cpdp_q8_xent(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw,
+                 const float* w_scale, const int64_t* target, int64_t T, int64_t V, int64_t K,
+                 float* loss, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t cpdp_q8_xent_bwd_workspace(int64_t T, int64_t V, int64_t K, int dx_dt, int dw_dt);
+int cpdp_q8_xent_bwd(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w,
+                     int64_t ldw, const float* w_scale, const int64_t* target, const float* lse,
+                     const float* g, int64_t T, int64_t V, int64_t K, void* dx, int64_t lddx,
+                     int dx_dt, void* dw, int64_t lddw, int dw_dt, void* workspace,
+                     int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -44,6 +44,8 @@ CLIP_SOURCES = ("kernels_clip.hip", "clip_api.cpp")
 # libcpdp_q8.so: kernel translation units and the host validation layer
 Q8_SOURCES = ("q8_rows.hip", "q8_norm.hip", "q8_act.hip", "q8_matmul.hip", "q8_grad.hip",
               "q8_grad_few.hip", "q8_api.cpp")
+# the loss on that path (in the same library)
+XENT_SOURCES = ("q8_xent.hip", "q8_xent_api.cpp")
 OBJ_ROOT = os.path.join(ROOT, "_build")
 
 
@@ -75,7 +77,7 @@ def build_cpdp(out: str = LIB_CPDP, extra=(),
 
 
 def build_q8(out: str = LIB_Q8) -> str:
-    return build_cpdp(out, sources=Q8_SOURCES)
+    return build_cpdp(out, sources=Q8_SOURCES + XENT_SOURCES)
 
 
 def build_q8_extension(out: str = EXT_Q8) -> str:

@@ -100,6 +100,16 @@ class Call {
                              shape_of(t));
         return place(t, name);
     }
+    const int64_t* wholes(PyObject* o, const char* name, int64_t n) {
+        const at::Tensor& t = tensor(o, name);
+        if (t.scalar_type() != at::kLong)
+            refuse(name, std::string("torch.int64 expected, the tensor is ") +
+                             c10::toString(t.scalar_type()));
+        if (t.dim() != 1 || t.size(0) != n || (n > 1 && t.stride(0) != 1))
+            refuse(name, "a dense vector of " + std::to_string(n) + " expected, the tensor is " +
+                             shape_of(t));
+        return static_cast<const int64_t*>(place(t, name));
+    }
     float* scales(PyObject* o, const char* name, int64_t n) {
         return static_cast<float*>(vec(o, name, n));
     }
@@ -360,12 +370,59 @@ PyObject* grad_weight(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// x, x_scale, w, w_scale, target, loss, lse, workspace, stream
+PyObject* xent(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return entry(args, n, 9, [](PyObject* const* a) {
+        Call c;
+        const Mat x = c.mat(a[0], "x", at::kChar);
+        const int64_t T = x.rows, K = x.cols;
+        const float* xs = c.scales(a[1], "x_scale", T);
+        const Mat w = c.mat(a[2], "w", at::kChar, -1, K);
+        const float* ws = c.scales(a[3], "w_scale", w.rows);
+        const int64_t* target = c.wholes(a[4], "target", T);
+        float* loss = c.scales(a[5], "loss", T);
+        float* lse = c.scales(a[6], "lse", T);
+        void* stream = c.stream(a[8]);
+        int64_t bytes;
+        void* room = c.workspace(a[7], cpdp_q8_xent_workspace(T, w.rows, K), &bytes);
+        return cpdp_q8_xent(static_cast<int8_t*>(x.p), x.ld, xs, static_cast<int8_t*>(w.p), w.ld,
+                            ws, target, T, w.rows, K, loss, lse, room, bytes, stream);
+    });
+}
+
+// x, x_scale, w, w_scale, target, lse, g, dx, dw, workspace, stream
+PyObject* xent_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return entry(args, n, 11, [](PyObject* const* a) {
+        Call c;
+        const Mat x = c.mat(a[0], "x", at::kChar);
+        const int64_t T = x.rows, K = x.cols;
+        const float* xs = c.scales(a[1], "x_scale", T);
+        const Mat w = c.mat(a[2], "w", at::kChar, -1, K);
+        const float* ws = c.scales(a[3], "w_scale", w.rows);
+        const int64_t* target = c.wholes(a[4], "target", T);
+        const float* lse = c.scales(a[5], "lse", T);
+        const float* g = c.scales(a[6], "g", T);
+        Mat dx = c.maybe(a[7], "dx", kEither, T, K);
+        Mat dw = c.maybe(a[8], "dw", kEither, w.rows, K);
+        if (a[7] == Py_None && a[8] == Py_None) refuse("dx", "neither dx nor dw is given");
+        if (a[7] == Py_None) dx.dt = dw.dt;
+        if (a[8] == Py_None) dw.dt = dx.dt;
+        void* stream = c.stream(a[10]);
+        int64_t bytes;
+        void* room = c.workspace(
+            a[9], cpdp_q8_xent_bwd_workspace(T, w.rows, K, dx.dt, dw.dt), &bytes);
+        return cpdp_q8_xent_bwd(static_cast<int8_t*>(x.p), x.ld, xs, static_cast<int8_t*>(w.p),
+                                w.ld, ws, target, lse, g, T, w.rows, K, dx.p, dx.ld, dx.dt, dw.p,
+                                dw.ld, dw.dt, room, bytes, stream);
+    });
+}
+
 #define ENTRY(name)                                                                          \
     {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, \
      nullptr}
 PyMethodDef methods[] = {ENTRY(rows),   ENTRY(values),  ENTRY(norm),       ENTRY(norm_bwd),
                          ENTRY(matmul), ENTRY(act),     ENTRY(act_bwd),    ENTRY(grad_input),
-                         ENTRY(grad_weight), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(grad_weight), ENTRY(xent), ENTRY(xent_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_q8", nullptr, -1, methods,
                       nullptr,               nullptr, nullptr, nullptr};
 

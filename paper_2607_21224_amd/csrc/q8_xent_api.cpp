@@ -1,0 +1,87 @@
+// C ABI of the loss on 8-bit rows: argument validation on the host, then the kernel
+// launches on the caller's stream.  No HIP call is made before every argument has been
+// checked.  The contract is documented in include/cpdp_q8.h.
+#include <cstdint>
+
+#include "q8_check.h"
+#include "q8_xent_launch.h"
+
+namespace {
+
+bool sizes_ok(int64_t T, int64_t V, int64_t K) {
+    return T >= 0 && V >= 1 && T <= CPDP_Q8_MAX_T && V <= kMaxRows && K >= 1 &&
+           K <= CPDP_Q8_MAX_K;
+}
+
+void inputs(Buffers& b, const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w,
+            int64_t ldw, const float* w_scale, const int64_t* target, int64_t T, int64_t V,
+            int64_t K) {
+    b.in(x, ldx, T, K, 1);
+    b.in(x_scale, T, 4, 4);
+    // (without rows nothing is read)
+    b.in(w, ldw, T == 0 ? 0 : V, K, 1);
+    b.in(w_scale, T == 0 ? 0 : V, 4, 4);
+    b.in(target, T, 8, 8);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t cpdp_q8_xent_workspace(int64_t T, int64_t V, int64_t K) {
+    return sizes_ok(T, V, K) && T > 0 ? cpdp::q8::xent_workspace(T, V, K) : 0;
+}
+
+int cpdp_q8_xent(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw,
+                 const float* w_scale, const int64_t* target, int64_t T, int64_t V, int64_t K,
+                 float* loss, float* lse, void* workspace, int64_t workspace_bytes,
+                 void* stream) {
+    if (!sizes_ok(T, V, K)) return CPDP_ERR_INVALID_ARG;
+    const int64_t need = cpdp_q8_xent_workspace(T, V, K);
+    if (workspace_bytes < need) return CPDP_ERR_INVALID_ARG;
+    Buffers b;
+    inputs(b, x, ldx, x_scale, w, ldw, w_scale, target, T, V, K);
+    b.out(loss, T, 4, 4);
+    b.out(lse, T, 4, 4);
+    if (need > 0) b.out(workspace, need, 1, 16);
+    if (int s = b.status()) return s;
+    if (ldx > kMaxTileLd || ldw > kMaxTileLd) return CPDP_ERR_TOO_LARGE;
+    if (T == 0) return CPDP_OK;
+    return hip_status(cpdp::q8::launch_xent({held(x, ldx, x_scale), held(w, ldw, w_scale), target,
+                                             T, V, K},
+                                            loss, lse, workspace, stream));
+}
+
+int64_t cpdp_q8_xent_bwd_workspace(int64_t T, int64_t V, int64_t K, int dx_dt, int dw_dt) {
+    return sizes_ok(T, V, K) && T > 0 && is_dtype(dx_dt) && is_dtype(dw_dt)
+               ? cpdp::q8::xent_bwd_workspace(T, V, K, dx_dt == CPDP_BF16, dw_dt == CPDP_BF16)
+               : 0;
+}
+
+int cpdp_q8_xent_bwd(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w,
+                     int64_t ldw, const float* w_scale, const int64_t* target, const float* lse,
+                     const float* g, int64_t T, int64_t V, int64_t K, void* dx, int64_t lddx,
+                     int dx_dt, void* dw, int64_t lddw, int dw_dt, void* workspace,
+                     int64_t workspace_bytes, void* stream) {
+    if (!sizes_ok(T, V, K)) return CPDP_ERR_INVALID_ARG;
+    if (!is_dtype(dx_dt) || !is_dtype(dw_dt)) return CPDP_ERR_DTYPE;
+    if (dx == nullptr && dw == nullptr && T > 0) return CPDP_ERR_NULL;
+    const int64_t need = cpdp_q8_xent_bwd_workspace(T, V, K, dx_dt, dw_dt);
+    if (workspace_bytes < need) return CPDP_ERR_INVALID_ARG;
+    Buffers b;
+    inputs(b, x, ldx, x_scale, w, ldw, w_scale, target, T, V, K);
+    b.in(lse, T, 4, 4);
+    b.in(g, T, 4, 4);
+    if (dx != nullptr) b.out(dx, lddx, T, K, esize(dx_dt == CPDP_BF16));
+    if (dw != nullptr) b.out(dw, lddw, V, K, esize(dw_dt == CPDP_BF16));
+    if (need > 0) b.out(workspace, need, 1, 16);
+    if (int s = b.status()) return s;
+    if (ldx > kMaxTileLd || ldw > kMaxTileLd) return CPDP_ERR_TOO_LARGE;
+    if (T == 0 && dw == nullptr) return CPDP_OK;
+    return hip_status(cpdp::q8::launch_xent_bwd({held(x, ldx, x_scale), held(w, ldw, w_scale),
+                                                 target, T, V, K},
+                                                lse, g, mat(dx, lddx, dx_dt), mat(dw, lddw, dw_dt),
+                                                workspace, stream));
+}
+
+}  // extern "C"

@@ -33,6 +33,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libcpdp_q8.so")
 
 CPDP_Q8_MAX_K = 131071
+CPDP_Q8_MAX_T = 4194232
 CPDP_ACT_GELU = 0
 CPDP_ACT_SWIGLU = 1
 ACTIVATIONS = {"gelu": CPDP_ACT_GELU, "swiglu": CPDP_ACT_SWIGLU}
@@ -41,7 +42,8 @@ ACTIVATIONS = {"gelu": CPDP_ACT_GELU, "swiglu": CPDP_ACT_SWIGLU}
 EXPORTS = ("cpdp_q8_rows", "cpdp_q8_values", "cpdp_q8_norm", "cpdp_q8_norm_bwd_workspace",
            "cpdp_q8_norm_bwd", "cpdp_q8_matmul_workspace", "cpdp_q8_matmul", "cpdp_q8_act",
            "cpdp_q8_act_bwd", "cpdp_q8_grad_input_workspace", "cpdp_q8_grad_input",
-           "cpdp_q8_grad_weight_workspace", "cpdp_q8_grad_weight")
+           "cpdp_q8_grad_weight_workspace", "cpdp_q8_grad_weight", "cpdp_q8_xent_workspace",
+           "cpdp_q8_xent", "cpdp_q8_xent_bwd_workspace", "cpdp_q8_xent_bwd")
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -67,6 +69,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "cpdp_q8_grad_input": [p, n, i, p, n, p, n, n, n, p, n, i, p, n, p],
         "cpdp_q8_grad_weight_workspace": [n, n, n, i, i],
         "cpdp_q8_grad_weight": [p, n, i, p, n, p, n, n, n, p, n, i, p, n, p],
+        "cpdp_q8_xent_workspace": [n, n, n],
+        "cpdp_q8_xent": [p, n, p, p, n, p, p, n, n, n, p, p, p, n, p],
+        "cpdp_q8_xent_bwd_workspace": [n, n, n, i, i],
+        "cpdp_q8_xent_bwd": [p, n, p, p, n, p, p, p, p, n, n, n, p, n, i, p, n, i, p, n, p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -176,3 +182,28 @@ def cpdp_q8_grad_weight(dy, a, a_scale, dw, workspace=None, stream=None, check=T
     """dw <- dy^T a, with a's rows scaled."""
     s = _q8.grad_weight(dy, a, a_scale, dw, workspace, _stream(stream))
     return _done(s, "cpdp_q8_grad_weight", check)
+
+
+def cpdp_q8_xent_workspace(T, V, K) -> int:
+    return lib.cpdp_q8_xent_workspace(T, V, K)
+
+
+def cpdp_q8_xent(x, x_scale, w, w_scale, target, loss, lse, workspace=None, stream=None,
+                 check=True):
+    """lse, loss <- the softmax cross entropy of the logits x w^T (rows of both scaled) and
+    target, (T,) int64; tokens whose target is negative do not count."""
+    s = _q8.xent(x, x_scale, w, w_scale, target, loss, lse, workspace, _stream(stream))
+    return _done(s, "cpdp_q8_xent", check)
+
+
+def cpdp_q8_xent_bwd_workspace(T, V, K, dx_dtype, dw_dtype) -> int:
+    """(the type of a gradient that is left out does not matter: that of the other)"""
+    return lib.cpdp_q8_xent_bwd_workspace(T, V, K, _CODE[dx_dtype], _CODE[dw_dtype])
+
+
+def cpdp_q8_xent_bwd(x, x_scale, w, w_scale, target, lse, g, dx=None, dw=None, workspace=None,
+                     stream=None, check=True):
+    """dx, dw (the ones that are given) <- the gradients of x's and w's values, where g (T,)
+    is the gradient of the loss and lse is cpdp_q8_xent's."""
+    s = _q8.xent_bwd(x, x_scale, w, w_scale, target, lse, g, dx, dw, workspace, _stream(stream))
+    return _done(s, "cpdp_q8_xent_bwd", check)
