@@ -390,23 +390,18 @@ struct Gemm {
         }
     }
 
-    static __device__ __forceinline__ void run(const Operands& o, const Target& t, int64_t tiles_m,
-                               int64_t tiles_n, int slices) {
-        __shared__ __attribute__((aligned(1024))) char lds[S * kBuffer];
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const int lane = threadIdx.x & 63;
-        const TileAt tile = tile_at(tiles_m, tiles_n, BM, BN);
-        const Loads l = loads(o, tile.m, tile.n, wave, lane);
-        const char* a0 = o.a + tile.m * o.lda;
-        const char* b0 = o.b + tile.n * o.ldb;
-
-        // whole steps of this slice: k0 to k1, and the short one at the end of the
-        // last slice
-        const int steps = o.row / kStep, tail = o.row % kStep;
-        const int k0 = (int)((int64_t)steps * tile.slice / slices);
-        const int k1 = (int)((int64_t)steps * (tile.slice + 1) / slices);
-
-        typename Op::Acc acc[MT][NT] = {};
+    // Adds up steps k0 to k1 of a tile whose first rows are a0 and b0, and (tail: its
+    // bytes) the short step at the end of the rows, which `last` holds (kEarly), or is
+    // read into it.
+    // What the end needs, the short step and the scales, is sent for first where
+    // registers are to be had and a block's time short enough for it to show
+    // (2000 x 2000 x 2000 18.5 us, and 19.8 with both at the end; 1576 x 1153 x
+    // 385 8.1 and 8.4).
+    static constexpr bool kEarly = BM <= 128;
+    static __device__ __forceinline__ void sums(const Operands& o, const Loads& l, const char* a0,
+                                                const char* b0, int k0, int k1, int tail,
+                                                Tail& last, char* lds, int wave, int lane,
+                                                typename Op::Acc (&acc)[MT][NT]) {
         // KS == 2: which half of a step the wavefront takes, and then of its rows of C
         const int wk = KS == 1 ? 0 : wave / (WM * WN);
         const int wm = wave / WN % WM, wn = wave % WN, r = lane & 15, g = lane >> 4;
@@ -419,35 +414,6 @@ struct Gemm {
         // buffer done with, one barrier, and the step S on is sent for into that
         // buffer while the second half is multiplied and the next step's first is
         // read.
-        // What the end needs, the short step and the scales, is sent for first where
-        // registers are to be had and a block's time short enough for it to show
-        // (2000 x 2000 x 2000 18.5 us, and 19.8 with both at the end; 1576 x 1153 x
-        // 385 8.1 and 8.4).
-        constexpr bool kEarly = BM <= 128;
-        constexpr int COLS = 4 * NT, MO = MT / KS;
-        const int64_t n0 = tile.n + wn * NT * 16 + g * COLS;
-        const bool has_tail = tail != 0 && tile.slice == slices - 1;
-        Tail last;
-        float cs[COLS], rs[MO];
-        const auto scales = [&] {
-            if (slices > 1 || t.row_scale == nullptr) return;
-#pragma unroll
-            for (int k = 0; k < COLS; ++k) {
-                const int64_t c = n0 + k;
-                cs[k] = t.col_scale[c < o.N ? c : o.N - 1];
-            }
-#pragma unroll
-            for (int i = 0; i < MO; ++i) {
-                const int64_t m = tile.m + (wm * MT + wk * MO + i) * 16 + r;
-                rs[i] = t.row_scale[m < o.M ? m : o.M - 1];
-            }
-        };
-        if constexpr (kEarly) {
-            if (has_tail)
-                load(last, a0 + (int64_t)steps * kStep, b0 + (int64_t)steps * kStep, l, wave, lane,
-                     tail, steps * kStep);
-            scales();
-        }
 
         const char* a_at = a0 + (int64_t)k0 * kStep;
         const char* b_at = b0 + (int64_t)k0 * kStep;
@@ -502,13 +468,13 @@ struct Gemm {
             if (k < k1 - 2) step(k++, Int<2>());
         if (k < k1 - 1) step(k++, Int<1>());
         if (k < k1) step(k, Int<0>());
-        if (has_tail) {
+        if (tail != 0) {
             // no load is on its way, and all wavefronts are past their reads of every
             // buffer but the last step's
             char* now = lds + (k1 - k0) % S * kBuffer;
             if constexpr (!kEarly)
-                load(last, a0 + (int64_t)steps * kStep, b0 + (int64_t)steps * kStep, l, wave, lane,
-                     tail, steps * kStep);
+                load(last, a0 + (int64_t)k1 * kStep, b0 + (int64_t)k1 * kStep, l, wave, lane, tail,
+                     k1 * kStep);
             store(last, now, wave, lane);
             __syncthreads();
             read(h0, now + off_a, now + off_b, wk, swap);
@@ -516,6 +482,52 @@ struct Gemm {
             multiply(h0, acc);
             if constexpr (KS == 1) multiply(h1, acc);
         }
+    }
+
+    static __device__ __forceinline__ void run(const Operands& o, const Target& t, int64_t tiles_m,
+                               int64_t tiles_n, int slices) {
+        __shared__ __attribute__((aligned(1024))) char lds[S * kBuffer];
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63;
+        const TileAt tile = tile_at(tiles_m, tiles_n, BM, BN);
+        const Loads l = loads(o, tile.m, tile.n, wave, lane);
+        const char* a0 = o.a + tile.m * o.lda;
+        const char* b0 = o.b + tile.n * o.ldb;
+
+        // whole steps of this slice: k0 to k1, and the short one at the end of the
+        // last slice
+        const int steps = o.row / kStep, tail = o.row % kStep;
+        const int k0 = (int)((int64_t)steps * tile.slice / slices);
+        const int k1 = (int)((int64_t)steps * (tile.slice + 1) / slices);
+
+        typename Op::Acc acc[MT][NT] = {};
+        const int wk = KS == 1 ? 0 : wave / (WM * WN);
+        const int wm = wave / WN % WM, wn = wave % WN, r = lane & 15, g = lane >> 4;
+        constexpr int COLS = 4 * NT, MO = MT / KS;
+        const int64_t n0 = tile.n + wn * NT * 16 + g * COLS;
+        const bool has_tail = tail != 0 && tile.slice == slices - 1;
+        Tail last;
+        float cs[COLS], rs[MO];
+        const auto scales = [&] {
+            if (slices > 1 || t.row_scale == nullptr) return;
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) {
+                const int64_t c = n0 + k;
+                cs[k] = t.col_scale[c < o.N ? c : o.N - 1];
+            }
+#pragma unroll
+            for (int i = 0; i < MO; ++i) {
+                const int64_t m = tile.m + (wm * MT + wk * MO + i) * 16 + r;
+                rs[i] = t.row_scale[m < o.M ? m : o.M - 1];
+            }
+        };
+        if constexpr (kEarly) {
+            if (has_tail)
+                load(last, a0 + (int64_t)steps * kStep, b0 + (int64_t)steps * kStep, l, wave, lane,
+                     tail, steps * kStep);
+            scales();
+        }
+        sums(o, l, a0, b0, k0, k1, has_tail ? tail : 0, last, lds, wave, lane, acc);
         typename Op::Acc sum[MO][NT];
         if constexpr (KS == 1) {
 #pragma unroll

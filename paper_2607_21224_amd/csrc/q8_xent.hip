@@ -1,69 +1,337 @@
 // Softmax cross entropy of 8-bit rows over the classes of 8-bit weights, and its
-// gradients, without the logits being kept: the classes are taken in pieces, whose
-// logits are made, used and overwritten by the next piece's.
-#include <initializer_list>
-
-#include "q8_gemm.h"
-#include "q8_xent_launch.h"
+// gradients, without the logits being kept.
+//
+// More than 64 tokens: tiles of the product of rows and weights whose results are used
+// where they are made (q8_xent_tile.h).  The loss takes one launch over all tiles and
+// one that joins what they found of each token.  Its gradients make the logits again, a
+// piece of the classes at a time, and leave the gradient of them laid out for two
+// products on the bf16 matrix cores (q8_grad_gemm.h).
+//
+// Up to 64 tokens: the logits are small (a piece of them at most 128 MB), and the
+// kernels of few tokens (q8_matmul.hip, q8_grad_few.hip) read the weights once each.
+#include "q8_grad_layout.h"
+#include "q8_xent_tile.h"
 
 namespace cpdp {
 namespace q8 {
 namespace {
 
-// Logits of a piece: 2^25 at most (128 MB), whole steps of 256 classes.
+constexpr int64_t kFewTokens = 64;
+
+// Takes parts of a workspace, each on a 256-byte boundary.
+struct Room {
+    int64_t bytes = 0;
+    int64_t take(int64_t n) {
+        const int64_t at = bytes;
+        bytes += up(n, 256) * 256;
+        return at;
+    }
+};
+template <class T>
+T* at(void* workspace, int64_t offset) {
+    return reinterpret_cast<T*>(static_cast<char*>(workspace) + offset);
+}
+
+// ---- many tokens ------------------------------------------------------------------
+
+// Joins the tiles' parts of each row's statistics: 16 rows a block, 16 threads a row.
+__global__ __launch_bounds__(256) void xent_join_kernel(const Stats* part, const float* hit,
+                                                        int64_t T, int64_t tiles, int64_t V,
+                                                        const int64_t* target, float* loss,
+                                                        float* lse) {
+    __shared__ Stats words[16][17];
+    const int row = threadIdx.x % 16, slice = threadIdx.x / 16;
+    const int64_t t = (int64_t)blockIdx.x * 16 + row, from = t < T ? t : T - 1;
+    Stats s = {-__builtin_inff(), 0.0f};
+    int64_t j = slice;
+    for (; j + 48 < tiles; j += 64) {
+        Stats v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = part[(j + 16 * i) * T + from];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = join(s, v[i]);
+    }
+    for (; j < tiles; j += 16) s = join(s, part[j * T + from]);
+    words[slice][row] = s;
+    __syncthreads();
+    if (slice != 0 || t >= T) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s = join(s, words[i][row]);
+    const float l = s.top + logf(s.sum);
+    const int64_t y = target[t];
+    lse[t] = l;
+    loss[t] = y < 0 ? 0.0f : l - (y < V ? hit[t] : __builtin_nanf(""));
+}
+
+// f(tile) with the tile's size as a compile-time number
+template <class F>
+int with_tile(int tile, F f) {
+    if (tile == 256) return f(Int<256>());
+    if (tile == 128) return f(Int<128>());
+    return f(Int<64>());
+}
+// wavefronts across a tile, LDS buffers of its loop, threads
+constexpr int across(int tile) { return tile == 256 ? 4 : 2; }
+constexpr int buffers(int tile) { return tile == 64 ? 4 : 2; }
+constexpr int threads(int tile) { return 128 * across(tile); }
+
+Logits logits_of(const Loss& l, int64_t first, int64_t n) {
+    Logits z{};
+    z.o.a = reinterpret_cast<const char*>(l.x.q);
+    z.o.b = reinterpret_cast<const char*>(l.w.q + first * l.w.ld);
+    z.o.lda = l.x.ld;
+    z.o.ldb = l.w.ld;
+    z.o.M = l.T;
+    z.o.N = n;
+    z.o.row = (int)l.K;
+    z.x_scale = l.x.scale;
+    z.w_scale = l.w.scale + first;
+    z.target = l.target;
+    z.first = first;
+    return z;
+}
+
+struct ForwardRoom : Room {
+    int tile;
+    int64_t tiles, part, hit;
+};
+ForwardRoom forward_room(int64_t T, int64_t V, int64_t K) {
+    ForwardRoom r;
+    r.tile = logit_tile(T, V, up(K, kStep));
+    r.tiles = up(V, r.tile);
+    r.part = r.take(r.tiles * T * (int64_t)sizeof(Stats));
+    r.hit = r.take(T * 4);
+    return r;
+}
+
+int forward(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
+    const ForwardRoom r = forward_room(l.T, l.V, l.K);
+    auto* part = at<Stats>(ws, r.part);
+    auto* hit = at<float>(ws, r.hit);
+    const int e = with_tile(r.tile, [&](auto tile) {
+        const int64_t tm = up(l.T, tile);
+        // (a launch holds fewer than 2^32 work items)
+        const int64_t most = (((int64_t)1 << 32) / threads(tile) - 1) / tm;
+        for (int64_t j = 0; j < r.tiles; j += most) {
+            const int64_t tn = r.tiles - j < most ? r.tiles - j : most, v = j * tile;
+            const Logits z = logits_of(l, v, l.V - v < tn * tile ? l.V - v : tn * tile);
+            if (int s = launch(xent_stats_kernel<tile, tile, 2, across(tile), buffers(tile)>,
+                               dim3((uint32_t)(tm * tn)), threads(tile), stream, z, part, hit, tm,
+                               tn, j))
+                return s;
+        }
+        return 0;
+    });
+    if (e) return e;
+    return launch(xent_join_kernel, dim3((uint32_t)up(l.T, 16)), 256, stream, part, hit, l.T,
+                  r.tiles, l.V, l.target, loss, lse);
+}
+
+// An 8-bit operand [R x C] as out [C x pad] in bf16, zeros from R to pad.
+__global__ __launch_bounds__(256) void xent_turn_kernel(Source s) {
+    __shared__ Tile<1, tile_cols<int8_t>()> tile;
+    transpose<I8, 1>(s, blockIdx.x, tile);
+}
+int turn(const Held& h, int64_t R, int64_t C, int64_t pad, uint16_t* out, void* stream) {
+    const Source s{h.q, h.ld, nullptr, R, C, out, pad, pad / 64 * up(C, tile_cols<int8_t>())};
+    if (s.blocks * 256 >= (int64_t)1 << 32) return (int)hipErrorInvalidValue;
+    return launch(xent_turn_kernel, dim3((uint32_t)s.blocks), 256, stream, s);
+}
+
+// Classes of a piece: 2^27 logits' gradients at most (268 MB a part), whole tiles.
 int64_t piece_of(int64_t T, int64_t V) {
-    int64_t n = ((int64_t)1 << 25) / (T < 1 ? 1 : T) / 256 * 256;
-    if (n < 256) n = 256;
+    const int64_t n = ((int64_t)1 << 27) / T / 1024 * 1024;
+    return n < 1024 ? (V < 1024 ? V : 1024) : n < V ? n : V;
+}
+
+struct BackwardRoom : Room {
+    int64_t piece, row_ld, class_ld;  // classes of a piece; row lengths of the slopes
+    int px, pw;                       // parts
+    int64_t by_row, by_class, x, w, sum, part, slices;
+};
+Shape product_shape(int64_t M, int64_t N, int64_t R, int parts) {
+    return grad_shape(M, N, up(R, kRound), parts, false);
+}
+BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
+    BackwardRoom r;
+    r.piece = piece_of(T, V);
+    r.row_ld = up(r.piece, kRound) * kRound;
+    r.class_ld = up(T, kRound) * kRound;
+    r.px = dx_bf16 ? 1 : 3;
+    r.pw = dw_bf16 ? 1 : 3;
+    r.by_row = r.take(r.px * T * r.row_ld * 2);
+    r.by_class = r.take(r.pw * r.piece * r.class_ld * 2);
+    r.x = r.take(K * r.class_ld * 2);
+    r.w = r.take(K * r.row_ld * 2);
+    if (r.piece < V) {
+        r.sum = r.take(T * K * 4);
+        r.part = r.take(T * up(K, 4) * 16);
+    }
+    int64_t most = 0;
+    const int64_t last = V - (V - 1) / r.piece * r.piece;
+    for (int i = 0; i < 2; ++i) {
+        const int64_t n = i ? last : r.piece;
+        const int64_t a = slices_bytes(T, K, product_shape(T, K, n, r.px));
+        const int64_t b = slices_bytes(n, K, product_shape(n, K, T, r.pw));
+        most = a > most ? a : most;
+        most = b > most ? b : most;
+    }
+    r.slices = r.take(most);
+    return r;
+}
+
+// c [M x N] = the product of A, laid out in parts, and B, laid out, over R values
+int product(const uint16_t* a, int64_t a_part, const uint16_t* b, int64_t ld, int64_t M,
+            int64_t N, int64_t R, int parts, Mat c, void* slices, void* stream) {
+    GradOperands o{};
+    o.a = reinterpret_cast<const char*>(a);
+    o.lda = o.ldb = ld * 2;
+    o.a_part = a_part * 2;
+    o.b = reinterpret_cast<const char*>(b);
+    o.R = R;
+    o.M = M;
+    o.N = N;
+    o.steps = (int)up(R, kRound);
+    o.parts = parts;
+    Target t{};
+    t.c = c.p;
+    t.ldc = c.ld;
+    t.bf16 = c.bf16;
+    const Shape s = product_shape(M, N, R, parts);
+    return parts == 1 ? launch_grad_gemm<false, false, 1>(o, t, s, slices, stream)
+                      : launch_grad_gemm<false, false, 3>(o, t, s, slices, stream);
+}
+
+// sum <- sum + part, to dx after the last piece
+__global__ __launch_bounds__(256) void xent_add_kernel(float* sum, const float* part,
+                                                       int64_t part_ld, int64_t K, int first,
+                                                       int last, Target out) {
+    const int64_t t = blockIdx.x;
+    for (int64_t k = threadIdx.x; k < K; k += 256) {
+        const float p = part[t * part_ld + k], x = first ? p : sum[t * K + k] + p;
+        if (!last) sum[t * K + k] = x;
+        else if (out.bf16) narrow(x, static_cast<uint16_t*>(out.c) + t * out.ldc + k);
+        else static_cast<float*>(out.c)[t * out.ldc + k] = x;
+    }
+}
+
+template <int PX, int PW>
+int launch_slopes(const Logits& z, const Slopes& to, int64_t K, void* stream) {
+    return with_tile(logit_tile(z.o.M, z.o.N, up(K, kStep)), [&](auto tile) {
+        const int64_t tm = up(z.o.M, tile), tn = up(z.o.N, tile);
+        if (tm * tn * threads(tile) >= (int64_t)1 << 32) return (int)hipErrorInvalidValue;
+        return launch(xent_slopes_kernel<tile, tile, 2, across(tile), buffers(tile), PX, PW>,
+                      dim3((uint32_t)(tm * tn)), threads(tile), stream, z, to, tm, tn);
+    });
+}
+
+int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, void* ws,
+             void* stream) {
+    const BackwardRoom r = backward_room(l.T, l.V, l.K, dx.bf16, dw.bf16);
+    const bool x = dx.p != nullptr, w = dw.p != nullptr;
+    if (w)
+        if (int e = turn(l.x, l.T, l.K, r.class_ld, at<uint16_t>(ws, r.x), stream)) return e;
+    for (int64_t v = 0; v < l.V; v += r.piece) {
+        const int64_t n = l.V - v < r.piece ? l.V - v : r.piece;
+        const Logits z = logits_of(l, v, n);
+        Slopes to{};
+        to.by_row = at<uint16_t>(ws, r.by_row);
+        to.by_class = at<uint16_t>(ws, r.by_class);
+        to.row_ld = up(n, kRound) * kRound;
+        to.row_part = l.T * to.row_ld;
+        to.class_ld = r.class_ld;
+        to.class_part = n * r.class_ld;
+        to.lse = lse;
+        to.g = g;
+        to.classes = l.V;
+        const int px = x ? r.px : 0, pw = w ? r.pw : 0;
+        const int e = px == 0   ? pw == 1 ? launch_slopes<0, 1>(z, to, l.K, stream)
+                                          : launch_slopes<0, 3>(z, to, l.K, stream)
+                      : px == 1 ? pw == 0   ? launch_slopes<1, 0>(z, to, l.K, stream)
+                                  : pw == 1 ? launch_slopes<1, 1>(z, to, l.K, stream)
+                                            : launch_slopes<1, 3>(z, to, l.K, stream)
+                      : pw == 0 ? launch_slopes<3, 0>(z, to, l.K, stream)
+                      : pw == 1 ? launch_slopes<3, 1>(z, to, l.K, stream)
+                                : launch_slopes<3, 3>(z, to, l.K, stream);
+        if (e) return e;
+        void* slices = at<char>(ws, r.slices);
+        if (x) {
+            auto* turned = at<uint16_t>(ws, r.w);
+            const bool whole = r.piece == l.V;
+            const int64_t ld = up(l.K, 4) * 4;
+            const Mat part{at<float>(ws, r.part), ld, false};
+            const Held held{l.w.q + v * l.w.ld, l.w.ld, nullptr};
+            if (int s = turn(held, n, l.K, to.row_ld, turned, stream)) return s;
+            if (int s = product(to.by_row, to.row_part, turned, to.row_ld, l.T, l.K, n, px,
+                                whole ? dx : part, slices, stream))
+                return s;
+            if (!whole) {
+                Target out{};
+                out.c = dx.p;
+                out.ldc = dx.ld;
+                out.bf16 = dx.bf16;
+                if (int s = launch(xent_add_kernel, dim3((uint32_t)l.T), 256, stream,
+                                   at<float>(ws, r.sum), static_cast<const float*>(part.p), ld,
+                                   l.K, (int)(v == 0), (int)(v + n == l.V), out))
+                    return s;
+            }
+        }
+        if (w) {
+            const Mat part{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4), dw.ld,
+                           dw.bf16};
+            if (int s = product(to.by_class, to.class_part, at<uint16_t>(ws, r.x), r.class_ld, n,
+                                l.K, l.T, pw, part, slices, stream))
+                return s;
+        }
+    }
+    return 0;
+}
+
+// ---- few tokens -------------------------------------------------------------------
+
+// Classes of a piece: 2^25 logits at most.
+int64_t few_piece(int64_t T, int64_t V) {
+    const int64_t n = ((int64_t)1 << 25) / T / 256 * 256;
     return n < V ? n : V;
 }
 
 // What is known of a row after some of the pieces.
-struct Stats {
+struct FewStats {
     float top, sum, hit;  // maximum, sum of exp(z - top), the target's logit
 };
 
-int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
-
-struct Room {
+struct FewRoom : Room {
     int64_t piece, ld;  // classes of a piece; its logits' row stride
-    int64_t logits, stats, scale, sum, part, product;  // where each begins
-    int64_t bytes;
+    int64_t logits, stats, scale, sum, part, product;
 };
-Room room_of(int64_t T, int64_t V, int64_t K, bool bwd, bool dx_bf16, bool dw_bf16) {
-    Room r{};
-    r.piece = piece_of(T, V);
-    r.ld = (r.piece + 15) / 16 * 16;
-    int64_t at = 0;
-    const auto take = [&](int64_t bytes) {
-        const int64_t here = at;
-        at += up256(bytes);
-        return here;
-    };
-    r.logits = take(T * r.ld * 4);
-    r.stats = take(T * (int64_t)sizeof(Stats));
-    int64_t product = matmul_workspace(T, r.piece, K);
+FewRoom few_room(int64_t T, int64_t V, int64_t K, bool bwd, bool dw_bf16) {
+    FewRoom r;
+    r.piece = few_piece(T, V);
+    r.ld = up(r.piece, 16) * 16;
+    r.logits = r.take(T * r.ld * 4);
+    r.stats = r.take(T * (int64_t)sizeof(FewStats));
+    int64_t most = 0;
     const int64_t last = V - (V - 1) / r.piece * r.piece;
-    for (const int64_t n : {r.piece, last}) {
+    for (int i = 0; i < 2; ++i) {
+        const int64_t n = i ? last : r.piece;
         const int64_t need[] = {matmul_workspace(T, n, K),
                                 bwd ? grad_input_workspace(T, n, K, false, false) : 0,
                                 bwd ? grad_weight_workspace(T, n, K, false, dw_bf16) : 0};
-        for (const int64_t b : need) product = b > product ? b : product;
+        for (const int64_t b : need) most = b > most ? b : most;
     }
     if (bwd) {
-        r.scale = take(T * 4);
-        const int64_t ldk = (K + 15) / 16 * 16;
-        r.sum = take(T * ldk * 4);
-        r.part = take(T * ldk * 4);
+        r.scale = r.take(T * 4);
+        r.sum = r.take(T * up(K, 16) * 64);
+        r.part = r.take(T * up(K, 16) * 64);
     }
-    r.product = take(product);
-    r.bytes = at;
+    r.product = r.take(most);
     return r;
 }
 
-struct Add2 {
+struct AddFloats {
     __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };
-struct Max2 {
+struct MaxFloats {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
 };
 
@@ -78,31 +346,28 @@ __device__ __forceinline__ float over_block(float x, Op op, float* words) {
     return x;
 }
 
-// exp(z - top), where top is the largest of some logits; nothing but -infinities: 0
-__device__ __forceinline__ float weight(float z, float top) {
-    return top == -__builtin_inff() ? (z == top ? 0.0f : z) : expf(z - top);
-}
-
 // A block takes a row of a piece's logits.
-__global__ __launch_bounds__(256) void xent_stats_kernel(const float* z, int64_t ld, int64_t v0,
-                                                         int n, const int64_t* target,
-                                                         Stats* stats, int first, int last,
-                                                         float* loss, float* lse) {
+__global__ __launch_bounds__(256) void xent_few_stats_kernel(const float* z, int64_t ld,
+                                                             int64_t v0, int n,
+                                                             const int64_t* target,
+                                                             FewStats* stats, int first, int last,
+                                                             float* loss, float* lse) {
     __shared__ float words[2][4];
     const int64_t t = blockIdx.x;
     const float* row = z + t * ld;
     float top = -__builtin_inff();
     for (int v = threadIdx.x; v < n; v += 256) top = fmaxf(top, row[v]);
-    top = over_block(top, Max2(), words[0]);
+    top = over_block(top, MaxFloats(), words[0]);
+    const float q = pivot(top);
     float sum = 0.0f;
-    for (int v = threadIdx.x; v < n; v += 256) sum += weight(row[v], top);
-    sum = over_block(sum, Add2(), words[1]);
+    for (int v = threadIdx.x; v < n; v += 256) sum += exp_of(row[v] - q);
+    sum = over_block(sum, AddFloats(), words[1]);
     if (threadIdx.x != 0) return;
-    Stats s = {-__builtin_inff(), 0.0f, __builtin_nanf("")};
+    FewStats s = {-__builtin_inff(), 0.0f, __builtin_nanf("")};
     if (!first) s = stats[t];
-    const float both = fmaxf(s.top, top);
-    s.sum = s.sum * weight(s.top, both) + sum * weight(top, both);
-    s.top = both;
+    const Stats both = join({s.top, s.sum}, {top, sum});
+    s.sum = both.sum;
+    s.top = both.top;
     const int64_t at = target[t] - v0;
     if (at >= 0 && at < n) s.hit = row[at];
     stats[t] = s;
@@ -114,15 +379,16 @@ __global__ __launch_bounds__(256) void xent_stats_kernel(const float* z, int64_t
 }
 
 // The logits' gradient takes the logits' place.  Rows that do not count have none.
-__global__ __launch_bounds__(256) void xent_grad_kernel(float* z, int64_t ld, int64_t v0, int n,
-                                                        int64_t V, const int64_t* target,
-                                                        const float* lse, const float* g) {
+__global__ __launch_bounds__(256) void xent_few_slopes_kernel(float* z, int64_t ld, int64_t v0,
+                                                              int n, int64_t V,
+                                                              const int64_t* target,
+                                                              const float* lse, const float* g) {
     const int64_t t = blockIdx.x;
     const int64_t y = target[t];
     const float l = y >= V ? __builtin_nanf("") : lse[t], f = g[t];
     for (int v = threadIdx.x; v < n; v += 256) {
         float* p = z + t * ld + v;
-        const float d = f * (expf(*p - l) - (v0 + v == y ? 1.0f : 0.0f));
+        const float d = f * (exp_of(*p - l) - (v0 + v == y ? 1.0f : 0.0f));
         *p = y < 0 ? 0.0f : d;
     }
 }
@@ -134,9 +400,10 @@ __global__ __launch_bounds__(256) void xent_scale_kernel(const float* scale, con
 }
 
 // sum <- sum + part, to dx after the last piece
-__global__ __launch_bounds__(256) void xent_add_kernel(float* sum, const float* part, int64_t ld,
-                                                       int64_t K, const int64_t* target, int first,
-                                                       int last, Target out) {
+__global__ __launch_bounds__(256) void xent_few_add_kernel(float* sum, const float* part,
+                                                           int64_t ld, int64_t K,
+                                                           const int64_t* target, int first,
+                                                           int last, Target out) {
     const int64_t t = blockIdx.x;
     for (int64_t k = threadIdx.x; k < K; k += 256) {
         const int64_t i = t * ld + k;
@@ -147,76 +414,87 @@ __global__ __launch_bounds__(256) void xent_add_kernel(float* sum, const float* 
     }
 }
 
-}  // namespace
-
-int64_t xent_workspace(int64_t T, int64_t V, int64_t K) {
-    return room_of(T, V, K, false, false, false).bytes;
-}
-
-int launch_xent(const Loss& l, float* loss, float* lse, void* workspace, void* stream) {
-    const Room r = room_of(l.T, l.V, l.K, false, false, false);
-    char* ws = static_cast<char*>(workspace);
-    auto* z = reinterpret_cast<float*>(ws + r.logits);
+int few_forward(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
+    const FewRoom r = few_room(l.T, l.V, l.K, false, false);
+    auto* z = at<float>(ws, r.logits);
     for (int64_t v = 0; v < l.V; v += r.piece) {
         const int64_t n = l.V - v < r.piece ? l.V - v : r.piece;
         const Held w{l.w.q + v * l.w.ld, l.w.ld, l.w.scale + v};
-        if (int e = launch_matmul(l.x, w, l.T, n, l.K, Mat{z, r.ld, false}, ws + r.product, stream))
+        if (int e = launch_matmul(l.x, w, l.T, n, l.K, Mat{z, r.ld, false},
+                                  at<char>(ws, r.product), stream))
             return e;
-        if (int e = launch(xent_stats_kernel, dim3((uint32_t)l.T), 256, stream, z, r.ld, v, (int)n,
-                           l.target, reinterpret_cast<Stats*>(ws + r.stats), (int)(v == 0),
+        if (int e = launch(xent_few_stats_kernel, dim3((uint32_t)l.T), 256, stream, z, r.ld, v,
+                           (int)n, l.target, at<FewStats>(ws, r.stats), (int)(v == 0),
                            (int)(v + n == l.V), loss, lse))
             return e;
     }
     return 0;
 }
 
-int64_t xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
-    return room_of(T, V, K, true, dx_bf16, dw_bf16).bytes;
-}
-
-int launch_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw,
-                    void* workspace, void* stream) {
-    const Room r = room_of(l.T, l.V, l.K, true, dx.bf16, dw.bf16);
-    char* ws = static_cast<char*>(workspace);
-    if (l.T == 0)
-        return launch_grad_weight(Mat{nullptr, 0, false}, l.x, 0, l.V, l.K, dw, ws, stream);
-    auto* z = reinterpret_cast<float*>(ws + r.logits);
-    auto* scale = reinterpret_cast<float*>(ws + r.scale);
-    const int64_t ldk = (l.K + 15) / 16 * 16;
-    if (int e = launch(xent_scale_kernel, dim3((uint32_t)((l.T + 255) / 256)), 256, stream,
-                       l.x.scale, l.target, l.T, scale))
+int few_backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, void* ws,
+                 void* stream) {
+    const FewRoom r = few_room(l.T, l.V, l.K, true, dw.bf16);
+    auto* z = at<float>(ws, r.logits);
+    auto* scale = at<float>(ws, r.scale);
+    char* room = at<char>(ws, r.product);
+    const int64_t ld = up(l.K, 16) * 16;
+    if (int e = launch(xent_scale_kernel, dim3((uint32_t)up(l.T, 256)), 256, stream, l.x.scale,
+                       l.target, l.T, scale))
         return e;
     for (int64_t v = 0; v < l.V; v += r.piece) {
         const int64_t n = l.V - v < r.piece ? l.V - v : r.piece;
         const Held w{l.w.q + v * l.w.ld, l.w.ld, l.w.scale + v};
         const Mat d{z, r.ld, false};
-        if (int e = launch_matmul(l.x, w, l.T, n, l.K, d, ws + r.product, stream)) return e;
-        if (int e = launch(xent_grad_kernel, dim3((uint32_t)l.T), 256, stream, z, r.ld, v, (int)n,
-                           l.V, l.target, lse, g))
+        if (int e = launch_matmul(l.x, w, l.T, n, l.K, d, room, stream)) return e;
+        if (int e = launch(xent_few_slopes_kernel, dim3((uint32_t)l.T), 256, stream, z, r.ld, v,
+                           (int)n, l.V, l.target, lse, g))
             return e;
         if (dx.p != nullptr) {
-            const Mat part{ws + r.part, ldk, false};
-            if (int e = launch_grad_input(d, w, l.T, n, l.K, part, ws + r.product, stream))
-                return e;
+            const Mat part{at<float>(ws, r.part), ld, false};
+            if (int e = launch_grad_input(d, w, l.T, n, l.K, part, room, stream)) return e;
             Target out{};
             out.c = dx.p;
             out.ldc = dx.ld;
             out.bf16 = dx.bf16;
-            if (int e = launch(xent_add_kernel, dim3((uint32_t)l.T), 256, stream,
-                               reinterpret_cast<float*>(ws + r.sum),
-                               reinterpret_cast<const float*>(ws + r.part), ldk, l.K, l.target,
+            if (int e = launch(xent_few_add_kernel, dim3((uint32_t)l.T), 256, stream,
+                               at<float>(ws, r.sum), at<float>(ws, r.part), ld, l.K, l.target,
                                (int)(v == 0), (int)(v + n == l.V), out))
                 return e;
         }
         if (dw.p != nullptr) {
-            const int64_t e = dw.bf16 ? 2 : 4;
-            const Mat part{static_cast<char*>(dw.p) + v * dw.ld * e, dw.ld, dw.bf16};
-            if (int s = launch_grad_weight(d, Held{l.x.q, l.x.ld, scale}, l.T, n, l.K, part,
-                                           ws + r.product, stream))
-                return s;
+            const Mat part{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4), dw.ld,
+                           dw.bf16};
+            if (int e = launch_grad_weight(d, Held{l.x.q, l.x.ld, scale}, l.T, n, l.K, part, room,
+                                           stream))
+                return e;
         }
     }
     return 0;
+}
+
+}  // namespace
+
+int64_t xent_workspace(int64_t T, int64_t V, int64_t K) {
+    return T <= kFewTokens ? few_room(T, V, K, false, false).bytes : forward_room(T, V, K).bytes;
+}
+
+int launch_xent(const Loss& l, float* loss, float* lse, void* workspace, void* stream) {
+    return l.T <= kFewTokens ? few_forward(l, loss, lse, workspace, stream)
+                             : forward(l, loss, lse, workspace, stream);
+}
+
+int64_t xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
+    return T <= kFewTokens ? few_room(T, V, K, true, dw_bf16).bytes
+                           : backward_room(T, V, K, dx_bf16, dw_bf16).bytes;
+}
+
+int launch_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw,
+                    void* workspace, void* stream) {
+    // a sum over no tokens
+    if (l.T == 0)
+        return launch_grad_weight(Mat{nullptr, 0, false}, l.x, 0, l.V, l.K, dw, workspace, stream);
+    return l.T <= kFewTokens ? few_backward(l, lse, g, dx, dw, workspace, stream)
+                             : backward(l, lse, g, dx, dw, workspace, stream);
 }
 
 }  // namespace q8
