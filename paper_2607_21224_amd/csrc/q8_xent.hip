@@ -57,10 +57,10 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const Stats* part, const
     if (slice != 0 || t >= T) return;
 #pragma unroll
     for (int i = 1; i < 16; ++i) s = join(s, words[i][row]);
-    const float l = s.top + logf(s.sum);
+    const float l = s.top + log2f(s.sum);
     const int64_t y = target[t];
-    lse[t] = l;
-    loss[t] = y < 0 ? 0.0f : l - (y < V ? hit[t] : __builtin_nanf(""));
+    lse[t] = l * kLn2;
+    loss[t] = y < 0 ? 0.0f : (l - (y < V ? hit[t] : __builtin_nanf(""))) * kLn2;
 }
 
 // f(tile) with the tile's size as a compile-time number
@@ -115,7 +115,7 @@ int forward(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
         for (int64_t j = 0; j < r.tiles; j += most) {
             const int64_t tn = r.tiles - j < most ? r.tiles - j : most, v = j * tile;
             const Logits z = logits_of(l, v, l.V - v < tn * tile ? l.V - v : tn * tile);
-            if (int s = launch(xent_stats_kernel<tile, tile, 2, across(tile), buffers(tile)>,
+            if (int s = launch(xent_stats_kernel<tile, across(tile), buffers(tile)>,
                                dim3((uint32_t)(tm * tn)), threads(tile), stream, z, part, hit, tm,
                                tn, j))
                 return s;
@@ -147,11 +147,38 @@ int64_t piece_of(int64_t T, int64_t V) {
 struct BackwardRoom : Room {
     int64_t piece, row_ld, class_ld;  // classes of a piece; row lengths of the slopes
     int px, pw;                       // parts
-    int64_t by_row, by_class, x, w, sum, part, slices;
+    int64_t by_row, by_class, x, w, sum, slices;
 };
+
+// The tile of a gradient's product, and the slices that its sum over R is cut into where
+// there are fewer tiles than CUs.  A step of a tile takes what it takes in grad_shape;
+// here the large tiles are cut, too: dx of 4096 x 1024 over 32768 classes has 64 tiles of
+// 256 x 256, and in 4 slices takes 260 us, in 256 tiles of 128 x 128 335.
 Shape product_shape(int64_t M, int64_t N, int64_t R, int parts) {
-    return grad_shape(M, N, up(R, kRound), parts, false);
+    const int64_t steps = up(R, kRound);
+    struct {
+        int bm, bn, passes, alone, each, end;
+    } const tiles[] = {{256, 256, parts, 1800, 1800, 2000},
+                       {256, 128, parts, 1100, 1100, 1500},
+                       {128, 128, 1, 310 + 290 * parts, 230 + 390 * parts, 800},
+                       {64, 64, 1, 250 + 100 * parts, 105 + 115 * parts, 500}};
+    Shape best = {0, 0, 1, -1};
+    for (const auto& t : tiles) {
+        if (t.bm + t.bn == 384 && parts > 1) continue;
+        const int64_t n = up(M, t.bm) * up(N, t.bn), all = steps * t.passes;
+        if (t.bm < 256 && n >= (int64_t)1 << 23) continue;
+        for (int slices = 1; slices <= 64; slices *= 2) {
+            if (slices > 1 && (n * slices > (t.bm == 64 ? 2048 : 512) || all < 4 * slices)) break;
+            const int64_t turns = up(n * slices, kCus);
+            const double step = turns == 1 ? t.alone : (double)turns * t.each;
+            const double time = (double)up(all, slices) * step + turns * t.end +
+                                (slices > 1 ? 4500.0 + slices * (double)M * (double)N / 500.0 : 0);
+            if (best.ns < 0 || time < best.ns) best = {t.bm, t.bn, slices, time};
+        }
+    }
+    return best;
 }
+
 BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
     BackwardRoom r;
     r.piece = piece_of(T, V);
@@ -163,15 +190,14 @@ BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
     r.by_class = r.take(r.pw * r.piece * r.class_ld * 2);
     r.x = r.take(K * r.class_ld * 2);
     r.w = r.take(K * r.row_ld * 2);
-    if (r.piece < V) {
-        r.sum = r.take(T * K * 4);
-        r.part = r.take(T * up(K, 4) * 16);
-    }
+    const bool pieces = r.piece < V;
+    if (pieces) r.sum = r.take(T * slices_ld(K) * 4);
     int64_t most = 0;
     const int64_t last = V - (V - 1) / r.piece * r.piece;
     for (int i = 0; i < 2; ++i) {
         const int64_t n = i ? last : r.piece;
-        const int64_t a = slices_bytes(T, K, product_shape(T, K, n, r.px));
+        const int64_t a = pieces ? T * slices_ld(K) * 4 * product_shape(T, K, n, r.px).slices
+                                 : slices_bytes(T, K, product_shape(T, K, n, r.px));
         const int64_t b = slices_bytes(n, K, product_shape(n, K, T, r.pw));
         most = a > most ? a : most;
         most = b > most ? b : most;
@@ -180,7 +206,18 @@ BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
     return r;
 }
 
-// c [M x N] = the product of A, laid out in parts, and B, laid out, over R values
+template <int P>
+int launch_product(const GradOperands& o, const Target& t, const Shape& s, void* stream) {
+    if (s.bn == 256) return launch_grad_tiles<256, 256, 2, 4, false, false, 1>(o, t, s.slices, stream);
+    if constexpr (P == 1)
+        if (s.bm == 256)
+            return launch_grad_tiles<256, 128, 4, 2, false, false, 1>(o, t, s.slices, stream);
+    if (s.bm == 128) return launch_grad_tiles<128, 128, 2, 2, false, false, P>(o, t, s.slices, stream);
+    return launch_grad_tiles<64, 64, 2, 2, false, false, P>(o, t, s.slices, stream);
+}
+
+// c [M x N] = the product of A, laid out in parts, and B, laid out, over R values.
+// Without c, the slices (one at least) are left for xent_add_kernel.
 int product(const uint16_t* a, int64_t a_part, const uint16_t* b, int64_t ld, int64_t M,
             int64_t N, int64_t R, int parts, Mat c, void* slices, void* stream) {
     GradOperands o{};
@@ -194,25 +231,53 @@ int product(const uint16_t* a, int64_t a_part, const uint16_t* b, int64_t ld, in
     o.steps = (int)up(R, kRound);
     o.parts = parts;
     Target t{};
-    t.c = c.p;
-    t.ldc = c.ld;
-    t.bf16 = c.bf16;
+    t.c = c.p != nullptr ? c.p : slices;
+    t.ldc = c.p != nullptr ? c.ld : slices_ld(N);
+    t.bf16 = c.p != nullptr && c.bf16;
+    t.ws = slices;
+    t.ldws = slices_ld(N);
+    t.slice = M * t.ldws;
     const Shape s = product_shape(M, N, R, parts);
-    return parts == 1 ? launch_grad_gemm<false, false, 1>(o, t, s, slices, stream)
-                      : launch_grad_gemm<false, false, 3>(o, t, s, slices, stream);
+    if (int e = parts == 1 ? launch_product<1>(o, t, s, stream)
+                           : launch_product<3>(o, t, s, stream))
+        return e;
+    return c.p == nullptr || s.slices == 1 ? 0 : launch_join<Bf16>(t, M, N, s.slices, stream);
 }
 
-// sum <- sum + part, to dx after the last piece
-__global__ __launch_bounds__(256) void xent_add_kernel(float* sum, const float* part,
-                                                       int64_t part_ld, int64_t K, int first,
-                                                       int last, Target out) {
-    const int64_t t = blockIdx.x;
-    for (int64_t k = threadIdx.x; k < K; k += 256) {
-        const float p = part[t * part_ld + k], x = first ? p : sum[t * K + k] + p;
-        if (!last) sum[t * K + k] = x;
-        else if (out.bf16) narrow(x, static_cast<uint16_t*>(out.c) + t * out.ldc + k);
-        else static_cast<float*>(out.c)[t * out.ldc + k] = x;
+// sum <- sum and the slices of a piece, to dx after the last piece; 4 columns a thread
+__global__ __launch_bounds__(256) void xent_add_kernel(float* sum, const float* part, int64_t ld,
+                                                       int64_t slice, int64_t T, int64_t K,
+                                                       int slices, int first, int last,
+                                                       Target out) {
+    const int64_t across = (K + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t t = i / across, k = i % across * 4;
+    if (t >= T) return;
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (!first) x = *reinterpret_cast<const f32x4*>(sum + t * ld + k);
+    for (int z = 0; z < slices; ++z)
+        x += *reinterpret_cast<const f32x4*>(part + z * slice + t * ld + k);
+    if (!last) {
+        *reinterpret_cast<f32x4*>(sum + t * ld + k) = x;
+        return;
     }
+    const float v[4] = {x[0], x[1], x[2], x[3]};
+    store_cols<4>(out, t, k, (int)(K - k < 4 ? K - k : 4), v);
+}
+int add(const BackwardRoom& r, void* ws, const Loss& l, int slices, bool first, bool last, Mat dx,
+        void* stream) {
+    Target out{};
+    out.c = dx.p;
+    out.ldc = dx.ld;
+    out.bf16 = dx.bf16;
+    const int64_t ld = slices_ld(l.K), across = up(l.K, 4);
+    // (a launch holds fewer than 2^32 work items)
+    return in_parts(l.T, across, [&](int64_t t, int64_t n) {
+        Target part = out;
+        part.c = static_cast<char*>(out.c) + t * out.ldc * (out.bf16 ? 2 : 4);
+        return launch(xent_add_kernel, dim3((uint32_t)up(n * across, 256)), 256, stream,
+                      at<float>(ws, r.sum) + t * ld, at<const float>(ws, r.slices) + t * ld, ld,
+                      l.T * ld, n, l.K, slices, (int)first, (int)last, part);
+    });
 }
 
 template <int PX, int PW>
@@ -220,7 +285,7 @@ int launch_slopes(const Logits& z, const Slopes& to, int64_t K, void* stream) {
     return with_tile(logit_tile(z.o.M, z.o.N, up(K, kStep)), [&](auto tile) {
         const int64_t tm = up(z.o.M, tile), tn = up(z.o.N, tile);
         if (tm * tn * threads(tile) >= (int64_t)1 << 32) return (int)hipErrorInvalidValue;
-        return launch(xent_slopes_kernel<tile, tile, 2, across(tile), buffers(tile), PX, PW>,
+        return launch(xent_slopes_kernel<tile, across(tile), buffers(tile), PX, PW>,
                       dim3((uint32_t)(tm * tn)), threads(tile), stream, z, to, tm, tn);
     });
 }
@@ -258,23 +323,15 @@ int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, vo
         if (x) {
             auto* turned = at<uint16_t>(ws, r.w);
             const bool whole = r.piece == l.V;
-            const int64_t ld = up(l.K, 4) * 4;
-            const Mat part{at<float>(ws, r.part), ld, false};
             const Held held{l.w.q + v * l.w.ld, l.w.ld, nullptr};
             if (int s = turn(held, n, l.K, to.row_ld, turned, stream)) return s;
             if (int s = product(to.by_row, to.row_part, turned, to.row_ld, l.T, l.K, n, px,
-                                whole ? dx : part, slices, stream))
+                                whole ? dx : Mat{nullptr, 0, false}, slices, stream))
                 return s;
-            if (!whole) {
-                Target out{};
-                out.c = dx.p;
-                out.ldc = dx.ld;
-                out.bf16 = dx.bf16;
-                if (int s = launch(xent_add_kernel, dim3((uint32_t)l.T), 256, stream,
-                                   at<float>(ws, r.sum), static_cast<const float*>(part.p), ld,
-                                   l.K, (int)(v == 0), (int)(v + n == l.V), out))
+            if (!whole)
+                if (int s = add(r, ws, l, product_shape(l.T, l.K, n, px).slices, v == 0,
+                                v + n == l.V, dx, stream))
                     return s;
-            }
         }
         if (w) {
             const Mat part{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4), dw.ld,
@@ -361,6 +418,7 @@ __global__ __launch_bounds__(256) void xent_few_stats_kernel(const float* z, int
     const float q = pivot(top);
     float sum = 0.0f;
     for (int v = threadIdx.x; v < n; v += 256) sum += exp_of(row[v] - q);
+    top *= kLog2e;
     sum = over_block(sum, AddFloats(), words[1]);
     if (threadIdx.x != 0) return;
     FewStats s = {-__builtin_inff(), 0.0f, __builtin_nanf("")};
@@ -372,9 +430,9 @@ __global__ __launch_bounds__(256) void xent_few_stats_kernel(const float* z, int
     if (at >= 0 && at < n) s.hit = row[at];
     stats[t] = s;
     if (last) {
-        const float l = s.top + logf(s.sum);
-        lse[t] = l;
-        loss[t] = target[t] < 0 ? 0.0f : l - s.hit;
+        const float l = s.top + log2f(s.sum);
+        lse[t] = l * kLn2;
+        loss[t] = target[t] < 0 ? 0.0f : (l - s.hit * kLog2e) * kLn2;
     }
 }
 

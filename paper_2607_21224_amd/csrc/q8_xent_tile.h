@@ -32,52 +32,90 @@ struct Slopes {
     int64_t classes;  // of the loss
 };
 
-// What is known of a row's logits after some of the classes: the largest, and the sum of
-// exp(z - top).
+// What is known of a row's logits, in units of log 2 (as powers of two), after some of the
+// classes: the largest, and the sum of 2^(z - top).
 struct Stats {
     float top, sum;
 };
 
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
 // exp(x) for x <= 0 or NaN, as 2^(x log2 e): v_exp is within a unit of the last place,
 // what its argument's rounding adds is |x| 2^-24 at most.  Results below 2^-126 are 0.
-__device__ __forceinline__ float exp_of(float x) {
-    return __builtin_amdgcn_exp2f(x * 1.44269504f);
-}
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
-// `top` to subtract: with nothing but -infinities, 0 (their exp is then 0)
+// `top` to subtract: with nothing but -infinities, 0 (their powers are then 0)
 __device__ __forceinline__ float pivot(float top) { return top == -__builtin_inff() ? 0.0f : top; }
 
 __device__ __forceinline__ Stats join(Stats a, Stats b) {
     const float top = fmaxf(a.top, b.top), p = pivot(top);
-    return {top, a.sum * exp_of(a.top - p) + b.sum * exp_of(b.top - p)};
+    return {top, a.sum * __builtin_amdgcn_exp2f(a.top - p) +
+                     b.sum * __builtin_amdgcn_exp2f(b.top - p)};
 }
 
-template <int BM, int BN, int WM, int WN, int S>
+// Tiles of TILE rows and classes by 2 x WN wavefronts, with S LDS buffers.
+template <int TILE, int WN, int S>
 struct LogitTile {
-    using G = Gemm<Int8, BM, BN, WM, WN, S>;
+    using G = Gemm<Int8, TILE, TILE, 2, WN, S>;
     static constexpr int MT = G::MT, NT = G::NT, COLS = 4 * NT;
-    static constexpr int kThreads = G::kThreads;
-    static constexpr int kLds = S * G::kBuffer;
+    static constexpr int kThreads = G::kThreads, kWaves = G::kWaves;
+    static constexpr int kBuffers = S * G::kBuffer;
 
     struct Place {
         TileAt tile;
         int wave, lane, wm, wn, r, g;
-        int64_t n0;  // the lane's first class
+        int row;    // of the tile, the lane's first (16 apart)
+        int first;  // class of the tile, the lane's first
     };
     static __device__ __forceinline__ Place place(int64_t tiles_m, int64_t tiles_n) {
         Place p;
-        p.tile = tile_at(tiles_m, tiles_n, BM, BN);
+        p.tile = tile_at(tiles_m, tiles_n, TILE, TILE);
         p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         p.lane = threadIdx.x & 63;
         p.wm = p.wave / WN;
         p.wn = p.wave % WN;
         p.r = p.lane & 15;
         p.g = p.lane >> 4;
-        p.n0 = p.tile.n + p.wn * NT * 16 + p.g * COLS;
+        p.row = p.wm * MT * 16 + p.r;
+        p.first = p.wn * NT * 16 + p.g * COLS;
         return p;
     }
-    static __device__ __forceinline__ int64_t row(const Place& p, int i) {
-        return p.tile.m + (p.wm * MT + i) * 16 + p.r;
+
+    // What the end needs of each row and class of the tile, sent for into LDS before the
+    // sums' loads, so that it is there when they are done.  (Held in registers from the
+    // start, or loaded at the end, it made the large tile's kernels spill; in an LDS array of
+    // its own it made the compiler wait for all loads in the loop, 1945 -> 2275 us for the
+    // logits of 8192 x 131072 x 2048.)
+    struct Vectors {
+        float x_scale[TILE], w_scale[TILE];
+        uint32_t target[2][TILE];  // halves
+        float lse[TILE], g[TILE];
+    };
+    static __device__ __forceinline__ void send(const Logits& l, const Slopes* to, const Place& p,
+                                                Vectors& v) {
+        constexpr int kEach = TILE / 64;
+        const int count = (to != nullptr ? 6 : 4) * kEach;
+#pragma unroll
+        for (int j = 0; j < (6 * kEach + kWaves - 1) / kWaves; ++j) {
+            const int k = j * kWaves + p.wave;
+            if (k >= count) break;
+            const int what = k / kEach, at = k % kEach * 64;
+            // rows and classes that are not there take the last one's
+            const int64_t m = p.tile.m + at + p.lane < l.o.M ? p.tile.m + at + p.lane : l.o.M - 1;
+            const int64_t n = p.tile.n + at + p.lane < l.o.N ? p.tile.n + at + p.lane : l.o.N - 1;
+            const auto* half = reinterpret_cast<const uint32_t*>(l.target + m);
+            const void* from = what == 0   ? static_cast<const void*>(l.x_scale + m)
+                               : what == 1 ? static_cast<const void*>(l.w_scale + n)
+                               : what == 2 ? static_cast<const void*>(half)
+                               : what == 3 ? static_cast<const void*>(half + 1)
+                               : what == 4 ? static_cast<const void*>(to->lse + m)
+                                           : static_cast<const void*>(to->g + m);
+            __builtin_amdgcn_global_load_lds(
+                (__attribute__((address_space(1))) void*)(from),
+                (__attribute__((address_space(3))) void*)(reinterpret_cast<char*>(&v) +
+                                                          (what * TILE + at) * 4),
+                4, 0, 0);
+        }
     }
 
     static __device__ __forceinline__ void sums(const Logits& l, const Place& p, char* lds,
@@ -93,90 +131,81 @@ struct LogitTile {
                 G::load(last, a0 + (int64_t)steps * kStep, b0 + (int64_t)steps * kStep, at, p.wave,
                         p.lane, tail, steps * kStep);
         G::sums(o, at, a0, b0, 0, steps, tail, last, lds, p.wave, p.lane, acc);
+        // all have read the last step, and the vectors are there
+        wait_loads<0>();
+        barrier();
     }
 
-    // f(i, row, z, hot) for each of the lane's rows with its logits; hot: which of them is
-    // the target's, in [0, COLS) if any.  Classes that are not there have -infinity.
-    template <class F>
-    static __device__ __forceinline__ void for_rows(const Logits& l, const Place& p,
-                                                    const i32x4 (&acc)[MT][NT], F f) {
-        float ws[COLS], xs[MT];
-        int64_t y[MT];
-#pragma unroll
-        for (int k = 0; k < COLS; ++k) {
-            const int64_t c = p.n0 + k;
-            ws[k] = l.w_scale[c < l.o.N ? c : l.o.N - 1];
-        }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int64_t m = row(p, i), at = m < l.o.M ? m : l.o.M - 1;
-            xs[i] = l.x_scale[at];
-            y[i] = l.target[at];
-        }
-        const bool whole = p.tile.n + BN <= l.o.N;
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            float z[COLS];
-#pragma unroll
-            for (int k = 0; k < COLS; ++k) z[k] = (float)acc[i][k / 4][k % 4] * xs[i] * ws[k];
-            if (!whole) {
-#pragma unroll
-                for (int k = 0; k < COLS; ++k)
-                    z[k] = p.n0 + k < l.o.N ? z[k] : -__builtin_inff();
-            }
-            // (a negative target is before every class)
-            const int64_t hot = y[i] - l.first - p.n0;
-            f(i, row(p, i), z, hot >= 0 && hot < COLS && p.n0 + hot < l.o.N ? (int)hot : -1, xs[i],
-              ws, y[i]);
-        }
+    // the target of the lane's row i
+    static __device__ __forceinline__ int64_t target(const Vectors& v, const Place& p, int i) {
+        const int row = p.row + i * 16;
+        return (int64_t)((uint64_t)v.target[1][row] << 32 | v.target[0][row]);
+    }
+    // which of the lane's COLS classes it is, or something else (a negative target is
+    // before every class)
+    static __device__ __forceinline__ int hot(const Logits& l, const Place& p, int64_t y) {
+        const int64_t at = y - l.first - p.tile.n - p.first;
+        return at >= 0 && at < COLS ? (int)at : -1;
     }
 
     // Each row's largest logit and sum of exp's over the tile's classes, and its target's
-    // logit where the tile has it.
+    // logit where the tile has it, all as powers of two: logits are scaled by log2 e with
+    // x_scale, which saves a product each (and one more rounding of a row's scale is
+    // well below the roundings of its logits' sum).
     static __device__ __forceinline__ void stats(const Logits& l, Stats* part, float* hit,
                                                  int64_t tiles_m, int64_t tiles_n,
                                                  int64_t first_tile) {
-        __shared__ __attribute__((aligned(1024))) char lds[kLds];
+        __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
+        Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
+        send(l, nullptr, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
-        Stats of[MT];
-        for_rows(l, p, acc, [&](int i, int64_t m, const float(&z)[COLS], int hot, float,
-                                const float(&)[COLS], int64_t) {
+        float ws[COLS];
+#pragma unroll
+        for (int k = 0; k < COLS; ++k) ws[k] = v.w_scale[p.first + k];
+        const bool whole = p.tile.n + TILE <= l.o.N;
+        const int64_t n0 = p.tile.n + p.first;
+        auto* words = reinterpret_cast<Stats(*)[TILE]>(lds);  // [WN][TILE]
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const float xs = v.x_scale[p.row + i * 16] * kLog2e;
+            float z[COLS];
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) z[k] = (float)acc[i][k / 4][k % 4] * xs * ws[k];
+            if (!whole) {
+#pragma unroll
+                for (int k = 0; k < COLS; ++k) z[k] = n0 + k < l.o.N ? z[k] : -__builtin_inff();
+            }
             // a lane's classes against their own largest: the lanes' sums are joined after
-            // that, at two exp's a row and not a maximum over the lanes first
+            // that, at two powers a row and not a maximum over the lanes first
             float top = z[0];
 #pragma unroll
             for (int k = 1; k < COLS; ++k) top = fmaxf(top, z[k]);
             const float q = pivot(top);
-            float sum = 0.0f;
+            float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int k = 0; k < COLS; ++k) sum += exp_of(z[k] - q);
-            of[i] = {top, sum};
-            if (__any(hot >= 0)) {
+            for (int k = 0; k < COLS; ++k) sum[k % 2] += __builtin_amdgcn_exp2f(z[k] - q);
+            const int at = hot(l, p, target(v, p, i));
+            const int64_t m = p.tile.m + p.row + i * 16;
+            if (__any(at >= 0)) {
 #pragma unroll
                 for (int k = 0; k < COLS; ++k)
-                    if (k == hot && m < l.o.M) hit[m] = z[k];
+                    if (k == at && m < l.o.M && n0 + k < l.o.N) hit[m] = z[k];
             }
-        });
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
+            Stats s = {top, sum[0] + sum[1]};
 #pragma unroll
             for (int off = 16; off < 64; off <<= 1)
-                of[i] = join(of[i], {__shfl_xor(of[i].top, off), __shfl_xor(of[i].sum, off)});
-        __syncthreads();
-        auto* words = reinterpret_cast<Stats(*)[BM]>(lds);  // [WN][BM]
-        if (p.g == 0) {
-#pragma unroll
-            for (int i = 0; i < MT; ++i) words[p.wn][(p.wm * MT + i) * 16 + p.r] = of[i];
+                s = join(s, {__shfl_xor(s.top, off), __shfl_xor(s.sum, off)});
+            if (p.g == 0) words[p.wn][p.row + i * 16] = s;
         }
         __syncthreads();
-        if ((int)threadIdx.x >= BM) return;
+        if ((int)threadIdx.x >= TILE) return;
         Stats s = words[0][threadIdx.x];
 #pragma unroll
         for (int w = 1; w < WN; ++w) s = join(s, words[w][threadIdx.x]);
         const int64_t m = p.tile.m + threadIdx.x;
-        if (m < l.o.M) part[(first_tile + p.tile.n / BN) * l.o.M + m] = s;
+        if (m < l.o.M) part[(first_tile + p.tile.n / TILE) * l.o.M + m] = s;
     }
 
     // The gradient of the logits, times g, twice: by rows, each class scaled by w_scale, for
@@ -185,113 +214,136 @@ struct LogitTile {
     template <int PX, int PW>
     static __device__ __forceinline__ void grads(const Logits& l, const Slopes& to,
                                                  int64_t tiles_m, int64_t tiles_n) {
-        __shared__ __attribute__((aligned(1024))) char lds[kLds];
+        __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
+        Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
+        send(l, &to, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
-        // the wavefront's own rows and classes, to be turned
-        constexpr int kRow = NT * 32;  // bytes
-        static_assert(G::kWaves * MT * 16 * kRow <= kLds, "room to turn a part");
-        char* room = lds + p.wave * MT * 16 * kRow;
-        float turn[MT][COLS];  // (in the sums' place)
-        for_rows(l, p, acc, [&](int i, int64_t m, const float(&z)[COLS], int hot, float xs,
-                                const float(&ws)[COLS], int64_t y) {
-            const int64_t at = m < l.o.M ? m : l.o.M - 1;
-            const float lse = y >= to.classes ? __builtin_nanf("") : to.lse[at], g = to.g[at];
-            float e[COLS];
+        const int64_t n0 = p.tile.n + p.first;
+        float ws[COLS];
 #pragma unroll
-            for (int k = 0; k < COLS; ++k) e[k] = exp_of(z[k] - lse);
-            if (__any(hot >= 0)) {
+        for (int k = 0; k < COLS; ++k) ws[k] = v.w_scale[p.first + k];
+        float turn[PW > 0 ? MT : 1][COLS];  // (in the sums' place)
 #pragma unroll
-                for (int k = 0; k < COLS; ++k) e[k] = k == hot ? e[k] - 1.0f : e[k];
+        for (int i = 0; i < MT; ++i) {
+            const int row = p.row + i * 16;
+            const int64_t y = target(v, p, i), m = p.tile.m + row;
+            const int at = hot(l, p, y);
+            const float xs = v.x_scale[row], g = v.g[row];
+            const float lse = y >= to.classes ? __builtin_nanf("") : v.lse[row];
+            float e[COLS], t[COLS];
+#pragma unroll
+            for (int k = 0; k < COLS; ++k)
+                e[k] = exp_of((float)acc[i][k / 4][k % 4] * xs * ws[k] - lse);
+            if (__any(at >= 0)) {
+#pragma unroll
+                for (int k = 0; k < COLS; ++k) e[k] = k == at ? e[k] - 1.0f : e[k];
             }
 #pragma unroll
             for (int k = 0; k < COLS; ++k) {
                 e[k] *= g;
-                turn[i][k] = e[k] * xs;
+                t[k] = e[k] * xs;
                 e[k] *= ws[k];
             }
             const bool counts = y >= 0 && m < l.o.M;
-            if (__any(!counts) || p.tile.n + BN > l.o.N) {
+            if (__any(!counts) || p.tile.n + TILE > l.o.N) {
                 // what is not there is 0, whatever was computed for it
 #pragma unroll
                 for (int k = 0; k < COLS; ++k) {
-                    const bool there = counts && p.n0 + k < l.o.N;
-                    turn[i][k] = there ? turn[i][k] : 0.0f;
+                    const bool there = counts && n0 + k < l.o.N;
+                    t[k] = there ? t[k] : 0.0f;
                     e[k] = there ? e[k] : 0.0f;
                 }
             }
-            const int64_t m0 = p.tile.m + (p.wm * MT + i) * 16, c0 = p.tile.n + p.wn * NT * 16;
+            if constexpr (PW > 0) {
 #pragma unroll
-            for (int q = 0; q < PX; ++q) {
-                u32x4 v[COLS / 8];
-#pragma unroll
-                for (int k = 0; k < COLS; k += 2)
-                    v[k / 8][k % 8 / 2] =
-                        q + 1 < PX ? take2(e[k], e[k + 1]) : narrow2(e[k], e[k + 1]);
-                store_turned(v, to.by_row + q * to.row_part + m0 * to.row_ld + c0, to.row_ld,
-                             l.o.M - m0, to.row_ld - c0, p.r, p.g);
+                for (int k = 0; k < COLS; ++k) turn[i][k] = t[k];
             }
-        });
+            if constexpr (PX > 0) {
+                const int64_t m0 = m - p.r, c0 = p.tile.n + p.wn * NT * 16;
+                const bool finite = is_finite<PX>(e);
+#pragma unroll
+                for (int q = 0; q < PX; ++q) {
+                    u32x4 x[COLS / 8];
+#pragma unroll
+                    for (int k = 0; k < COLS; k += 2)
+                        x[k / 8][k % 8 / 2] = take2<PX>(q, e[k], e[k + 1], finite);
+                    if (c0 < to.row_ld)
+                        store_whole(x, to.by_row + q * to.row_part + m0 * to.row_ld + c0,
+                                    to.row_ld, l.o.M - m0, p);
+                }
+            }
+        }
         if constexpr (PW > 0) {
-            __syncthreads();  // (all have read the last step)
+            // The wavefront's rows go into LDS, of which it has a part to itself and whose
+            // reads and writes are done in order, their 16-byte pieces exchanged so that
+            // the 16 lanes of a piece touch all banks.
+            constexpr int kRow = NT * 32;  // bytes
+            static_assert(kWaves * MT * 16 * kRow <= kBuffers, "room to turn a part");
+            char* room = lds + p.wave * MT * 16 * kRow;
+            bool finite = true;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) finite = finite && is_finite<PW>(turn[i]);
 #pragma unroll
             for (int q = 0; q < PW; ++q) {
-                // rows of the tile into LDS, their 16-byte pieces exchanged so that the 16
-                // lanes of a row's piece touch all banks
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
                     for (int j = 0; j < COLS / 8; ++j) {
-                        u32x4 v;
+                        u32x4 x;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            float &a = turn[i][8 * j + 2 * k], &b = turn[i][8 * j + 2 * k + 1];
-                            v[k] = q + 1 < PW ? take2(a, b) : narrow2(a, b);
-                        }
+                        for (int k = 0; k < 4; ++k)
+                            x[k] = take2<PW>(q, turn[i][8 * j + 2 * k], turn[i][8 * j + 2 * k + 1],
+                                             finite);
                         const int at = i * 16 + p.r, piece = p.g * (COLS / 8) + j;
-                        *reinterpret_cast<u32x4*>(room + at * kRow + ((piece ^ swap(at)) << 4)) = v;
+                        *reinterpret_cast<u32x4*>(room + at * kRow + ((piece ^ swap(at)) << 4)) = x;
                     }
-                __syncthreads();
-                // and out of it by classes: 16 lanes read 4 rows of 16 classes, and each gets
-                // one class' 4 rows; two reads are 8 rows, 16 bytes
-#pragma unroll
-                for (int c = 0; c < NT; ++c)
-#pragma unroll
-                    for (int i = 0; i < MT / 2; ++i) {
-                        const int at = i * 32 + p.g * 8;
-                        const u32x2 lo = turned(room, at, c, p.r);
-                        const u32x2 hi = turned(room, at + 4, c, p.r);
-                        const int64_t v = p.tile.n + (p.wn * NT + c) * 16 + p.r;
-                        const int64_t t = p.tile.m + p.wm * MT * 16 + at;
-                        if (v < l.o.N && t < to.class_ld)
-                            *reinterpret_cast<u32x4*>(to.by_class + q * to.class_part +
-                                                      v * to.class_ld + t) =
-                                u32x4{lo[0], lo[1], hi[0], hi[1]};
-                    }
-                if (q + 1 < PW) __syncthreads();
+                asm volatile("" ::: "memory");
+                by_classes(l, to, p, room, to.by_class + q * to.class_part);
+                asm volatile("" ::: "memory");
             }
         }
     }
-    // The first of the parts that a and b are still to be held in (see split), which is
-    // taken off them.
-    static __device__ __forceinline__ uint32_t take2(float& a, float& b) {
-        uint32_t v = narrow2(a, b);
-        float x[2] = {a, b};
+
+    // Stores a part by classes.  16 lanes read 4 rows of 16 classes, and each gets one
+    // class' 4 rows; two reads are 8 rows, 16 bytes.  With 64 rows, the lanes exchange
+    // pieces (see Turn), so that a store covers 128 bytes of 8 classes and not 64 of 16.
+    static __device__ __forceinline__ void by_classes(const Logits& l, const Slopes& to,
+                                                      const Place& p, const char* room,
+                                                      uint16_t* out) {
+        constexpr int PIECES = MT % 4 == 0 ? 2 : 1;
+        const int64_t t0 = p.tile.m + p.wm * MT * 16;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            uint32_t bits = k == 0 ? v << 16 : v & 0xffff0000u;
-            const bool finite = magnitude(x[k]) < 0x7f800000u;
-            // a number past the largest bf16 keeps its first bits
-            if (finite && (bits & 0x7f800000u) == 0x7f800000u) {
-                bits = __float_as_uint(x[k]) & 0xffff0000u;
-                v = k == 0 ? (v & 0xffff0000u) | bits >> 16 : (v & 0xffffu) | bits;
+        for (int c = 0; c < NT; ++c) {
+            const int64_t v0 = p.tile.n + (p.wn * NT + c) * 16;
+#pragma unroll
+            for (int i = 0; i < MT / 2 / PIECES; ++i) {
+                u32x4 x[PIECES];
+#pragma unroll
+                for (int j = 0; j < PIECES; ++j) {
+                    const int at = i * 32 * PIECES + (p.g * PIECES + j) * 8;
+                    const u32x2 lo = turned(room, at, c, p.r), hi = turned(room, at + 4, c, p.r);
+                    x[j] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                }
+                const int64_t t = t0 + i * 32 * PIECES;
+                if (t < to.class_ld)
+                    store_whole(x, out + v0 * to.class_ld + t, to.class_ld, l.o.N - v0, p);
             }
-            x[k] = finite ? x[k] - __uint_as_float(bits) : 0.0f;
         }
-        a = x[0];
-        b = x[1];
-        return v;
+    }
+    // store_turned where all of a row's pieces are there: `ld` is whole steps
+    template <int PIECES>
+    static __device__ __forceinline__ void store_whole(u32x4 (&x)[PIECES], uint16_t* c, int64_t ld,
+                                                       int64_t rows, const Place& p) {
+        Turn<PIECES>::run(x, p.r);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int row = Turn<PIECES>::row_of(i, p.r);
+            if (row < rows)
+                *reinterpret_cast<u32x4*>(c + row * ld + Turn<PIECES>::place_of(p.g, p.r) * 8) =
+                    x[i];
+        }
     }
     static __device__ __forceinline__ int swap(int row) {
         return NT == 4 ? (row >> 1) & 7 : (row >> 1) & 3;
@@ -303,19 +355,47 @@ struct LogitTile {
         return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                              (__attribute__((address_space(3))) i16x4*)(from)));
     }
+
+    // Whether none of the wavefront's numbers is an infinity (asked for numbers that are
+    // to be taken apart).
+    template <int P>
+    static __device__ __forceinline__ bool is_finite(const float (&x)[COLS]) {
+        if constexpr (P == 1) return true;
+        float most = 0.0f;
+#pragma unroll
+        for (int k = 0; k < COLS; ++k) most = fmaxf(most, fabsf(x[k]));
+        return !__any(most == __builtin_inff());
+    }
+    // Part q of P of two numbers, which is taken off them: the 24 bits of one are three times
+    // 8, so the first two parts are its first bits as they are, the last is the rest.  With
+    // one part, it is rounded.  A NaN's first bits are one; nothing is left of an infinity.
+    template <int P>
+    static __device__ __forceinline__ uint32_t take2(int q, float& a, float& b, bool finite) {
+        static_assert(P == 1 || P == 3, "rounded, or exactly");
+        if constexpr (P == 1) return narrow2(a, b);
+        const uint32_t u = __float_as_uint(a), w = __float_as_uint(b);
+        if (q + 1 < P) {
+            a -= __uint_as_float(u & 0xffff0000u);
+            b -= __uint_as_float(w & 0xffff0000u);
+            if (!finite) {
+                a = magnitude(__uint_as_float(u)) == 0x7f800000u ? 0.0f : a;
+                b = magnitude(__uint_as_float(w)) == 0x7f800000u ? 0.0f : b;
+            }
+        }
+        return __builtin_amdgcn_perm(w, u, 0x07060302u);
+    }
 };
 
-template <int BM, int BN, int WM, int WN, int S>
-__global__ __launch_bounds__(64 * WM * WN) void xent_stats_kernel(Logits l, Stats* part, float* hit,
-                                                                  int64_t tiles_m, int64_t tiles_n,
-                                                                  int64_t first_tile) {
-    LogitTile<BM, BN, WM, WN, S>::stats(l, part, hit, tiles_m, tiles_n, first_tile);
+template <int TILE, int WN, int S>
+__global__ __launch_bounds__(128 * WN) void xent_stats_kernel(Logits l, Stats* part, float* hit,
+                                                              int64_t tiles_m, int64_t tiles_n,
+                                                              int64_t first_tile) {
+    LogitTile<TILE, WN, S>::stats(l, part, hit, tiles_m, tiles_n, first_tile);
 }
-template <int BM, int BN, int WM, int WN, int S, int PX, int PW>
-__global__ __launch_bounds__(64 * WM * WN) void xent_slopes_kernel(Logits l, Slopes to,
-                                                                   int64_t tiles_m,
-                                                                   int64_t tiles_n) {
-    LogitTile<BM, BN, WM, WN, S>::template grads<PX, PW>(l, to, tiles_m, tiles_n);
+template <int TILE, int WN, int S, int PX, int PW>
+__global__ __launch_bounds__(128 * WN) void xent_slopes_kernel(Logits l, Slopes to,
+                                                               int64_t tiles_m, int64_t tiles_n) {
+    LogitTile<TILE, WN, S>::template grads<PX, PW>(l, to, tiles_m, tiles_n);
 }
 
 // Rows and classes of the tile that some logits are made in: 256, 128 or 64.
