@@ -45,7 +45,7 @@ CLIP_SOURCES = ("kernels_clip.hip", "clip_api.cpp")
 Q8_SOURCES = ("q8_rows.hip", "q8_norm.hip", "q8_act.hip", "q8_matmul.hip", "q8_grad.hip",
               "q8_grad_few.hip", "q8_api.cpp")
 # the loss on that path (in the same library)
-XENT_SOURCES = ("q8_xent.hip", "q8_xent_api.cpp")
+XENT_SOURCES = ("q8_xent.hip", "q8_xent_few.hip", "q8_xent_api.cpp")
 OBJ_ROOT = os.path.join(ROOT, "_build")
 
 

@@ -1,14 +1,11 @@
 // Softmax cross entropy of 8-bit rows over the classes of 8-bit weights, and its
 // gradients, without the logits being kept.
 //
-// More than 64 tokens: tiles of the product of rows and weights whose results are used
+// More than 64 tokens (fewer: q8_xent_few.hip): tiles of the product of rows and weights whose results are used
 // where they are made (q8_xent_tile.h).  The loss takes one launch over all tiles and
 // one that joins what they found of each token.  Its gradients make the logits again, a
 // piece of the classes at a time, and leave the gradient of them laid out for two
 // products on the bf16 matrix cores (q8_grad_gemm.h).
-//
-// Up to 64 tokens: the logits are small (a piece of them at most 128 MB), and the
-// kernels of few tokens (q8_matmul.hip, q8_grad_few.hip) read the weights once each.
 #include "q8_grad_layout.h"
 #include "q8_xent_tile.h"
 
@@ -17,22 +14,6 @@ namespace q8 {
 namespace {
 
 constexpr int64_t kFewTokens = 64;
-
-// Takes parts of a workspace, each on a 256-byte boundary.
-struct Room {
-    int64_t bytes = 0;
-    int64_t take(int64_t n) {
-        const int64_t at = bytes;
-        bytes += up(n, 256) * 256;
-        return at;
-    }
-};
-template <class T>
-T* at(void* workspace, int64_t offset) {
-    return reinterpret_cast<T*>(static_cast<char*>(workspace) + offset);
-}
-
-// ---- many tokens ------------------------------------------------------------------
 
 // Joins the tiles' parts of each row's statistics: 16 rows a block, 16 threads a row.
 __global__ __launch_bounds__(256) void xent_join_kernel(const Stats* part, const float* hit,
@@ -57,10 +38,7 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const Stats* part, const
     if (slice != 0 || t >= T) return;
 #pragma unroll
     for (int i = 1; i < 16; ++i) s = join(s, words[i][row]);
-    const float l = s.top + log2f(s.sum);
-    const int64_t y = target[t];
-    lse[t] = l * kLn2;
-    loss[t] = y < 0 ? 0.0f : (l - (y < V ? hit[t] : __builtin_nanf(""))) * kLn2;
+    write_loss(s, hit[t], target[t], V, lse + t, loss + t);
 }
 
 // f(tile) with the tile's size as a compile-time number
@@ -344,205 +322,19 @@ int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, vo
     return 0;
 }
 
-// ---- few tokens -------------------------------------------------------------------
-
-// Classes of a piece: 2^25 logits at most.
-int64_t few_piece(int64_t T, int64_t V) {
-    const int64_t n = ((int64_t)1 << 25) / T / 256 * 256;
-    return n < V ? n : V;
-}
-
-// What is known of a row after some of the pieces.
-struct FewStats {
-    float top, sum, hit;  // maximum, sum of exp(z - top), the target's logit
-};
-
-struct FewRoom : Room {
-    int64_t piece, ld;  // classes of a piece; its logits' row stride
-    int64_t logits, stats, scale, sum, part, product;
-};
-FewRoom few_room(int64_t T, int64_t V, int64_t K, bool bwd, bool dw_bf16) {
-    FewRoom r;
-    r.piece = few_piece(T, V);
-    r.ld = up(r.piece, 16) * 16;
-    r.logits = r.take(T * r.ld * 4);
-    r.stats = r.take(T * (int64_t)sizeof(FewStats));
-    int64_t most = 0;
-    const int64_t last = V - (V - 1) / r.piece * r.piece;
-    for (int i = 0; i < 2; ++i) {
-        const int64_t n = i ? last : r.piece;
-        const int64_t need[] = {matmul_workspace(T, n, K),
-                                bwd ? grad_input_workspace(T, n, K, false, false) : 0,
-                                bwd ? grad_weight_workspace(T, n, K, false, dw_bf16) : 0};
-        for (const int64_t b : need) most = b > most ? b : most;
-    }
-    if (bwd) {
-        r.scale = r.take(T * 4);
-        r.sum = r.take(T * up(K, 16) * 64);
-        r.part = r.take(T * up(K, 16) * 64);
-    }
-    r.product = r.take(most);
-    return r;
-}
-
-struct AddFloats {
-    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
-};
-struct MaxFloats {
-    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
-};
-
-template <class Op>
-__device__ __forceinline__ float over_block(float x, Op op, float* words) {
-    x = wave_reduce(x, op);
-    if (threadIdx.x % 64 == 0) words[threadIdx.x / 64] = x;
-    __syncthreads();
-    x = words[0];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) x = op(x, words[w]);
-    return x;
-}
-
-// A block takes a row of a piece's logits.
-__global__ __launch_bounds__(256) void xent_few_stats_kernel(const float* z, int64_t ld,
-                                                             int64_t v0, int n,
-                                                             const int64_t* target,
-                                                             FewStats* stats, int first, int last,
-                                                             float* loss, float* lse) {
-    __shared__ float words[2][4];
-    const int64_t t = blockIdx.x;
-    const float* row = z + t * ld;
-    float top = -__builtin_inff();
-    for (int v = threadIdx.x; v < n; v += 256) top = fmaxf(top, row[v]);
-    top = over_block(top, MaxFloats(), words[0]);
-    const float q = pivot(top);
-    float sum = 0.0f;
-    for (int v = threadIdx.x; v < n; v += 256) sum += exp_of(row[v] - q);
-    top *= kLog2e;
-    sum = over_block(sum, AddFloats(), words[1]);
-    if (threadIdx.x != 0) return;
-    FewStats s = {-__builtin_inff(), 0.0f, __builtin_nanf("")};
-    if (!first) s = stats[t];
-    const Stats both = join({s.top, s.sum}, {top, sum});
-    s.sum = both.sum;
-    s.top = both.top;
-    const int64_t at = target[t] - v0;
-    if (at >= 0 && at < n) s.hit = row[at];
-    stats[t] = s;
-    if (last) {
-        const float l = s.top + log2f(s.sum);
-        lse[t] = l * kLn2;
-        loss[t] = target[t] < 0 ? 0.0f : (l - s.hit * kLog2e) * kLn2;
-    }
-}
-
-// The logits' gradient takes the logits' place.  Rows that do not count have none.
-__global__ __launch_bounds__(256) void xent_few_slopes_kernel(float* z, int64_t ld, int64_t v0,
-                                                              int n, int64_t V,
-                                                              const int64_t* target,
-                                                              const float* lse, const float* g) {
-    const int64_t t = blockIdx.x;
-    const int64_t y = target[t];
-    const float l = y >= V ? __builtin_nanf("") : lse[t], f = g[t];
-    for (int v = threadIdx.x; v < n; v += 256) {
-        float* p = z + t * ld + v;
-        const float d = f * (exp_of(*p - l) - (v0 + v == y ? 1.0f : 0.0f));
-        *p = y < 0 ? 0.0f : d;
-    }
-}
-
-__global__ __launch_bounds__(256) void xent_scale_kernel(const float* scale, const int64_t* target,
-                                                         int64_t T, float* out) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t < T) out[t] = target[t] < 0 ? 0.0f : scale[t];
-}
-
-// sum <- sum + part, to dx after the last piece
-__global__ __launch_bounds__(256) void xent_few_add_kernel(float* sum, const float* part,
-                                                           int64_t ld, int64_t K,
-                                                           const int64_t* target, int first,
-                                                           int last, Target out) {
-    const int64_t t = blockIdx.x;
-    for (int64_t k = threadIdx.x; k < K; k += 256) {
-        const int64_t i = t * ld + k;
-        const float x = target[t] < 0 ? 0.0f : first ? part[i] : sum[i] + part[i];
-        if (!last) sum[i] = x;
-        else if (out.bf16) narrow(x, static_cast<uint16_t*>(out.c) + t * out.ldc + k);
-        else static_cast<float*>(out.c)[t * out.ldc + k] = x;
-    }
-}
-
-int few_forward(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
-    const FewRoom r = few_room(l.T, l.V, l.K, false, false);
-    auto* z = at<float>(ws, r.logits);
-    for (int64_t v = 0; v < l.V; v += r.piece) {
-        const int64_t n = l.V - v < r.piece ? l.V - v : r.piece;
-        const Held w{l.w.q + v * l.w.ld, l.w.ld, l.w.scale + v};
-        if (int e = launch_matmul(l.x, w, l.T, n, l.K, Mat{z, r.ld, false},
-                                  at<char>(ws, r.product), stream))
-            return e;
-        if (int e = launch(xent_few_stats_kernel, dim3((uint32_t)l.T), 256, stream, z, r.ld, v,
-                           (int)n, l.target, at<FewStats>(ws, r.stats), (int)(v == 0),
-                           (int)(v + n == l.V), loss, lse))
-            return e;
-    }
-    return 0;
-}
-
-int few_backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, void* ws,
-                 void* stream) {
-    const FewRoom r = few_room(l.T, l.V, l.K, true, dw.bf16);
-    auto* z = at<float>(ws, r.logits);
-    auto* scale = at<float>(ws, r.scale);
-    char* room = at<char>(ws, r.product);
-    const int64_t ld = up(l.K, 16) * 16;
-    if (int e = launch(xent_scale_kernel, dim3((uint32_t)up(l.T, 256)), 256, stream, l.x.scale,
-                       l.target, l.T, scale))
-        return e;
-    for (int64_t v = 0; v < l.V; v += r.piece) {
-        const int64_t n = l.V - v < r.piece ? l.V - v : r.piece;
-        const Held w{l.w.q + v * l.w.ld, l.w.ld, l.w.scale + v};
-        const Mat d{z, r.ld, false};
-        if (int e = launch_matmul(l.x, w, l.T, n, l.K, d, room, stream)) return e;
-        if (int e = launch(xent_few_slopes_kernel, dim3((uint32_t)l.T), 256, stream, z, r.ld, v,
-                           (int)n, l.V, l.target, lse, g))
-            return e;
-        if (dx.p != nullptr) {
-            const Mat part{at<float>(ws, r.part), ld, false};
-            if (int e = launch_grad_input(d, w, l.T, n, l.K, part, room, stream)) return e;
-            Target out{};
-            out.c = dx.p;
-            out.ldc = dx.ld;
-            out.bf16 = dx.bf16;
-            if (int e = launch(xent_few_add_kernel, dim3((uint32_t)l.T), 256, stream,
-                               at<float>(ws, r.sum), at<float>(ws, r.part), ld, l.K, l.target,
-                               (int)(v == 0), (int)(v + n == l.V), out))
-                return e;
-        }
-        if (dw.p != nullptr) {
-            const Mat part{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4), dw.ld,
-                           dw.bf16};
-            if (int e = launch_grad_weight(d, Held{l.x.q, l.x.ld, scale}, l.T, n, l.K, part, room,
-                                           stream))
-                return e;
-        }
-    }
-    return 0;
-}
-
 }  // namespace
 
 int64_t xent_workspace(int64_t T, int64_t V, int64_t K) {
-    return T <= kFewTokens ? few_room(T, V, K, false, false).bytes : forward_room(T, V, K).bytes;
+    return T <= kFewTokens ? few_xent_workspace(T, V, K) : forward_room(T, V, K).bytes;
 }
 
 int launch_xent(const Loss& l, float* loss, float* lse, void* workspace, void* stream) {
-    return l.T <= kFewTokens ? few_forward(l, loss, lse, workspace, stream)
+    return l.T <= kFewTokens ? launch_few_xent(l, loss, lse, workspace, stream)
                              : forward(l, loss, lse, workspace, stream);
 }
 
 int64_t xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
-    return T <= kFewTokens ? few_room(T, V, K, true, dw_bf16).bytes
+    return T <= kFewTokens ? few_xent_bwd_workspace(T, V, K, dx_bf16, dw_bf16)
                            : backward_room(T, V, K, dx_bf16, dw_bf16).bytes;
 }
 
@@ -551,7 +343,7 @@ int launch_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx, Mat
     // a sum over no tokens
     if (l.T == 0)
         return launch_grad_weight(Mat{nullptr, 0, false}, l.x, 0, l.V, l.K, dw, workspace, stream);
-    return l.T <= kFewTokens ? few_backward(l, lse, g, dx, dw, workspace, stream)
+    return l.T <= kFewTokens ? launch_few_xent_bwd(l, lse, g, dx, dw, workspace, stream)
                              : backward(l, lse, g, dx, dw, workspace, stream);
 }
 

@@ -21,5 +21,12 @@ int64_t xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
 int launch_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw,
                     void* workspace, void* stream);
 
+// The same for up to 64 tokens (q8_xent_few.hip).
+int64_t few_xent_workspace(int64_t T, int64_t V, int64_t K);
+int launch_few_xent(const Loss& l, float* loss, float* lse, void* workspace, void* stream);
+int64_t few_xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16);
+int launch_few_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw,
+                        void* workspace, void* stream);
+
 }  // namespace q8
 }  // namespace cpdp

@@ -7,7 +7,7 @@
 #pragma once
 
 #include "q8_grad_gemm.h"
-#include "q8_xent_launch.h"
+#include "q8_xent_stats.h"
 
 namespace cpdp {
 namespace q8 {
@@ -31,27 +31,6 @@ struct Slopes {
     const float* g;
     int64_t classes;  // of the loss
 };
-
-// What is known of a row's logits, in units of log 2 (as powers of two), after some of the
-// classes: the largest, and the sum of 2^(z - top).
-struct Stats {
-    float top, sum;
-};
-
-constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
-
-// exp(x) for x <= 0 or NaN, as 2^(x log2 e): v_exp is within a unit of the last place,
-// what its argument's rounding adds is |x| 2^-24 at most.  Results below 2^-126 are 0.
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-
-// `top` to subtract: with nothing but -infinities, 0 (their powers are then 0)
-__device__ __forceinline__ float pivot(float top) { return top == -__builtin_inff() ? 0.0f : top; }
-
-__device__ __forceinline__ Stats join(Stats a, Stats b) {
-    const float top = fmaxf(a.top, b.top), p = pivot(top);
-    return {top, a.sum * __builtin_amdgcn_exp2f(a.top - p) +
-                     b.sum * __builtin_amdgcn_exp2f(b.top - p)};
-}
 
 // Tiles of TILE rows and classes by 2 x WN wavefronts, with S LDS buffers.
 template <int TILE, int WN, int S>
@@ -149,9 +128,7 @@ struct LogitTile {
     }
 
     // Each row's largest logit and sum of exp's over the tile's classes, and its target's
-    // logit where the tile has it, all as powers of two: logits are scaled by log2 e with
-    // x_scale, which saves a product each (and one more rounding of a row's scale is
-    // well below the roundings of its logits' sum).
+    // logit where the tile has it.
     static __device__ __forceinline__ void stats(const Logits& l, Stats* part, float* hit,
                                                  int64_t tiles_m, int64_t tiles_n,
                                                  int64_t first_tile) {
@@ -169,7 +146,7 @@ struct LogitTile {
         auto* words = reinterpret_cast<Stats(*)[TILE]>(lds);  // [WN][TILE]
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const float xs = v.x_scale[p.row + i * 16] * kLog2e;
+            const float xs = v.x_scale[p.row + i * 16];
             float z[COLS];
 #pragma unroll
             for (int k = 0; k < COLS; ++k) z[k] = (float)acc[i][k / 4][k % 4] * xs * ws[k];
@@ -178,14 +155,14 @@ struct LogitTile {
                 for (int k = 0; k < COLS; ++k) z[k] = n0 + k < l.o.N ? z[k] : -__builtin_inff();
             }
             // a lane's classes against their own largest: the lanes' sums are joined after
-            // that, at two powers a row and not a maximum over the lanes first
+            // that, at two exp's a row and not a maximum over the lanes first
             float top = z[0];
 #pragma unroll
             for (int k = 1; k < COLS; ++k) top = fmaxf(top, z[k]);
             const float q = pivot(top);
             float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int k = 0; k < COLS; ++k) sum[k % 2] += __builtin_amdgcn_exp2f(z[k] - q);
+            for (int k = 0; k < COLS; ++k) sum[k % 2] += exp_of(z[k] - q);
             const int at = hot(l, p, target(v, p, i));
             const int64_t m = p.tile.m + p.row + i * 16;
             if (__any(at >= 0)) {
