@@ -7,7 +7,7 @@ namespace cpdp {
 namespace q8 {
 namespace {
 
-// For M <= 16 MT tokens.  A block takes 16 channels, from n0 on; its wavefronts take
+// For M <= 16 MT tokens, U steps of a wavefront on their way together.  A block takes 16 channels, from n0 on; its wavefronts take
 // the steps of K in turn, each lane 32 consecutive bytes of a weight row, so a
 // step reads 128 bytes of 16 rows.  Those go to the matrix cores as they are: a
 // sum does not depend on which of its terms an instruction takes together, as
@@ -16,7 +16,7 @@ namespace {
 // has element e, of token e / 16 and channel e % 16, at [e / 4][e % 4].
 template <int MT>
 using FewSums = i32x4[16][MT * 64];
-template <int MT>
+template <int MT, int U>
 __device__ __forceinline__ void few_sums(const int8_t* a, int64_t lda, const int8_t* b,
                                          int64_t ldb, int M, int64_t N, int K, int64_t n0,
                                          FewSums<MT>& sums) {
@@ -29,8 +29,6 @@ __device__ __forceinline__ void few_sums(const int8_t* a, int64_t lda, const int
         ap[i] = reinterpret_cast<const char*>(a) + (i * 16 + r < M ? i * 16 + r : M - 1) * lda +
                 g * 32;
     i32x4 acc[MT] = {};
-    // U steps are on their way together
-    constexpr int U = MT == 1 ? 4 : 2;
     const int steps = K / kStep;
     for (int k = wave; k < steps; k += waves * U) {
         u32x4 w[U][2], x[U][MT][2];

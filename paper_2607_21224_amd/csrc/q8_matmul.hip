@@ -16,7 +16,7 @@ __global__ __launch_bounds__(1024) void few_kernel(const int8_t* a, int64_t lda,
     __shared__ FewSums<MT> sums;
     const int waves = blockDim.x >> 6;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
-    few_sums<MT>(a, lda, b, ldb, M, N, K, n0, sums);
+    few_sums<MT, MT == 1 ? 4 : 2>(a, lda, b, ldb, M, N, K, n0, sums);
     // element e: token e / 16, channel e % 16
     for (int e = threadIdx.x; e < MT * 256; e += blockDim.x) {
         const int m = e / 16;

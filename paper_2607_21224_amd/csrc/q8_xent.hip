@@ -75,17 +75,20 @@ struct ForwardRoom : Room {
 };
 ForwardRoom forward_room(int64_t T, int64_t V, int64_t K) {
     ForwardRoom r;
-    r.tile = logit_tile(T, V, up(K, kStep));
+    r.tile = logit_tile(T, V, up(K, kStep), 3500, 0);
     r.tiles = up(V, r.tile);
-    r.part = r.take(r.tiles * T * (int64_t)sizeof(Stats));
-    r.hit = r.take(T * 4);
+    if (r.tiles > 1) {
+        r.part = r.take(r.tiles * T * (int64_t)sizeof(Stats));
+        r.hit = r.take(T * 4);
+    }
     return r;
 }
 
 int forward(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
     const ForwardRoom r = forward_room(l.T, l.V, l.K);
-    auto* part = at<Stats>(ws, r.part);
-    auto* hit = at<float>(ws, r.hit);
+    const bool one = r.tiles == 1;
+    const Found to{one ? nullptr : at<Stats>(ws, r.part), one ? nullptr : at<float>(ws, r.hit), lse,
+                   loss};
     const int e = with_tile(r.tile, [&](auto tile) {
         const int64_t tm = up(l.T, tile);
         // (a launch holds fewer than 2^32 work items)
@@ -94,26 +97,31 @@ int forward(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
             const int64_t tn = r.tiles - j < most ? r.tiles - j : most, v = j * tile;
             const Logits z = logits_of(l, v, l.V - v < tn * tile ? l.V - v : tn * tile);
             if (int s = launch(xent_stats_kernel<tile, across(tile), buffers(tile)>,
-                               dim3((uint32_t)(tm * tn)), threads(tile), stream, z, part, hit, tm,
-                               tn, j))
+                               dim3((uint32_t)(tm * tn)), threads(tile), stream, z, to, tm, tn, j))
                 return s;
         }
         return 0;
     });
-    if (e) return e;
-    return launch(xent_join_kernel, dim3((uint32_t)up(l.T, 16)), 256, stream, part, hit, l.T,
+    if (e || one) return e;
+    return launch(xent_join_kernel, dim3((uint32_t)up(l.T, 16)), 256, stream, to.part, to.hit, l.T,
                   r.tiles, l.V, l.target, loss, lse);
 }
 
-// An 8-bit operand [R x C] as out [C x pad] in bf16, zeros from R to pad.
-__global__ __launch_bounds__(256) void xent_turn_kernel(Source s) {
+// 8-bit operands [R x C] as out [C x pad] in bf16, zeros from R to pad: two of them in a
+// launch, or one (the other has no blocks).
+__global__ __launch_bounds__(256) void xent_turn_kernel(Source a, Source b) {
     __shared__ Tile<1, tile_cols<int8_t>()> tile;
-    transpose<I8, 1>(s, blockIdx.x, tile);
+    if (blockIdx.x < a.blocks) transpose<I8, 1>(a, blockIdx.x, tile);
+    else transpose<I8, 1>(b, blockIdx.x - (uint32_t)a.blocks, tile);
 }
-int turn(const Held& h, int64_t R, int64_t C, int64_t pad, uint16_t* out, void* stream) {
-    const Source s{h.q, h.ld, nullptr, R, C, out, pad, pad / 64 * up(C, tile_cols<int8_t>())};
-    if (s.blocks * 256 >= (int64_t)1 << 32) return (int)hipErrorInvalidValue;
-    return launch(xent_turn_kernel, dim3((uint32_t)s.blocks), 256, stream, s);
+Source source(const int8_t* q, int64_t ld, int64_t R, int64_t C, int64_t pad, uint16_t* out) {
+    return {q, ld, nullptr, R, C, out, pad, pad / 64 * up(C, tile_cols<int8_t>())};
+}
+int turn(const Source& a, const Source& b, void* stream) {
+    const int64_t blocks = a.blocks + b.blocks;
+    if (blocks == 0) return 0;
+    if (blocks * 256 >= (int64_t)1 << 32) return (int)hipErrorInvalidValue;
+    return launch(xent_turn_kernel, dim3((uint32_t)blocks), 256, stream, a, b);
 }
 
 // Classes of a piece: 2^27 logits' gradients at most (268 MB a part), whole tiles.
@@ -132,8 +140,15 @@ struct BackwardRoom : Room {
 // there are fewer tiles than CUs.  A step of a tile takes what it takes in grad_shape;
 // here the large tiles are cut, too: dx of 4096 x 1024 over 32768 classes has 64 tiles of
 // 256 x 256, and in 4 slices takes 260 us, in 256 tiles of 128 x 128 335.
+// Whether a product is small: tiles that find a CU each, and few steps.  What it takes is
+// mostly its launch, and two of them are made in one (128 x 100 x 384 fp32: two of 4.7 us,
+// BOTH together).
+bool small(int64_t M, int64_t N, int64_t R, int parts) {
+    return up(M, 64) * up(N, 64) <= kCus / 2 && up(R, kRound) * parts <= 24;
+}
 Shape product_shape(int64_t M, int64_t N, int64_t R, int parts) {
     const int64_t steps = up(R, kRound);
+    if (small(M, N, R, parts)) return {64, 64, 1, 0};
     struct {
         int bm, bn, passes, alone, each, end;
     } const tiles[] = {{256, 256, parts, 1800, 1800, 2000},
@@ -185,7 +200,7 @@ BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
 }
 
 template <int P>
-int launch_product(const GradOperands& o, const Target& t, const Shape& s, void* stream) {
+int launch_tiles_of(const GradOperands& o, const Target& t, const Shape& s, void* stream) {
     if (s.bn == 256) return launch_grad_tiles<256, 256, 2, 4, false, false, 1>(o, t, s.slices, stream);
     if constexpr (P == 1)
         if (s.bm == 256)
@@ -196,30 +211,62 @@ int launch_product(const GradOperands& o, const Target& t, const Shape& s, void*
 
 // c [M x N] = the product of A, laid out in parts, and B, laid out, over R values.
 // Without c, the slices (one at least) are left for xent_add_kernel.
-int product(const uint16_t* a, int64_t a_part, const uint16_t* b, int64_t ld, int64_t M,
-            int64_t N, int64_t R, int parts, Mat c, void* slices, void* stream) {
-    GradOperands o{};
-    o.a = reinterpret_cast<const char*>(a);
-    o.lda = o.ldb = ld * 2;
-    o.a_part = a_part * 2;
-    o.b = reinterpret_cast<const char*>(b);
-    o.R = R;
-    o.M = M;
-    o.N = N;
-    o.steps = (int)up(R, kRound);
-    o.parts = parts;
-    Target t{};
-    t.c = c.p != nullptr ? c.p : slices;
-    t.ldc = c.p != nullptr ? c.ld : slices_ld(N);
-    t.bf16 = c.p != nullptr && c.bf16;
-    t.ws = slices;
-    t.ldws = slices_ld(N);
-    t.slice = M * t.ldws;
-    const Shape s = product_shape(M, N, R, parts);
-    if (int e = parts == 1 ? launch_product<1>(o, t, s, stream)
-                           : launch_product<3>(o, t, s, stream))
+struct Product {
+    GradOperands o;
+    Target t;
+    Shape shape;
+    bool join;
+};
+Product product_of(const uint16_t* a, int64_t a_part, const uint16_t* b, int64_t ld, int64_t M,
+                   int64_t N, int64_t R, int parts, Mat c, void* slices) {
+    Product p{};
+    p.o.a = reinterpret_cast<const char*>(a);
+    p.o.lda = p.o.ldb = ld * 2;
+    p.o.a_part = a_part * 2;
+    p.o.b = reinterpret_cast<const char*>(b);
+    p.o.R = R;
+    p.o.M = M;
+    p.o.N = N;
+    p.o.steps = (int)up(R, kRound);
+    p.o.parts = parts;
+    p.t.c = c.p != nullptr ? c.p : slices;
+    p.t.ldc = c.p != nullptr ? c.ld : slices_ld(N);
+    p.t.bf16 = c.p != nullptr && c.bf16;
+    p.t.ws = slices;
+    p.t.ldws = slices_ld(N);
+    p.t.slice = M * p.t.ldws;
+    p.shape = product_shape(M, N, R, parts);
+    p.join = c.p != nullptr && p.shape.slices > 1;
+    return p;
+}
+int launch_product(const Product& p, void* stream) {
+    if (int e = p.o.parts == 1 ? launch_tiles_of<1>(p.o, p.t, p.shape, stream)
+                               : launch_tiles_of<3>(p.o, p.t, p.shape, stream))
         return e;
-    return c.p == nullptr || s.slices == 1 ? 0 : launch_join<Bf16>(t, M, N, s.slices, stream);
+    return p.join ? launch_join<Bf16>(p.t, p.o.M, p.o.N, p.shape.slices, stream) : 0;
+}
+
+// Two small products in one launch, blockIdx.y the one.
+template <int P>
+__global__ __launch_bounds__(256) void xent_both_kernel(GradOperands a, Target to_a,
+                                                        GradOperands b, Target to_b) {
+    const bool second = blockIdx.y != 0;
+    const GradOperands o = second ? b : a;
+    const int64_t tm = (o.M + 63) / 64, tn = (o.N + 63) / 64;
+    if (blockIdx.x >= tm * tn) return;
+    GradGemm<64, 64, 2, 2, false, false, P, 4>::run(o, second ? to_b : to_a, tm, tn, 1);
+}
+// Whether they may be: of as many parts, and small.
+bool both_small(const Product& a, const Product& b) {
+    return a.o.parts == b.o.parts && small(a.o.M, a.o.N, a.o.R, a.o.parts) &&
+           small(b.o.M, b.o.N, b.o.R, b.o.parts);
+}
+int launch_both(const Product& a, const Product& b, void* stream) {
+    const int64_t na = up(a.o.M, 64) * up(a.o.N, 64), nb = up(b.o.M, 64) * up(b.o.N, 64);
+    const dim3 grid((uint32_t)(na > nb ? na : nb), 2);
+    return a.o.parts == 3
+               ? launch(xent_both_kernel<3>, grid, 256, stream, a.o, a.t, b.o, b.t)
+               : launch(xent_both_kernel<1>, grid, 256, stream, a.o, a.t, b.o, b.t);
 }
 
 // sum <- sum and the slices of a piece, to dx after the last piece; 4 columns a thread
@@ -260,7 +307,7 @@ int add(const BackwardRoom& r, void* ws, const Loss& l, int slices, bool first, 
 
 template <int PX, int PW>
 int launch_slopes(const Logits& z, const Slopes& to, int64_t K, void* stream) {
-    return with_tile(logit_tile(z.o.M, z.o.N, up(K, kStep)), [&](auto tile) {
+    return with_tile(logit_tile(z.o.M, z.o.N, up(K, kStep), 0, PX + PW), [&](auto tile) {
         const int64_t tm = up(z.o.M, tile), tn = up(z.o.N, tile);
         if (tm * tn * threads(tile) >= (int64_t)1 << 32) return (int)hipErrorInvalidValue;
         return launch(xent_slopes_kernel<tile, across(tile), buffers(tile), PX, PW>,
@@ -272,8 +319,6 @@ int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, vo
              void* stream) {
     const BackwardRoom r = backward_room(l.T, l.V, l.K, dx.bf16, dw.bf16);
     const bool x = dx.p != nullptr, w = dw.p != nullptr;
-    if (w)
-        if (int e = turn(l.x, l.T, l.K, r.class_ld, at<uint16_t>(ws, r.x), stream)) return e;
     for (int64_t v = 0; v < l.V; v += r.piece) {
         const int64_t n = l.V - v < r.piece ? l.V - v : r.piece;
         const Logits z = logits_of(l, v, n);
@@ -297,27 +342,33 @@ int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, vo
                       : pw == 1 ? launch_slopes<3, 1>(z, to, l.K, stream)
                                 : launch_slopes<3, 3>(z, to, l.K, stream);
         if (e) return e;
+        auto* turned_x = at<uint16_t>(ws, r.x);
+        auto* turned_w = at<uint16_t>(ws, r.w);
+        const Source none{};
+        if (int s = turn(w && v == 0 ? source(l.x.q, l.x.ld, l.T, l.K, r.class_ld, turned_x) : none,
+                         x ? source(l.w.q + v * l.w.ld, l.w.ld, n, l.K, to.row_ld, turned_w) : none,
+                         stream))
+            return s;
         void* slices = at<char>(ws, r.slices);
+        const bool whole = r.piece == l.V;
+        Product of_x{}, of_w{};
+        if (x)
+            of_x = product_of(to.by_row, to.row_part, turned_w, to.row_ld, l.T, l.K, n, px,
+                             whole ? dx : Mat{nullptr, 0, false}, slices);
+        if (w)
+            of_w = product_of(to.by_class, to.class_part, turned_x, r.class_ld, n, l.K, l.T, pw,
+                             Mat{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4), dw.ld,
+                                 dw.bf16},
+                             slices);
+        if (x && w && whole && both_small(of_x, of_w)) return launch_both(of_x, of_w, stream);
         if (x) {
-            auto* turned = at<uint16_t>(ws, r.w);
-            const bool whole = r.piece == l.V;
-            const Held held{l.w.q + v * l.w.ld, l.w.ld, nullptr};
-            if (int s = turn(held, n, l.K, to.row_ld, turned, stream)) return s;
-            if (int s = product(to.by_row, to.row_part, turned, to.row_ld, l.T, l.K, n, px,
-                                whole ? dx : Mat{nullptr, 0, false}, slices, stream))
-                return s;
+            if (int s = launch_product(of_x, stream)) return s;
             if (!whole)
-                if (int s = add(r, ws, l, product_shape(l.T, l.K, n, px).slices, v == 0,
-                                v + n == l.V, dx, stream))
+                if (int s = add(r, ws, l, of_x.shape.slices, v == 0, v + n == l.V, dx, stream))
                     return s;
         }
-        if (w) {
-            const Mat part{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4), dw.ld,
-                           dw.bf16};
-            if (int s = product(to.by_class, to.class_part, at<uint16_t>(ws, r.x), r.class_ld, n,
-                                l.K, l.T, pw, part, slices, stream))
-                return s;
-        }
+        if (w)
+            if (int s = launch_product(of_w, stream)) return s;
     }
     return 0;
 }

@@ -13,7 +13,7 @@ constexpr int kClasses = 16;  // of a block (see few_sums)
 // A block's classes: each token's largest logit and sum of exp's, part [token][block], and
 // the target's logit of the tokens that have it here.
 template <int MT>
-__global__ __launch_bounds__(1024) void xent_few_stats_kernel(Held x, Held w,
+__global__ __launch_bounds__(1024, MT == 1 ? 8 : 4) void xent_few_stats_kernel(Held x, Held w,
                                                               const int64_t* target, int M,
                                                               int64_t V, int K, int64_t first,
                                                               int64_t blocks, Stats* part,
@@ -21,7 +21,7 @@ __global__ __launch_bounds__(1024) void xent_few_stats_kernel(Held x, Held w,
     __shared__ FewSums<MT> sums;
     const int waves = blockDim.x >> 6;
     const int64_t block = first + blockIdx.x, n0 = block * kClasses;
-    few_sums<MT>(x.q, x.ld, w.q, w.ld, M, V, K, n0, sums);
+    few_sums<MT, 2>(x.q, x.ld, w.q, w.ld, M, V, K, n0, sums);
     const int64_t n = n0 + threadIdx.x % kClasses, from = n < V ? n : V - 1;
     const float ws = w.scale[from];
     for (int e = threadIdx.x; e < MT * 256; e += blockDim.x) {
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(1024) void xent_few_slopes_kernel(Held x, Held w,
     __shared__ FewSums<MT> sums;
     const int waves = blockDim.x >> 6;
     const int64_t n0 = (int64_t)blockIdx.x * kClasses;
-    few_sums<MT>(x.q, x.ld, w.q, w.ld, M, N, K, n0, sums);
+    few_sums<MT, 2>(x.q, x.ld, w.q, w.ld, M, N, K, n0, sums);
     if (blockIdx.x == 0 && (int)threadIdx.x < M)
         scale[threadIdx.x] = target[threadIdx.x] < 0 ? 0.0f : x.scale[threadIdx.x];
     const int64_t n = n0 + threadIdx.x % kClasses;

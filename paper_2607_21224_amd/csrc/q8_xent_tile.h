@@ -32,6 +32,15 @@ struct Slopes {
     int64_t classes;  // of the loss
 };
 
+// Where a tile's findings go: its part of each row's statistics [tile][row] and the
+// targets' logits; or, without parts, the loss.
+struct Found {
+    Stats* part;
+    float* hit;
+    float* lse;
+    float* loss;
+};
+
 // Tiles of TILE rows and classes by 2 x WN wavefronts, with S LDS buffers.
 template <int TILE, int WN, int S>
 struct LogitTile {
@@ -115,9 +124,8 @@ struct LogitTile {
         barrier();
     }
 
-    // the target of the lane's row i
-    static __device__ __forceinline__ int64_t target(const Vectors& v, const Place& p, int i) {
-        const int row = p.row + i * 16;
+    // the target of a row of the tile
+    static __device__ __forceinline__ int64_t target(const Vectors& v, int row) {
         return (int64_t)((uint64_t)v.target[1][row] << 32 | v.target[0][row]);
     }
     // which of the lane's COLS classes it is, or something else (a negative target is
@@ -128,10 +136,9 @@ struct LogitTile {
     }
 
     // Each row's largest logit and sum of exp's over the tile's classes, and its target's
-    // logit where the tile has it.
-    static __device__ __forceinline__ void stats(const Logits& l, Stats* part, float* hit,
-                                                 int64_t tiles_m, int64_t tiles_n,
-                                                 int64_t first_tile) {
+    // logit where the tile has it; the loss, if these are all the classes.
+    static __device__ __forceinline__ void stats(const Logits& l, const Found& to, int64_t tiles_m,
+                                                 int64_t tiles_n, int64_t first_tile) {
         __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
         Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
@@ -144,6 +151,7 @@ struct LogitTile {
         const bool whole = p.tile.n + TILE <= l.o.N;
         const int64_t n0 = p.tile.n + p.first;
         auto* words = reinterpret_cast<Stats(*)[TILE]>(lds);  // [WN][TILE]
+        float* hit = v.g;  // (free here)
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const float xs = v.x_scale[p.row + i * 16];
@@ -163,12 +171,11 @@ struct LogitTile {
             float sum[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < COLS; ++k) sum[k % 2] += exp_of(z[k] - q);
-            const int at = hot(l, p, target(v, p, i));
-            const int64_t m = p.tile.m + p.row + i * 16;
+            const int at = hot(l, p, target(v, p.row + i * 16));
             if (__any(at >= 0)) {
 #pragma unroll
                 for (int k = 0; k < COLS; ++k)
-                    if (k == at && m < l.o.M && n0 + k < l.o.N) hit[m] = z[k];
+                    if (k == at) hit[p.row + i * 16] = z[k];
             }
             Stats s = {top, sum[0] + sum[1]};
 #pragma unroll
@@ -181,8 +188,16 @@ struct LogitTile {
         Stats s = words[0][threadIdx.x];
 #pragma unroll
         for (int w = 1; w < WN; ++w) s = join(s, words[w][threadIdx.x]);
-        const int64_t m = p.tile.m + threadIdx.x;
-        if (m < l.o.M) part[(first_tile + p.tile.n / TILE) * l.o.M + m] = s;
+        const int64_t m = p.tile.m + threadIdx.x, y = target(v, (int)threadIdx.x);
+        if (m >= l.o.M) return;
+        const int64_t at = y - l.first - p.tile.n;
+        const bool here = at >= 0 && at < TILE && p.tile.n + at < l.o.N;
+        if (to.part == nullptr) {
+            write_loss(s, hit[threadIdx.x], y, here ? y + 1 : 0, to.lse + m, to.loss + m);
+            return;
+        }
+        to.part[(first_tile + p.tile.n / TILE) * l.o.M + m] = s;
+        if (here) to.hit[m] = hit[threadIdx.x];
     }
 
     // The gradient of the logits, times g, twice: by rows, each class scaled by w_scale, for
@@ -205,7 +220,7 @@ struct LogitTile {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int row = p.row + i * 16;
-            const int64_t y = target(v, p, i), m = p.tile.m + row;
+            const int64_t y = target(v, row), m = p.tile.m + row;
             const int at = hot(l, p, y);
             const float xs = v.x_scale[row], g = v.g[row];
             const float lse = y >= to.classes ? __builtin_nanf("") : v.lse[row];
@@ -364,10 +379,10 @@ struct LogitTile {
 };
 
 template <int TILE, int WN, int S>
-__global__ __launch_bounds__(128 * WN) void xent_stats_kernel(Logits l, Stats* part, float* hit,
+__global__ __launch_bounds__(128 * WN) void xent_stats_kernel(Logits l, Found to,
                                                               int64_t tiles_m, int64_t tiles_n,
                                                               int64_t first_tile) {
-    LogitTile<TILE, WN, S>::stats(l, part, hit, tiles_m, tiles_n, first_tile);
+    LogitTile<TILE, WN, S>::stats(l, to, tiles_m, tiles_n, first_tile);
 }
 template <int TILE, int WN, int S, int PX, int PW>
 __global__ __launch_bounds__(128 * WN) void xent_slopes_kernel(Logits l, Slopes to,
@@ -375,17 +390,32 @@ __global__ __launch_bounds__(128 * WN) void xent_slopes_kernel(Logits l, Slopes 
     LogitTile<TILE, WN, S>::template grads<PX, PW>(l, to, tiles_m, tiles_n);
 }
 
-// Rows and classes of the tile that some logits are made in: 256, 128 or 64.
-inline int logit_tile(int64_t M, int64_t N, int64_t steps) {
+// Rows and classes of the tile that some logits are made in: 256, 128 or 64, whichever
+// should take least.  `join`: ns that more than one tile of classes costs; `parts`: in
+// which their gradient is written (0: the loss).  Measured on one card, us:
+//                              loss                  gradients, bf16 (2 parts)
+//   tokens, classes, channels  256   128   64        256   128   64
+//   128 x 100 x 384            14.4  8.3   7.3       26.6  17.9  11.8
+//   512 x 4096 x 384           15.6  10.5  7.9       42.6  33.7  30.4
+//   997 x 12345 x 385          20.7  24.5  35.6      79.8  84.0  89.6
+//   256 x 32768 x 1024         21.4  18.2  28.2      111   105   110
+//   2048 x 32768 x 1024        81.4  93.1  157       425   445   519
+//   100 x 50000 x 2048         34.0  26.6  38.7      234   227   226
+//   4096 x 4096 x 2048         34.7  45.0  63.9      168   180   197
+inline int logit_tile(int64_t M, int64_t N, int64_t steps, int join, int parts) {
     struct {
-        int tile, alone, each, end;  // ns of a step, and of what follows the last
-    } const tiles[] = {{256, 1800, 1800, 6000}, {128, 540, 620, 3000}, {64, 280, 220, 1500}};
+        int tile, alone, each;  // ns of a step: one tile a CU, and several
+        int end, more;          // and of what follows the last
+    } const tiles[] = {{256, 1650, 1650, 7000 + 4500 * parts, 5500 + 4500 * parts},
+                       {128, 540, 620, 4200 + 1700 * parts, 1300 + 1100 * parts},
+                       {64, 280, 220, 300 + 750 * parts, 1100 + 300 * parts}};
     double best = -1;
     int tile = 0;
     for (const auto& t : tiles) {
-        const int64_t n = up(M, t.tile) * up(N, t.tile);
-        const double time = n <= kCus ? steps * (double)t.alone + t.end
-                                      : (double)up(n, kCus) * (steps * (double)t.each + t.end / 2);
+        const int64_t tn = up(N, t.tile), n = up(M, t.tile) * tn;
+        const double time = (n <= kCus ? steps * (double)t.alone + t.end
+                                       : (double)up(n, kCus) * (steps * (double)t.each + t.more)) +
+                            (tn > 1 ? join : 0);
         if (best < 0 || time < best) {
             best = time;
             tile = t.tile;
