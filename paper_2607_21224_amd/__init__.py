@@ -8,10 +8,10 @@ Submodules
          it, step tables and HIP-graph capture, checkpoint/resume
   multi  the same for a model held as separate tensors (multi-tensor plans)
   q8     binding of include/cpdp_q8.h (libcpdp_q8.so, through the extension module
-         _q8): norm, products and activations on rows of 8-bit numbers, and their
-         backward passes
-  layer  the MLP half of a transformer block on that path, with its weights and
-         gradients in replica rows
+         _q8): norm, products, activations and the loss on rows of 8-bit numbers,
+         and their backward passes
+  layer  the MLP half of a transformer block, and a model's head with its loss, on
+         that path, with their weights and gradients in replica rows
   build  hipcc build of the shared libraries
 
 Importing ``cpdp`` or ``q8`` (directly or through ``state``) raises ImportError

@@ -3,9 +3,9 @@
 //   c_i = min(1, max_norm / (norm_i + 1e-6));  g_i <- c_i g_i
 //
 // Both are bound by HBM.  A first launch gives each block a run of chunks of one
-// replica (of all replicas for the mean) and leaves one sum for each; a second one
-// adds a replica's sums up, every block of it by itself and in the same order, and
-// scales.  Squares and sums are fp64: they cannot overflow or lose small values, and
+// replica (of all replicas for the mean) and leaves one sum for each; a second one adds
+// them up, and a third scales.  Where the gradients are small, the second is left out:
+// every block of the last adds its replica's sums up by itself, in the same order.  Squares and sums are fp64: they cannot overflow or lose small values, and
 // cost nothing beside the memory (2 instructions a coordinate of 4 bytes).  There
 // are no atomics; the order of a sum is fixed by the sizes.
 #include "cpdp_device.h"
@@ -74,7 +74,7 @@ struct PlanRows {
     template <class F>
     __device__ __forceinline__ void runs(int64_t c0, int64_t c1, F f) const {
         const PlanView v = plan_view(plan, W, n);
-        int64_t t = plan_tensor_scalar(v, n, c0);
+        int64_t t = plan_tensor(v, n, c0);
         for (int64_t c = c0; c < c1; ++t) {
             const int64_t start = v.chunk_start[t], end = min(v.chunk_start[t + 1], c1);
             if (end <= c) continue;  // an empty tensor
@@ -85,31 +85,47 @@ struct PlanRows {
     }
 };
 
-// body(at, first) for the thread's pieces of `count` coordinates, U of them at a
-// time: a piece is read at `at`, and its coordinates from `first` on are the
-// thread's.  (A piece that the end cuts short is read as the last N coordinates,
+// body(whole, at, first) for the thread's pieces of `count` coordinates, U of them at a
+// time, and the rest together (at, first: arrays of them): a piece is read at `at`, and
+// its coordinates from `first` on are the thread's.  whole: all of them are, and pieces
+// are aligned.  (A piece that the end cuts short is read as the last N coordinates,
 // wherever they start.)  count >= N.
 template <int N, int U, class Body>
 __device__ __forceinline__ void pieces(int64_t count, Body body) {
     constexpr int64_t kRound = (int64_t)kThreads * N;
     const int64_t lane = (int64_t)threadIdx.x * N;
-    int64_t at[U];
-    int first[U];
     int64_t r = 0;
     for (; r + U * kRound <= count; r += U * kRound) {
+        int64_t at[U];
+        int first[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) at[u] = r + u * kRound + lane, first[u] = 0;
-        body(at, first);
+        body(std::true_type(), at, first);
     }
-    for (; r < count; r += U * kRound) {
+    const auto rest = [&](auto some) {
+        int64_t at[some];
+        int first[some];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < some; ++u) {
             const int64_t i = r + u * kRound + lane, last = count - N;
             at[u] = i < last ? i : last;
             first[u] = (int)min(i - at[u], (int64_t)N);
         }
-        body(at, first);
-    }
+        body(std::false_type(), at, first);
+    };
+    const int64_t left = count - r;
+    if (left <= 0) return;
+    if (left <= kRound) rest(std::integral_constant<int, 1>());
+    else if (left <= 2 * kRound) rest(std::integral_constant<int, 2>());
+    else if (left <= 4 * kRound) rest(std::integral_constant<int, 4>());
+    else rest(std::integral_constant<int, 8>());
+}
+// a piece that is read once more, if at all, long after (nontemporal, 8 at a time: the
+// norms of 8 x 21.3 M fp32 107 us; ordinary 121)
+template <bool WHOLE>
+__device__ __forceinline__ u32x4 read_once(const void* p) {
+    if constexpr (WHOLE) return __builtin_nontemporal_load(static_cast<const u32x4*>(p));
+    else return *static_cast<const u32x4_any*>(p);
 }
 
 __device__ __forceinline__ double wave_sum(double x) {
@@ -136,7 +152,7 @@ template <class G, bool MEAN, class Src>
 __device__ __forceinline__ double part_sum(const Src& src, int64_t row, int W, float inv_w,
                                            int64_t c0, int64_t c1) {
     using T = typename G::T;
-    constexpr int N = G::N, U = MEAN ? 1 : 4;
+    constexpr int N = G::N;
     double acc[4] = {0.0, 0.0, 0.0, 0.0};
     src.runs(c0, c1, [&](int64_t t, int64_t e, int64_t count) {
         if (count < N) {
@@ -153,13 +169,11 @@ __device__ __forceinline__ double part_sum(const Src& src, int64_t row, int W, f
             acc[0] = fma((double)x, (double)x, acc[0]);
             return;
         }
-        const auto load = [&](int64_t i, int64_t at) {
-            G g;
-            g.v = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(src.row(i, t)) + e +
-                                                      at);
-            return g;
-        };
-        pieces<N, U>(count, [&](const int64_t (&at)[U], const int (&first)[U]) {
+        pieces<N, MEAN ? 1 : 8>(count, [&](auto whole, const auto& at, const auto& first) {
+            constexpr int U = sizeof(at) / sizeof(at[0]);
+            const auto load = [&](int64_t i, int64_t at) {
+                return G{read_once<whole>(static_cast<const T*>(src.row(i, t)) + e + at)};
+            };
             if constexpr (MEAN) {
                 float s[N] = {};
                 const auto add = [&](int i, auto rows) {
@@ -177,7 +191,7 @@ __device__ __forceinline__ double part_sum(const Src& src, int64_t row, int W, f
                 if (i < W) add(i, std::integral_constant<int, 1>());
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
-                    const float x = k < first[0] ? 0.0f : s[k] * inv_w;
+                    const float x = !whole && k < first[0] ? 0.0f : s[k] * inv_w;
                     acc[k % 4] = fma((double)x, (double)x, acc[k % 4]);
                 }
             } else {
@@ -188,7 +202,7 @@ __device__ __forceinline__ double part_sum(const Src& src, int64_t row, int W, f
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int k = 0; k < N; ++k) {
-                        const float x = k < first[u] ? 0.0f : g[u].get(k);
+                        const float x = !whole && k < first[u] ? 0.0f : g[u].get(k);
                         acc[k % 4] = fma((double)x, (double)x, acc[k % 4]);
                     }
             }
@@ -232,17 +246,23 @@ __device__ __forceinline__ float clip_scale(float norm, float max_norm) {
     return c >= 1.0f ? 1.0f : c;
 }
 
-// Part k of `parts` of a row, whose norm is the sum of `of_sums` parts (mean: every
-// row's is the first's).  Rows that are not longer than max_norm are not read.
+// Part k of `parts` of a row (mean: every row's norm is the first's), whose norm is the
+// sum of `of_sums` parts, or, with 0 of them, there already.  Rows that are not longer
+// than max_norm are not read.
 template <class G, class Src>
 __global__ __launch_bounds__(kThreads) void clip_kernel(Src src, int64_t chunks, int parts,
                                                         const double* sums, int of_sums, int mean,
                                                         float max_norm, float* norm) {
     using T = typename G::T;
-    constexpr int N = G::N, U = 4;
+    constexpr int N = G::N;
     const int64_t row = blockIdx.x / parts, k = blockIdx.x % parts, of = mean ? 0 : row;
-    const float x = row_norm(sums + of * of_sums, of_sums);
-    if (k == 0 && row == of && threadIdx.x == 0) norm[of] = x;
+    float x;
+    if (of_sums > 0) {
+        x = row_norm(sums + of * of_sums, of_sums);
+        if (k == 0 && row == of && threadIdx.x == 0) norm[of] = x;
+    } else {
+        x = norm[of];
+    }
     const float c = clip_scale(x, max_norm);
     if (c == 1.0f) return;
     src.runs(part_start(chunks, parts, k), part_start(chunks, parts, k + 1),
@@ -253,16 +273,22 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(Src src, int64_t chunks,
                 p[threadIdx.x] = G::narrow(G::one(p[threadIdx.x]) * c);
             return;
         }
-        pieces<N, U>(count, [&](const int64_t (&at)[U], const int (&first)[U]) {
+        pieces<N, 4>(count, [&](auto whole, const auto& at, const auto& first) {
+            constexpr int U = sizeof(at) / sizeof(at[0]);
             G g[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) g[u].v = *reinterpret_cast<const u32x4_any*>(p + at[u]);
+            for (int u = 0; u < U; ++u)
+                if constexpr (whole) g[u].v = *reinterpret_cast<const u32x4*>(p + at[u]);
+                else g[u].v = *reinterpret_cast<const u32x4_any*>(p + at[u]);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 float y[N];
 #pragma unroll
                 for (int j = 0; j < N; ++j) y[j] = g[u].get(j) * c;
-                if (first[u] == 0) {
+                if constexpr (whole) {
+                    g[u].set(y);
+                    *reinterpret_cast<u32x4*>(p + at[u]) = g[u].v;
+                } else if (first[u] == 0) {
                     g[u].set(y);
                     *reinterpret_cast<u32x4_any*>(p + at[u]) = g[u].v;
                 } else {
@@ -317,12 +343,24 @@ int launch_clip_grads(const Gradients& g, bool mean, float max_norm, float* norm
                       void* stream) {
     return with_source(g, [&](auto piece, auto src) {
         using G = decltype(piece);
-        const int of_sums = (int)norm_parts(mean ? 1 : g.W, g.chunks);
-        const int parts = (int)norm_parts(g.W, g.chunks);
+        const int rows = mean ? 1 : g.W, of_sums = (int)norm_parts(rows, g.chunks);
         auto* sums = static_cast<double*>(workspace);
         if (int e = norm_parts_of<G>(g, src, mean, of_sums, sums, stream)) return e;
+        // Past 64 MB the norms get a launch of their own, and the blocks that scale are of 32 KB
+        // in the order they lie in memory: 8 x 21.3 M fp32 scaled by 2048 blocks 240 us, by
+        // 42,000 214.  (Of 16 KB they take 10 us where there is nothing to scale, of 32 KB 6;
+        // the norm alone 112, clipped 328.)
+        constexpr int64_t kRun = 32768 / (kCoords * (int64_t)sizeof(typename G::T));
+        const int64_t fine = (g.chunks + kRun - 1) / kRun;
+        const bool large = g.W * g.chunks * kCoords * (int64_t)sizeof(typename G::T) > (64 << 20) &&
+                           fine * g.W * kThreads < (int64_t)1 << 32;
+        if (large)
+            if (int e = launch_blocks(norm_join_kernel, rows, stream, sums, of_sums, norm))
+                return e;
+        const int parts = (int)(large ? fine : norm_parts(g.W, g.chunks));
         return launch_blocks(clip_kernel<G, decltype(src)>, (int64_t)parts * g.W, stream, src,
-                             g.chunks, parts, sums, of_sums, (int)mean, max_norm, norm);
+                             g.chunks, parts, sums, large ? 0 : of_sums, (int)mean, max_norm,
+                             norm);
     });
 }
 

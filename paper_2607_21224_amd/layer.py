@@ -1,5 +1,5 @@
-"""The MLP half of a transformer block on the 8-bit activation path, trained by the
-CPDP steps.
+"""Layers on the 8-bit activation path, trained by the CPDP steps: the MLP half of a
+transformer block (``Q8Mlp``), and a model's head with its loss (``Q8Head``, below).
 
 ``Q8Mlp`` holds no weights: they are slices of a replica's row of
 ``CpdpState.params``, and its gradients go into the same slices of a row of
@@ -93,7 +93,36 @@ class Saved:
         self.workspace = scratch.workspace
 
 
-class Q8Mlp:
+class _Tensors:
+    """A layer's tensors in a replica's row, each from a 16-byte boundary on in every
+    storage type."""
+
+    def _lay_out(self, shapes) -> None:
+        self.tensors, at = {}, 0
+        for name, shape in shapes:
+            n = shape[0] * (shape[1] if len(shape) == 2 else 1)
+            self.tensors[name] = (at, shape)
+            at = round_up(at + n, 8)
+        self.numel = at
+
+    def view(self, row: torch.Tensor, name: str) -> torch.Tensor:
+        """A tensor of the layer in a replica's row of parameters or gradients."""
+        at, shape = self.tensors[name]
+        n = shape[0] * (shape[1] if len(shape) == 2 else 1)
+        return row[at:at + n].view(shape)
+
+    def init(self, generator: torch.Generator | None = None, device="cuda") -> torch.Tensor:
+        """Initial parameters, (numel,) fp32: the norm's weight 1, the others normal
+        with the variance 1 / inputs."""
+        row = torch.zeros(self.numel, device=device)
+        self.view(row, "norm").fill_(1.0)
+        for name, (_, shape) in self.tensors.items():
+            if len(shape) == 2:
+                self.view(row, name).normal_(0.0, shape[1] ** -0.5, generator=generator)
+        return row
+
+
+class Q8Mlp(_Tensors):
     """dim -> hidden -> dim with a root-mean-square norm before it; kind "gelu", or
     "swiglu" with two inner products."""
 
@@ -115,33 +144,12 @@ class Q8Mlp:
         if self.gated:
             shapes.append(("w1u", (hidden, dim)))
         shapes.append(("w2", (dim, hidden)))
-        self.tensors, at = {}, 0
-        for name, shape in shapes:
-            n = shape[0] * (shape[1] if len(shape) == 2 else 1)
-            self.tensors[name] = (at, shape)
-            at = round_up(at + n, 8)
-        self.numel = at
-
-    def view(self, row: torch.Tensor, name: str) -> torch.Tensor:
-        """A tensor of the layer in a replica's row of parameters or gradients."""
-        at, shape = self.tensors[name]
-        n = shape[0] * (shape[1] if len(shape) == 2 else 1)
-        return row[at:at + n].view(shape)
+        self._lay_out(shapes)
 
     def _w_in(self, row: torch.Tensor) -> torch.Tensor:
         """The inner product's weights, (inner, dim): w1, and w1u after it."""
         at, _ = self.tensors["w1"]
         return row[at:at + self.inner * self.dim].view(self.inner, self.dim)
-
-    def init(self, generator: torch.Generator | None = None, device="cuda") -> torch.Tensor:
-        """Initial parameters, (numel,) fp32: the norm's weight 1, the others normal
-        with the variance 1 / inputs."""
-        row = torch.zeros(self.numel, device=device)
-        self.view(row, "norm").fill_(1.0)
-        for name, (_, shape) in self.tensors.items():
-            if len(shape) == 2:
-                self.view(row, name).normal_(0.0, shape[1] ** -0.5, generator=generator)
-        return row
 
     def saved(self, T: int, device="cuda", scratch: Scratch | None = None) -> Saved:
         return Saved(self, int(T), device, scratch)
@@ -193,6 +201,94 @@ class Q8Mlp:
                            du=s.z[1] if self.gated else None, stream=stream)
         q8.cpdp_q8_grad_weight(s.z_all, s.n, s.n_scale, self._w_in(grads), **kw)
         q8.cpdp_q8_grad_input(s.z_all, *s.w_in, s.dn, **kw)
+        q8.cpdp_q8_norm_bwd(s.dn, s.norm_of, self.view(params, "norm"), s.rstd, s.dx,
+                            self.view(grads, "norm"), dres=dres, **kw)
+        return s.dx
+
+
+class HeadSaved:
+    """What a head's forward pass over `T` tokens leaves for its backward pass, and the results
+    of both; it serves one replica after another.  The logits are not among it."""
+
+    def __init__(self, head: "Q8Head", T: int, device="cuda"):
+        def rows(r, c, dt=head.act_dtype):
+            return q8.empty_rows(r, c, dt, device)
+
+        def vec(n):
+            return torch.empty(n, device=device)
+
+        D, V, i8 = head.dim, head.classes, torch.int8
+        self.T = T
+        self.n, self.n_scale, self.rstd = rows(T, D, i8), vec(T), vec(T)
+        self.w = rows(V, D, i8), vec(V)  # the weights as they were used
+        self.loss, self.lse = vec(T), vec(T)
+        self.h, self.dn, self.dx = rows(T, D), rows(T, D), rows(T, D)
+        self.target = self.norm_of = None
+        self.workspace = torch.empty(head.workspace_bytes(T), dtype=torch.uint8, device=device)
+
+
+class Q8Head(_Tensors):
+    """A model's last norm and its classifier over `classes` (a vocabulary), with the softmax
+    cross entropy of the targets:
+        h = x + residual;  n = 8(norm(h) * w_norm)
+        loss[t] = log sum_v exp z[t, v] - z[t, target[t]],  z = n 8(W)^T
+    The logits z are never held as a whole.  Its weights and gradients are slices of a
+    replica's row, as Q8Mlp's::
+
+        head = Q8Head(dim=384, classes=32768)
+        row = torch.cat([mlp.init(), head.init()])       # one model of both
+        at = mlp.numel
+        loss = head.forward(st.params[i][at:], y, target, saved, residual=x)
+        dy = head.backward(st.params[i][at:], weight, saved, grads[i][at:])
+
+    ``target`` is (T,) int64; tokens whose target is negative do not count.
+    """
+
+    def __init__(self, dim: int, classes: int, eps: float = 1e-6, act_dt: str = "bf16"):
+        if act_dt not in _DT:
+            raise ValueError(f"act_dt must be 'f32' or 'bf16', got {act_dt!r}")
+        if dim % 8:
+            raise ValueError("dim must be a multiple of 8: the weights' rows lie one after the "
+                             "other in a replica's row, each on a 16-byte boundary")
+        self.dim, self.classes, self.eps = int(dim), int(classes), float(eps)
+        self.act_dtype = _DT[act_dt]
+        self._lay_out([("norm", (self.dim,)), ("w", (self.classes, self.dim))])
+
+    def saved(self, T: int, device="cuda") -> HeadSaved:
+        return HeadSaved(self, int(T), device)
+
+    def workspace_bytes(self, T: int) -> int:
+        """The largest workspace of the head's calls over T tokens."""
+        V, D = self.classes, self.dim
+        need = [q8.cpdp_q8_norm_bwd_workspace(T, D), q8.cpdp_q8_xent_workspace(T, V, D)]
+        need += [q8.cpdp_q8_xent_bwd_workspace(T, V, D, self.act_dtype, g) for g in _DT.values()]
+        return max(need + [16])
+
+    def forward(self, params, x, target, saved: HeadSaved, residual=None,
+                stream=None) -> torch.Tensor:
+        """saved.loss (T,) <- the losses of x (T, dim); params is the head's part of a replica's
+        row.  With a residual saved.h is x + residual; without one the backward pass reads x
+        again, and either way `target`: they have to stay as they are until then."""
+        s = saved
+        kw = {} if residual is None else {"residual": residual, "h": s.h}
+        s.norm_of, s.target = x if residual is None else s.h, target
+        q8.cpdp_q8_norm(x, self.view(params, "norm"), self.eps, q=s.n, scale=s.n_scale,
+                        rstd=s.rstd, stream=stream, **kw)
+        q8.cpdp_q8_rows(self.view(params, "w"), *s.w, stream=stream)
+        q8.cpdp_q8_xent(s.n, s.n_scale, *s.w, target, s.loss, s.lse, workspace=s.workspace,
+                        stream=stream)
+        return s.loss
+
+    def backward(self, params, g, saved: HeadSaved, grads, dres=None,
+                 stream=None) -> torch.Tensor:
+        """The gradients of the last forward pass over `saved`, with g (T,) fp32 that of
+        saved.loss (1 / T for the mean): of the parameters into `grads`, the head's part of a
+        row of gradients, and of the input, returned; dres is what reaches x + residual past
+        the head."""
+        s = saved
+        kw = {"workspace": s.workspace, "stream": stream}
+        q8.cpdp_q8_xent_bwd(s.n, s.n_scale, *s.w, s.target, s.lse, g, s.dn,
+                            self.view(grads, "w"), **kw)
         q8.cpdp_q8_norm_bwd(s.dn, s.norm_of, self.view(params, "norm"), s.rstd, s.dx,
                             self.view(grads, "norm"), dres=dres, **kw)
         return s.dx
