@@ -143,8 +143,7 @@ def test_gradients(q8, T, V, K, types):  # noqa: F811
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
 
 
-@pytest.mark.parametrize("T,V,K", [(5, 33, 17), (64, 1001, 384), (128, 100, 384), (997, 1235, 385),
-                                   (997, 70001, 70), (4099, 2051, 1030)])
+@pytest.mark.parametrize("T,V,K", xent_sizes.ONE)
 @pytest.mark.parametrize("types", xent_sizes.ALONE)
 def test_one_gradient_alone(q8, T, V, K, types):  # noqa: F811
     c = Case(T, V, K)
