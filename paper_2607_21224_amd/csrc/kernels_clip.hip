@@ -74,7 +74,7 @@ struct PlanRows {
     template <class F>
     __device__ __forceinline__ void runs(int64_t c0, int64_t c1, F f) const {
         const PlanView v = plan_view(plan, W, n);
-        int64_t t = plan_tensor(v, n, c0);
+        int64_t t = plan_tensor_scalar(v, n, c0);
         for (int64_t c = c0; c < c1; ++t) {
             const int64_t start = v.chunk_start[t], end = min(v.chunk_start[t + 1], c1);
             if (end <= c) continue;  // an empty tensor
