@@ -5,7 +5,8 @@
 // Both are bound by HBM.  A first launch gives each block a run of chunks of one
 // replica (of all replicas for the mean) and leaves one sum for each; a second one adds
 // them up, and a third scales.  Where the gradients are small, the second is left out:
-// every block of the last adds its replica's sums up by itself, in the same order.  Squares and sums are fp64: they cannot overflow or lose small values, and
+// every block of the last adds its replica's sums up by itself, in the same order; and a
+// replica of up to 80 KB is one block's, in one launch.  Squares and sums are fp64: they cannot overflow or lose small values, and
 // cost nothing beside the memory (2 instructions a coordinate of 4 bytes).  There
 // are no atomics; the order of a sum is fixed by the sizes.
 #include "cpdp_device.h"
@@ -15,7 +16,7 @@
 namespace cpdp {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kRowThreads = 1024;  // of a part's block, of a whole row's
 constexpr int64_t kCoords = (int64_t)kBlock * kVec;  // of a chunk
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -90,9 +91,9 @@ struct PlanRows {
 // its coordinates from `first` on are the thread's.  whole: all of them are, and pieces
 // are aligned.  (A piece that the end cuts short is read as the last N coordinates,
 // wherever they start.)  count >= N.
-template <int N, int U, class Body>
+template <int THREADS, int N, int U, class Body>
 __device__ __forceinline__ void pieces(int64_t count, Body body) {
-    constexpr int64_t kRound = (int64_t)kThreads * N;
+    constexpr int64_t kRound = (int64_t)THREADS * N;
     const int64_t lane = (int64_t)threadIdx.x * N;
     int64_t r = 0;
     for (; r + U * kRound <= count; r += U * kRound) {
@@ -148,7 +149,7 @@ __device__ __forceinline__ double block_sum(double x) {
 
 // A part of the sum of squares of a row, or (MEAN) of the mean of W rows: the rows'
 // coordinates are added up in fp32, in their order, as a synchronisation step does.
-template <class G, bool MEAN, class Src>
+template <int THREADS, class G, bool MEAN, class Src>
 __device__ __forceinline__ double part_sum(const Src& src, int64_t row, int W, float inv_w,
                                            int64_t c0, int64_t c1) {
     using T = typename G::T;
@@ -169,7 +170,7 @@ __device__ __forceinline__ double part_sum(const Src& src, int64_t row, int W, f
             acc[0] = fma((double)x, (double)x, acc[0]);
             return;
         }
-        pieces<N, MEAN ? 1 : 8>(count, [&](auto whole, const auto& at, const auto& first) {
+        pieces<THREADS, N, MEAN ? 1 : 8>(count, [&](auto whole, const auto& at, const auto& first) {
             constexpr int U = sizeof(at) / sizeof(at[0]);
             const auto load = [&](int64_t i, int64_t at) {
                 return G{read_once<whole>(static_cast<const T*>(src.row(i, t)) + e + at)};
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void norm_part_kernel(Src src, int W, flo
                                                              int64_t chunks, int parts,
                                                              double* sums) {
     const int64_t row = blockIdx.x / parts, k = blockIdx.x % parts;
-    const double s = block_sum<kThreads>(part_sum<G, MEAN>(src, row, W, inv_w,
+    const double s = block_sum<kThreads>(part_sum<kThreads, G, MEAN>(src, row, W, inv_w,
                                                            part_start(chunks, parts, k),
                                                            part_start(chunks, parts, k + 1)));
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
@@ -246,34 +247,20 @@ __device__ __forceinline__ float clip_scale(float norm, float max_norm) {
     return c >= 1.0f ? 1.0f : c;
 }
 
-// Part k of `parts` of a row (mean: every row's norm is the first's), whose norm is the
-// sum of `of_sums` parts, or, with 0 of them, there already.  Rows that are not longer
-// than max_norm are not read.
-template <class G, class Src>
-__global__ __launch_bounds__(kThreads) void clip_kernel(Src src, int64_t chunks, int parts,
-                                                        const double* sums, int of_sums, int mean,
-                                                        float max_norm, float* norm) {
+// Scales chunks c0 to c1 of a row by c.
+template <int THREADS, class G, class Src>
+__device__ __forceinline__ void scale(const Src& src, int64_t row, int64_t c0, int64_t c1,
+                                      float c) {
     using T = typename G::T;
     constexpr int N = G::N;
-    const int64_t row = blockIdx.x / parts, k = blockIdx.x % parts, of = mean ? 0 : row;
-    float x;
-    if (of_sums > 0) {
-        x = row_norm(sums + of * of_sums, of_sums);
-        if (k == 0 && row == of && threadIdx.x == 0) norm[of] = x;
-    } else {
-        x = norm[of];
-    }
-    const float c = clip_scale(x, max_norm);
-    if (c == 1.0f) return;
-    src.runs(part_start(chunks, parts, k), part_start(chunks, parts, k + 1),
-             [&](int64_t t, int64_t e, int64_t count) {
+    src.runs(c0, c1, [&](int64_t t, int64_t e, int64_t count) {
         T* const p = src.row(row, t) + e;
         if (count < N) {
             if ((int64_t)threadIdx.x < count)
                 p[threadIdx.x] = G::narrow(G::one(p[threadIdx.x]) * c);
             return;
         }
-        pieces<N, 4>(count, [&](auto whole, const auto& at, const auto& first) {
+        pieces<THREADS, N, 4>(count, [&](auto whole, const auto& at, const auto& first) {
             constexpr int U = sizeof(at) / sizeof(at[0]);
             G g[U];
 #pragma unroll
@@ -301,12 +288,59 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(Src src, int64_t chunks,
     });
 }
 
-template <class... Args>
+// Part k of `parts` of a row (mean: every row's norm is the first's), whose norm is the
+// sum of `of_sums` parts, or, with 0 of them, there already.  Rows that are not longer
+// than max_norm are not read.
+template <class G, class Src>
+__global__ __launch_bounds__(kThreads) void clip_kernel(Src src, int64_t chunks, int parts,
+                                                        const double* sums, int of_sums, int mean,
+                                                        float max_norm, float* norm) {
+    const int64_t row = blockIdx.x / parts, k = blockIdx.x % parts, of = mean ? 0 : row;
+    float x;
+    if (of_sums > 0) {
+        x = row_norm(sums + of * of_sums, of_sums);
+        if (k == 0 && row == of && threadIdx.x == 0) norm[of] = x;
+    } else {
+        x = norm[of];
+    }
+    const float c = clip_scale(x, max_norm);
+    if (c != 1.0f)
+        scale<kThreads, G>(src, row, part_start(chunks, parts, k),
+                           part_start(chunks, parts, k + 1), c);
+}
+
+// A block's whole row (or the mean of all rows): its norm, and (clip) the row scaled.  In a
+// block of its own a small row's sum needs no other's: 2 x 10007 fp32, clipping calls after
+// each other, 8.5 us in two launches, 5.7 in one.
+template <class G, bool MEAN, class Src>
+__global__ __launch_bounds__(kRowThreads) void norm_row_kernel(Src src, int W, float inv_w,
+                                                               int64_t chunks, int clip,
+                                                               float max_norm, float* norm) {
+    const int64_t row = blockIdx.x;
+    const float x = (float)sqrt(block_sum<kRowThreads>(
+        part_sum<kRowThreads, G, MEAN>(src, row, W, inv_w, (int64_t)0, chunks)));
+    if (threadIdx.x == 0) norm[row] = x;
+    if constexpr (!MEAN) {
+        const float c = clip_scale(x, max_norm);
+        if (clip && c != 1.0f) scale<kRowThreads, G>(src, row, 0, chunks, c);
+    }
+}
+
+template <int THREADS = kThreads, class... Args>
 int launch_blocks(void (*kernel)(Args...), int64_t blocks, void* stream,
                   typename same_type<Args>::type... args) {
     void* argv[] = {static_cast<void*>(&args)...};
     return (int)hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((uint32_t)blocks),
-                                dim3(kThreads), argv, 0, static_cast<hipStream_t>(stream));
+                                dim3(THREADS), argv, 0, static_cast<hipStream_t>(stream));
+}
+
+// Whether a block takes a row by itself: few enough for a CU each (1000 x 5000 fp32 13.3 us
+// so, 11.1 in parts), and small (clipped, 20000 fp32 9.1 and 10.4; 32768 10.1 and 9.5).  (Not
+// the mean's W rows where they are clipped: each would need the norm of all of them.)
+template <class G>
+bool small_rows(const Gradients& g, bool mean) {
+    const int64_t bytes = g.chunks * kCoords * (int64_t)sizeof(typename G::T);
+    return bytes * (mean ? g.W : 1) <= 81920 && (mean || g.W <= 256);
 }
 
 template <class G, class Src>
@@ -333,6 +367,12 @@ int launch_grad_norm(const Gradients& g, bool mean, float* norm, void* workspace
     return with_source(g, [&](auto piece, auto src) {
         using G = decltype(piece);
         const int rows = mean ? 1 : g.W, parts = (int)norm_parts(rows, g.chunks);
+        const float inv_w = 1.0f / (float)g.W;
+        if (small_rows<G>(g, mean))
+            return launch_blocks<kRowThreads>(mean ? norm_row_kernel<G, true, decltype(src)>
+                                                   : norm_row_kernel<G, false, decltype(src)>,
+                                              rows, stream, src, g.W, inv_w, g.chunks, 0, 0.0f,
+                                              norm);
         auto* sums = static_cast<double*>(workspace);
         if (int e = norm_parts_of<G>(g, src, mean, parts, sums, stream)) return e;
         return launch_blocks(norm_join_kernel, rows, stream, sums, parts, norm);
@@ -343,6 +383,9 @@ int launch_clip_grads(const Gradients& g, bool mean, float max_norm, float* norm
                       void* stream) {
     return with_source(g, [&](auto piece, auto src) {
         using G = decltype(piece);
+        if (!mean && small_rows<G>(g, false))
+            return launch_blocks<kRowThreads>(norm_row_kernel<G, false, decltype(src)>, g.W,
+                                              stream, src, g.W, 1.0f, g.chunks, 1, max_norm, norm);
         const int rows = mean ? 1 : g.W, of_sums = (int)norm_parts(rows, g.chunks);
         auto* sums = static_cast<double*>(workspace);
         if (int e = norm_parts_of<G>(g, src, mean, of_sums, sums, stream)) return e;
