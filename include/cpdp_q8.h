@@ -193,13 +193,16 @@ int cpdp_q8_grad_weight(const void* dy, int64_t lddy, int dy_dt, const int8_t* a
  * row of dx and all of dw.  dx [T x K] in dx_dt, dw [V x K] in dw_dt; either may be NULL
  * and is then not computed.
  * 0 <= T <= CPDP_Q8_MAX_T, 1 <= K <= CPDP_Q8_MAX_K.  Logits are exact sums, scaled in
- * fp32, and everything that is taken of them is fp32.  The gradients' products run on
- * the bfloat16 matrix cores with fp32 sums; each d[t, v], scaled, is held in three
- * bfloat16 numbers for an fp32 result (all of its 24 bits, down to 2^-126, below which
- * the matrix cores take a bfloat16 number as 0), in one for a bf16 result, as in the
- * gradients of a product from fp32 dy.
+ * fp32, and everything that is taken of them is fp32.  The gradients' products have fp32
+ * sums.  What they sum, with p the factor of g in d:
+ *   dx   p[t, v] * w_scale[v], each sum times g[t]
+ *   dw   p[t, v] * g[t] * x_scale[t]
+ * is held in two fp16 numbers for an fp32 result: 22 bits, but with an error of up to
+ * 2^-51 of the largest |w_scale|, or of the largest |g * x_scale| of the tokens that count;
+ * in one for a bf16 result: 11 bits, and 2^-39 of the largest.  (Up to 64 tokens: in bfloat16 numbers, as the gradients of a
+ * product from fp32 dy.)
  */
-#define CPDP_Q8_MAX_T 4194232 /* 2^22 - 72: what a gradient sums over */
+#define CPDP_Q8_MAX_T 2097088 /* 2^21 - 64: rows of sums that a tile can address */
 
 int64_t cpdp_q8_xent_workspace(int64_t T, int64_t V, int64_t K);
 int cpdp_q8_xent(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw,

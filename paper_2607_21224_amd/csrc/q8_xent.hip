@@ -5,8 +5,7 @@
 // where they are made (q8_xent_tile.h).  The loss takes one launch over all tiles and
 // one that joins what they found of each token.  Its gradients make the logits again, a
 // piece of the classes at a time, and leave the gradient of them laid out for two
-// products on the bf16 matrix cores (q8_grad_gemm.h).
-#include "q8_grad_layout.h"
+// products of fp16 numbers.
 #include "q8_xent_tile.h"
 
 namespace cpdp {
@@ -107,64 +106,174 @@ int forward(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
                   r.tiles, l.V, l.target, loss, lse);
 }
 
-// 8-bit operands [R x C] as out [C x pad] in bf16, zeros from R to pad: two of them in a
-// launch, or one (the other has no blocks).
-__global__ __launch_bounds__(256) void xent_turn_kernel(Source a, Source b) {
-    __shared__ Tile<1, tile_cols<int8_t>()> tile;
-    if (blockIdx.x < a.blocks) transpose<I8, 1>(a, blockIdx.x, tile);
-    else transpose<I8, 1>(b, blockIdx.x - (uint32_t)a.blocks, tile);
+// ---- what the products of the gradients need first ----------------------------------
+
+constexpr int kRound = kStep / 2;  // fp16 numbers in a step: rows are padded to whole steps
+
+// An 8-bit operand [R x C] laid out as fp16 [C][copies][pad], zeros from R to pad: as many
+// copies as the other operand has parts, the second over kSecond.
+struct Source {
+    const int8_t* q;
+    int64_t ld, R, C;
+    uint16_t* out;
+    int64_t pad;
+    int copies;
+    int64_t blocks;  // of 64 rows and 128 columns
+};
+Source source(const int8_t* q, int64_t ld, int64_t R, int64_t C, uint16_t* out, int64_t pad,
+              int copies) {
+    return {q, ld, R, C, out, pad, copies, pad / 64 * up(C, 128)};
 }
-Source source(const int8_t* q, int64_t ld, int64_t R, int64_t C, int64_t pad, uint16_t* out) {
-    return {q, ld, nullptr, R, C, out, pad, pad / 64 * up(C, tile_cols<int8_t>())};
+
+// (columns of 32 pairs of rows, a word more, so that the 64 lanes of a wavefront, 8 pairs of
+// rows and 8 columns 8 apart, write to 64 banks)
+using Turned = uint32_t[128][33];
+
+__device__ __forceinline__ void turn(const Source& s, uint32_t block, Turned& tile) {
+    const uint32_t down = (uint32_t)(s.pad / 64);
+    const int64_t r0 = (int64_t)(block % down) * 64, c0 = (int64_t)(block / down) * 128;
+    const int pair = (int)threadIdx.x / 8, col = (int)threadIdx.x % 8 * kPiece;
+    Raw<I8> x[2][2] = {};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t r = r0 + 2 * pair + i, c = c0 + h * 64 + col;
+            const int n = s.C - c > kPiece ? kPiece : (int)(s.C - c);
+            if (r < s.R && n > 0) x[h][i].load(s.q + r * s.ld + c, n, (int)(c < 8 ? c : 8));
+        }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k)
+            tile[h * 64 + col + k][pair] = halves(x[h][0][k], x[h][1][k]);
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 128; h += 32) {
+        const int c = h + (int)threadIdx.x / 8, w = (int)threadIdx.x % 8 * 4;
+        if (c0 + c >= s.C) continue;
+        u32x4 v = {tile[c][w], tile[c][w + 1], tile[c][w + 2], tile[c][w + 3]};
+        uint16_t* out = s.out + (c0 + c) * s.copies * s.pad + r0 + 2 * w;
+        *reinterpret_cast<u32x4*>(out) = v;
+        if (s.copies == 1) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t word = v[k];
+            const f16x2 two = __builtin_bit_cast(f16x2, word);
+            v[k] = halves((float)two[0] / kSecond, (float)two[1] / kSecond);
+        }
+        *reinterpret_cast<u32x4*>(out + s.pad) = v;
+    }
 }
-int turn(const Source& a, const Source& b, void* stream) {
-    const int64_t blocks = a.blocks + b.blocks;
+
+// What the slopes are scaled by (see Slopes), and ones.
+struct Scales {
+    Held x, w;
+    const int64_t* target;
+    const float* g;
+    int64_t T, V, K;
+    float* scale;  // [2]; null: not wanted
+    float* ones;   // [K]
+};
+__device__ __forceinline__ float over_block(float x, float* words) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
+    if (threadIdx.x % 64 == 0) words[threadIdx.x / 64] = x;
+    __syncthreads();
+    return fmaxf(fmaxf(words[0], words[1]), fmaxf(words[2], words[3]));
+}
+// |x|, 0 if it is not finite
+__device__ __forceinline__ float size_of(float x) {
+    return magnitude(x) < 0x7f800000u ? fabsf(x) : 0.0f;
+}
+// the power of two that brings x into [2^14, 2^15), as far as that and its inverse are
+// normal numbers
+__device__ __forceinline__ float scale_for(float x) {
+    if (x == 0.0f) return 1.0f;
+    const int e = (int)(__float_as_uint(x) >> 23) - 127;  // (below 2^-126: -127)
+    const int up = 14 - e;
+    return __uint_as_float((uint32_t)((up > 126 ? 126 : up) + 127) << 23);
+}
+__device__ __forceinline__ void find_scales(const Scales& s, float (&words)[2][4]) {
+    float w = 0.0f, x = 0.0f;
+    // (16 loads on their way at a time: with 131072 classes they are what a block waits for)
+    for (int64_t v = threadIdx.x; v < s.V; v += 16 * 256) {
+        float some[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) some[i] = s.w.scale[v + i * 256 < s.V ? v + i * 256 : v];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w = fmaxf(w, size_of(some[i]));
+    }
+    for (int64_t t = threadIdx.x; t < s.T; t += 4 * 256) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t at = t + i * 256 < s.T ? t + i * 256 : t;
+            const float f = size_of(s.g[at] * s.x.scale[at]);
+            x = fmaxf(x, s.target[at] < 0 ? 0.0f : f);
+        }
+    }
+    w = over_block(w, words[0]);
+    x = over_block(x, words[1]);
+    if (threadIdx.x == 0) {
+        s.scale[0] = scale_for(w);
+        s.scale[1] = scale_for(x);
+    }
+    for (int64_t k = threadIdx.x; k < s.K; k += 256) s.ones[k] = 1.0f;
+}
+
+// Two operands, or one (the other has no blocks), and the scales.
+__global__ __launch_bounds__(256) void xent_turn_kernel(Source a, Source b, Scales s) {
+    __shared__ Turned tile;
+    __shared__ float words[2][4];
+    if (blockIdx.x < a.blocks) turn(a, blockIdx.x, tile);
+    else if (blockIdx.x < a.blocks + b.blocks) turn(b, blockIdx.x - (uint32_t)a.blocks, tile);
+    else find_scales(s, words);
+}
+int launch_turn(const Source& a, const Source& b, const Scales& s, void* stream) {
+    const int64_t blocks = a.blocks + b.blocks + (s.scale != nullptr ? 1 : 0);
     if (blocks == 0) return 0;
     if (blocks * 256 >= (int64_t)1 << 32) return (int)hipErrorInvalidValue;
-    return launch(xent_turn_kernel, dim3((uint32_t)blocks), 256, stream, a, b);
+    return launch(xent_turn_kernel, dim3((uint32_t)blocks), 256, stream, a, b, s);
 }
 
-// Classes of a piece: 2^27 logits' gradients at most (268 MB a part), whole tiles.
+// ---- the products --------------------------------------------------------------------
+
+// Classes of a piece: 2^27 slopes at most (268 MB a part), whole tiles, and rows that a tile
+// can address.
 int64_t piece_of(int64_t T, int64_t V) {
-    const int64_t n = ((int64_t)1 << 27) / T / 1024 * 1024;
-    return n < 1024 ? (V < 1024 ? V : 1024) : n < V ? n : V;
+    int64_t n = ((int64_t)1 << 27) / T / 1024 * 1024;
+    n = n < 1024 ? 1024 : n > (int64_t)1 << 20 ? (int64_t)1 << 20 : n;
+    return n < V ? n : V;
 }
 
-struct BackwardRoom : Room {
-    int64_t piece, row_ld, class_ld;  // classes of a piece; row lengths of the slopes
-    int px, pw;                       // parts
-    int64_t by_row, by_class, x, w, sum, slices;
-};
-
-// The tile of a gradient's product, and the slices that its sum over R is cut into where
-// there are fewer tiles than CUs.  A step of a tile takes what it takes in grad_shape;
-// here the large tiles are cut, too: dx of 4096 x 1024 over 32768 classes has 64 tiles of
-// 256 x 256, and in 4 slices takes 260 us, in 256 tiles of 128 x 128 335.
 // Whether a product is small: tiles that find a CU each, and few steps.  What it takes is
-// mostly its launch, and two of them are made in one (128 x 100 x 384 fp32: two of 4.7 us,
-// BOTH together).
-bool small(int64_t M, int64_t N, int64_t R, int parts) {
-    return up(M, 64) * up(N, 64) <= kCus / 2 && up(R, kRound) * parts <= 24;
+// mostly its launch, and two of them are made in one (128 x 100 x 384: gradients in 13.0 us,
+// and 18.1 with two).
+bool small(int64_t M, int64_t N, int64_t steps) {
+    return up(M, 64) * up(N, 64) <= kCus / 2 && steps <= 16;
 }
-Shape product_shape(int64_t M, int64_t N, int64_t R, int parts) {
-    const int64_t steps = up(R, kRound);
-    if (small(M, N, R, parts)) return {64, 64, 1, 0};
+// The tile of a gradient's product, and the slices that its sum is cut into where there are
+// fewer tiles than CUs.  A step of a tile takes what it takes in shape_of; here the large
+// tiles are cut, too: dx of 4096 x 1024 over 32768 classes has 64 tiles of 256 x 256, and is
+// made in 4 slices (with dw: 750 us in bf16, 1415 in fp32; in tiles of 128 x 128 and 256 x
+// 128 844 and 1548).
+Shape product_shape(int64_t M, int64_t N, int64_t steps) {
+    if (small(M, N, steps)) return {64, 64, 1, 0};
     struct {
-        int bm, bn, passes, alone, each, end;
-    } const tiles[] = {{256, 256, parts, 1800, 1800, 2000},
-                       {256, 128, parts, 1100, 1100, 1500},
-                       {128, 128, 1, 310 + 290 * parts, 230 + 390 * parts, 800},
-                       {64, 64, 1, 250 + 100 * parts, 105 + 115 * parts, 500}};
+        int bm, bn, alone, each, end;
+    } const tiles[] = {{256, 256, 1800, 1800, 2000},
+                       {256, 128, 1100, 1100, 1500},
+                       {128, 128, 540, 620, 800},
+                       {64, 64, 280, 220, 500}};
     Shape best = {0, 0, 1, -1};
     for (const auto& t : tiles) {
-        if (t.bm + t.bn == 384 && parts > 1) continue;
-        const int64_t n = up(M, t.bm) * up(N, t.bn), all = steps * t.passes;
+        const int64_t n = up(M, t.bm) * up(N, t.bn);
         if (t.bm < 256 && n >= (int64_t)1 << 23) continue;
         for (int slices = 1; slices <= 64; slices *= 2) {
-            if (slices > 1 && (n * slices > (t.bm == 64 ? 2048 : 512) || all < 4 * slices)) break;
+            if (slices > 1 && (n * slices > (t.bm == 64 ? 2048 : 512) || steps < 4 * slices)) break;
             const int64_t turns = up(n * slices, kCus);
             const double step = turns == 1 ? t.alone : (double)turns * t.each;
-            const double time = (double)up(all, slices) * step + turns * t.end +
+            const double time = (double)up(steps, slices) * step + turns * t.end +
                                 (slices > 1 ? 4500.0 + slices * (double)M * (double)N / 500.0 : 0);
             if (best.ns < 0 || time < best.ns) best = {t.bm, t.bn, slices, time};
         }
@@ -172,26 +281,94 @@ Shape product_shape(int64_t M, int64_t N, int64_t R, int parts) {
     return best;
 }
 
+// c [M x N] = the product of A [M x length] and B [N x length], with rows scaled.
+// Without c, the slices (one at least) are left for xent_add_kernel, not scaled.
+struct Product {
+    Operands o;
+    Target t;
+    Shape shape;
+    bool join;
+};
+int64_t steps_of(int64_t length) { return length / kRound; }
+Product product_of(const uint16_t* a, const uint16_t* b, int64_t length, int64_t M, int64_t N,
+                   const float* rows, const float* ones, Mat c, void* slices) {
+    Product p{};
+    p.o.a = reinterpret_cast<const char*>(a);
+    p.o.b = reinterpret_cast<const char*>(b);
+    p.o.lda = p.o.ldb = length * 2;
+    p.o.M = M;
+    p.o.N = N;
+    p.o.row = (int)(length * 2);
+    const bool whole = c.p != nullptr;
+    p.t.c = whole ? c.p : slices;
+    p.t.ldc = whole ? c.ld : slices_ld(N);
+    p.t.bf16 = whole && c.bf16;
+    p.t.row_scale = whole ? rows : nullptr;
+    p.t.col_scale = whole ? ones : nullptr;
+    p.t.ws = slices;
+    p.t.ldws = slices_ld(N);
+    p.t.slice = M * p.t.ldws;
+    p.shape = product_shape(M, N, steps_of(length));
+    p.join = whole && p.shape.slices > 1;
+    return p;
+}
+int launch_product(const Product& p, void* stream) {
+    const Shape& s = p.shape;
+    const int e = s.bn == 256 ? launch_tiles<Half, 256, 256, 2, 4>(p.o, p.t, s.slices, stream)
+                  : s.bm == 256
+                      ? launch_tiles<Half, 256, 128, 4, 2>(p.o, p.t, s.slices, stream)
+                  : s.bm == 128
+                      ? launch_tiles<Half, 128, 128, 2, 2>(p.o, p.t, s.slices, stream)
+                      : launch_tiles<Half, 64, 64, 2, 2>(p.o, p.t, s.slices, stream);
+    return e != 0 || !p.join ? e : launch_join<Half>(p.t, p.o.M, p.o.N, s.slices, stream);
+}
+
+// Two small products in one launch, blockIdx.y the one.
+__global__ __launch_bounds__(512) void xent_both_kernel(Operands a, Target to_a, Operands b,
+                                                        Target to_b) {
+    const bool second = blockIdx.y != 0;
+    const Operands o = second ? b : a;
+    const int64_t tm = (o.M + 63) / 64, tn = (o.N + 63) / 64;
+    if (blockIdx.x >= tm * tn) return;
+    Gemm<Half, 64, 64, 2, 2, 4, 2>::run(o, second ? to_b : to_a, tm, tn, 1);
+}
+bool is_small(const Product& p) { return small(p.o.M, p.o.N, steps_of(p.o.row / 2)); }
+int launch_both(const Product& a, const Product& b, void* stream) {
+    const int64_t na = up(a.o.M, 64) * up(a.o.N, 64), nb = up(b.o.M, 64) * up(b.o.N, 64);
+    return launch(xent_both_kernel, dim3((uint32_t)(na > nb ? na : nb), 2), 512, stream, a.o, a.t,
+                  b.o, b.t);
+}
+
+struct BackwardRoom : Room {
+    int64_t piece, row_ld, class_ld;  // classes of a piece; row lengths of the slopes' parts
+    int px, pw;                       // parts
+    int64_t by_row, by_class, x, w, scale, ones, rows, classes, sum, slices;
+};
 BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
     BackwardRoom r;
     r.piece = piece_of(T, V);
     r.row_ld = up(r.piece, kRound) * kRound;
     r.class_ld = up(T, kRound) * kRound;
-    r.px = dx_bf16 ? 1 : 3;
-    r.pw = dw_bf16 ? 1 : 3;
+    r.px = dx_bf16 ? 1 : 2;
+    r.pw = dw_bf16 ? 1 : 2;
     r.by_row = r.take(r.px * T * r.row_ld * 2);
     r.by_class = r.take(r.pw * r.piece * r.class_ld * 2);
-    r.x = r.take(K * r.class_ld * 2);
-    r.w = r.take(K * r.row_ld * 2);
+    r.x = r.take(r.pw * K * r.class_ld * 2);
+    r.w = r.take(r.px * K * r.row_ld * 2);
+    r.scale = r.take(8);
+    r.ones = r.take(K * 4);
+    r.rows = r.take(T * 4);
+    r.classes = r.take(r.piece * 4);
     const bool pieces = r.piece < V;
     if (pieces) r.sum = r.take(T * slices_ld(K) * 4);
     int64_t most = 0;
     const int64_t last = V - (V - 1) / r.piece * r.piece;
     for (int i = 0; i < 2; ++i) {
         const int64_t n = i ? last : r.piece;
-        const int64_t a = pieces ? T * slices_ld(K) * 4 * product_shape(T, K, n, r.px).slices
-                                 : slices_bytes(T, K, product_shape(T, K, n, r.px));
-        const int64_t b = slices_bytes(n, K, product_shape(n, K, T, r.pw));
+        const Shape x = product_shape(T, K, r.px * up(n, kRound));
+        const Shape w = product_shape(n, K, r.pw * up(T, kRound));
+        const int64_t a = pieces ? T * slices_ld(K) * 4 * x.slices : slices_bytes(T, K, x);
+        const int64_t b = slices_bytes(n, K, w);
         most = a > most ? a : most;
         most = b > most ? b : most;
     }
@@ -199,81 +376,12 @@ BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
     return r;
 }
 
-template <int P>
-int launch_tiles_of(const GradOperands& o, const Target& t, const Shape& s, void* stream) {
-    if (s.bn == 256) return launch_grad_tiles<256, 256, 2, 4, false, false, 1>(o, t, s.slices, stream);
-    if constexpr (P == 1)
-        if (s.bm == 256)
-            return launch_grad_tiles<256, 128, 4, 2, false, false, 1>(o, t, s.slices, stream);
-    if (s.bm == 128) return launch_grad_tiles<128, 128, 2, 2, false, false, P>(o, t, s.slices, stream);
-    return launch_grad_tiles<64, 64, 2, 2, false, false, P>(o, t, s.slices, stream);
-}
-
-// c [M x N] = the product of A, laid out in parts, and B, laid out, over R values.
-// Without c, the slices (one at least) are left for xent_add_kernel.
-struct Product {
-    GradOperands o;
-    Target t;
-    Shape shape;
-    bool join;
-};
-Product product_of(const uint16_t* a, int64_t a_part, const uint16_t* b, int64_t ld, int64_t M,
-                   int64_t N, int64_t R, int parts, Mat c, void* slices) {
-    Product p{};
-    p.o.a = reinterpret_cast<const char*>(a);
-    p.o.lda = p.o.ldb = ld * 2;
-    p.o.a_part = a_part * 2;
-    p.o.b = reinterpret_cast<const char*>(b);
-    p.o.R = R;
-    p.o.M = M;
-    p.o.N = N;
-    p.o.steps = (int)up(R, kRound);
-    p.o.parts = parts;
-    p.t.c = c.p != nullptr ? c.p : slices;
-    p.t.ldc = c.p != nullptr ? c.ld : slices_ld(N);
-    p.t.bf16 = c.p != nullptr && c.bf16;
-    p.t.ws = slices;
-    p.t.ldws = slices_ld(N);
-    p.t.slice = M * p.t.ldws;
-    p.shape = product_shape(M, N, R, parts);
-    p.join = c.p != nullptr && p.shape.slices > 1;
-    return p;
-}
-int launch_product(const Product& p, void* stream) {
-    if (int e = p.o.parts == 1 ? launch_tiles_of<1>(p.o, p.t, p.shape, stream)
-                               : launch_tiles_of<3>(p.o, p.t, p.shape, stream))
-        return e;
-    return p.join ? launch_join<Bf16>(p.t, p.o.M, p.o.N, p.shape.slices, stream) : 0;
-}
-
-// Two small products in one launch, blockIdx.y the one.
-template <int P>
-__global__ __launch_bounds__(256) void xent_both_kernel(GradOperands a, Target to_a,
-                                                        GradOperands b, Target to_b) {
-    const bool second = blockIdx.y != 0;
-    const GradOperands o = second ? b : a;
-    const int64_t tm = (o.M + 63) / 64, tn = (o.N + 63) / 64;
-    if (blockIdx.x >= tm * tn) return;
-    GradGemm<64, 64, 2, 2, false, false, P, 4>::run(o, second ? to_b : to_a, tm, tn, 1);
-}
-// Whether they may be: of as many parts, and small.
-bool both_small(const Product& a, const Product& b) {
-    return a.o.parts == b.o.parts && small(a.o.M, a.o.N, a.o.R, a.o.parts) &&
-           small(b.o.M, b.o.N, b.o.R, b.o.parts);
-}
-int launch_both(const Product& a, const Product& b, void* stream) {
-    const int64_t na = up(a.o.M, 64) * up(a.o.N, 64), nb = up(b.o.M, 64) * up(b.o.N, 64);
-    const dim3 grid((uint32_t)(na > nb ? na : nb), 2);
-    return a.o.parts == 3
-               ? launch(xent_both_kernel<3>, grid, 256, stream, a.o, a.t, b.o, b.t)
-               : launch(xent_both_kernel<1>, grid, 256, stream, a.o, a.t, b.o, b.t);
-}
-
-// sum <- sum and the slices of a piece, to dx after the last piece; 4 columns a thread
+// sum <- sum and the slices of a piece, to dx, its rows scaled, after the last piece; 4
+// columns a thread
 __global__ __launch_bounds__(256) void xent_add_kernel(float* sum, const float* part, int64_t ld,
                                                        int64_t slice, int64_t T, int64_t K,
                                                        int slices, int first, int last,
-                                                       Target out) {
+                                                       const float* rows, Target out) {
     const int64_t across = (K + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t t = i / across, k = i % across * 4;
     if (t >= T) return;
@@ -285,23 +393,23 @@ __global__ __launch_bounds__(256) void xent_add_kernel(float* sum, const float* 
         *reinterpret_cast<f32x4*>(sum + t * ld + k) = x;
         return;
     }
-    const float v[4] = {x[0], x[1], x[2], x[3]};
+    const float f = rows[t], v[4] = {x[0] * f, x[1] * f, x[2] * f, x[3] * f};
     store_cols<4>(out, t, k, (int)(K - k < 4 ? K - k : 4), v);
 }
 int add(const BackwardRoom& r, void* ws, const Loss& l, int slices, bool first, bool last, Mat dx,
         void* stream) {
     Target out{};
-    out.c = dx.p;
     out.ldc = dx.ld;
     out.bf16 = dx.bf16;
     const int64_t ld = slices_ld(l.K), across = up(l.K, 4);
     // (a launch holds fewer than 2^32 work items)
     return in_parts(l.T, across, [&](int64_t t, int64_t n) {
         Target part = out;
-        part.c = static_cast<char*>(out.c) + t * out.ldc * (out.bf16 ? 2 : 4);
+        part.c = static_cast<char*>(dx.p) + t * dx.ld * (dx.bf16 ? 2 : 4);
         return launch(xent_add_kernel, dim3((uint32_t)up(n * across, 256)), 256, stream,
                       at<float>(ws, r.sum) + t * ld, at<const float>(ws, r.slices) + t * ld, ld,
-                      l.T * ld, n, l.K, slices, (int)first, (int)last, part);
+                      l.T * ld, n, l.K, slices, (int)first, (int)last,
+                      at<const float>(ws, r.rows) + t, part);
     });
 }
 
@@ -319,56 +427,62 @@ int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, vo
              void* stream) {
     const BackwardRoom r = backward_room(l.T, l.V, l.K, dx.bf16, dw.bf16);
     const bool x = dx.p != nullptr, w = dw.p != nullptr;
+    const int px = x ? r.px : 0, pw = w ? r.pw : 0;
+    auto* turned_x = at<uint16_t>(ws, r.x);
+    auto* turned_w = at<uint16_t>(ws, r.w);
+    auto* ones = at<float>(ws, r.ones);
     for (int64_t v = 0; v < l.V; v += r.piece) {
         const int64_t n = l.V - v < r.piece ? l.V - v : r.piece;
-        const Logits z = logits_of(l, v, n);
+        const bool first = v == 0, last = v + n == l.V;
         Slopes to{};
         to.by_row = at<uint16_t>(ws, r.by_row);
         to.by_class = at<uint16_t>(ws, r.by_class);
         to.row_ld = up(n, kRound) * kRound;
-        to.row_part = l.T * to.row_ld;
         to.class_ld = r.class_ld;
-        to.class_part = n * r.class_ld;
         to.lse = lse;
         to.g = g;
-        to.classes = l.V;
-        const int px = x ? r.px : 0, pw = w ? r.pw : 0;
+        to.scale = at<const float>(ws, r.scale);
+        to.rows = at<float>(ws, r.rows);
+        to.classes = at<float>(ws, r.classes);
+        to.V = l.V;
+        Source of_x{}, of_w{};
+        Scales scales{};
+        if (w && first)
+            of_x = source(l.x.q, l.x.ld, l.T, l.K, turned_x, r.class_ld, pw);
+        if (x) of_w = source(l.w.q + v * l.w.ld, l.w.ld, n, l.K, turned_w, to.row_ld, px);
+        if (first)
+            scales = {l.x, l.w, l.target, g, l.T, l.V, l.K, at<float>(ws, r.scale), ones};
+        if (int e = launch_turn(of_x, of_w, scales, stream)) return e;
+        const Logits z = logits_of(l, v, n);
         const int e = px == 0   ? pw == 1 ? launch_slopes<0, 1>(z, to, l.K, stream)
-                                          : launch_slopes<0, 3>(z, to, l.K, stream)
+                                          : launch_slopes<0, 2>(z, to, l.K, stream)
                       : px == 1 ? pw == 0   ? launch_slopes<1, 0>(z, to, l.K, stream)
                                   : pw == 1 ? launch_slopes<1, 1>(z, to, l.K, stream)
-                                            : launch_slopes<1, 3>(z, to, l.K, stream)
-                      : pw == 0 ? launch_slopes<3, 0>(z, to, l.K, stream)
-                      : pw == 1 ? launch_slopes<3, 1>(z, to, l.K, stream)
-                                : launch_slopes<3, 3>(z, to, l.K, stream);
+                                            : launch_slopes<1, 2>(z, to, l.K, stream)
+                      : pw == 0 ? launch_slopes<2, 0>(z, to, l.K, stream)
+                      : pw == 1 ? launch_slopes<2, 1>(z, to, l.K, stream)
+                                : launch_slopes<2, 2>(z, to, l.K, stream);
         if (e) return e;
-        auto* turned_x = at<uint16_t>(ws, r.x);
-        auto* turned_w = at<uint16_t>(ws, r.w);
-        const Source none{};
-        if (int s = turn(w && v == 0 ? source(l.x.q, l.x.ld, l.T, l.K, r.class_ld, turned_x) : none,
-                         x ? source(l.w.q + v * l.w.ld, l.w.ld, n, l.K, to.row_ld, turned_w) : none,
-                         stream))
-            return s;
         void* slices = at<char>(ws, r.slices);
-        const bool whole = r.piece == l.V;
-        Product of_x{}, of_w{};
+        const bool whole = first && last;
+        Product for_x{}, for_w{};
         if (x)
-            of_x = product_of(to.by_row, to.row_part, turned_w, to.row_ld, l.T, l.K, n, px,
-                             whole ? dx : Mat{nullptr, 0, false}, slices);
+            for_x = product_of(to.by_row, turned_w, px * to.row_ld, l.T, l.K, to.rows, ones,
+                               whole ? dx : Mat{nullptr, 0, false}, slices);
         if (w)
-            of_w = product_of(to.by_class, to.class_part, turned_x, r.class_ld, n, l.K, l.T, pw,
-                             Mat{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4), dw.ld,
-                                 dw.bf16},
-                             slices);
-        if (x && w && whole && both_small(of_x, of_w)) return launch_both(of_x, of_w, stream);
+            for_w = product_of(to.by_class, turned_x, pw * r.class_ld, n, l.K, to.classes, ones,
+                               Mat{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4),
+                                   dw.ld, dw.bf16},
+                               slices);
+        if (x && w && whole && is_small(for_x) && is_small(for_w))
+            return launch_both(for_x, for_w, stream);
         if (x) {
-            if (int s = launch_product(of_x, stream)) return s;
+            if (int s = launch_product(for_x, stream)) return s;
             if (!whole)
-                if (int s = add(r, ws, l, of_x.shape.slices, v == 0, v + n == l.V, dx, stream))
-                    return s;
+                if (int s = add(r, ws, l, for_x.shape.slices, first, last, dx, stream)) return s;
         }
         if (w)
-            if (int s = launch_product(of_w, stream)) return s;
+            if (int s = launch_product(for_w, stream)) return s;
     }
     return 0;
 }

@@ -6,7 +6,6 @@
 // and the WN wavefronts beside each other have the rest of its classes.
 #pragma once
 
-#include "q8_grad_gemm.h"
 #include "q8_xent_stats.h"
 
 namespace cpdp {
@@ -22,14 +21,50 @@ struct Logits {
     int64_t first;
 };
 
-// Where the logits' gradient goes, laid out for the gradients' products.
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Products of fp16 numbers, with fp32 sums (see Gemm).
+struct Half {
+    using Acc = f32x4;
+    using Sum = float;
+    static __device__ __forceinline__ Acc mfma(u32x4 a, u32x4 b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                      __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+
+// two fp32 values as fp16, rounded to nearest-even (the low half is the first)
+__device__ __forceinline__ uint32_t halves(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
+}
+
+constexpr float kSecond = 4096.0f;
+
+// Where the logits' gradient e = exp(z - lse) - [target] goes, laid out for the gradients'
+// products, in fp16 numbers: one for a bf16 result, 11 bits of it; two for an fp32 one, 22
+// bits, the second as a part of its own after the first and 2^12 times as large, so that
+// what is too small for the first is still in it.  8-bit numbers, the other operands, are
+// exact in fp16, and so are they over 2^12, which the second part is multiplied by.
+//   by_row    e w_scale[v] * scale[0]          [rows][parts][row_ld]
+//   by_class  e g[t] x_scale[t] * scale[1]     [classes][parts][class_ld]
+// scale are powers of two that bring the largest |w_scale| and |g x_scale| there are to
+// 2^14 or more and below 2^15.  What fp16 keeps of a number ends at 2^-24: at 2^-38 of that,
+// 2^-50 with two parts, where e itself has an error of 2^-24 at the target.  (In bfloat16
+// numbers, which do not end there, an fp32 result needs three, and its product half as
+// long again.)
+// What the products are then scaled by: rows[t] = g[t] / scale[0], classes[v] = 1 / scale[1].
 struct Slopes {
-    uint16_t* by_row;    // [parts][rows][row_ld]
-    uint16_t* by_class;  // [parts][classes][class_ld]
-    int64_t row_ld, row_part, class_ld, class_part;  // row lengths are whole steps
+    uint16_t* by_row;
+    uint16_t* by_class;
+    int64_t row_ld, class_ld;  // of a part; whole steps
     const float* lse;
     const float* g;
-    int64_t classes;  // of the loss
+    const float* scale;
+    float* rows;
+    float* classes;
+    int64_t V;  // classes of the loss
 };
 
 // Where a tile's findings go: its part of each row's statistics [tile][row] and the
@@ -200,9 +235,8 @@ struct LogitTile {
         if (here) to.hit[m] = hit[threadIdx.x];
     }
 
-    // The gradient of the logits, times g, twice: by rows, each class scaled by w_scale, for
-    // the gradient of x, and by classes, each row scaled by x_scale, for that of w; bf16
-    // numbers in PX and PW parts (0: not wanted), with zeros up to the end of a step.
+    // The gradient of the logits by rows, for the gradient of x, and by classes, for that of
+    // w, in PX and PW parts (0: not wanted), with zeros up to the end of a step.
     template <int PX, int PW>
     static __device__ __forceinline__ void grads(const Logits& l, const Slopes& to,
                                                  int64_t tiles_m, int64_t tiles_n) {
@@ -213,6 +247,13 @@ struct LogitTile {
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
         const int64_t n0 = p.tile.n + p.first;
+        const float scale_w = to.scale[0], scale_x = to.scale[1];
+        if ((int)threadIdx.x < TILE) {
+            const int64_t m = p.tile.m + threadIdx.x, n = p.tile.n + threadIdx.x;
+            if (p.tile.n == 0 && m < l.o.M)
+                to.rows[m] = target(v, (int)threadIdx.x) < 0 ? 0.0f : v.g[threadIdx.x] / scale_w;
+            if (p.tile.m == 0 && n < l.o.N) to.classes[n] = 1.0f / scale_x;
+        }
         float ws[COLS];
 #pragma unroll
         for (int k = 0; k < COLS; ++k) ws[k] = v.w_scale[p.first + k];
@@ -222,8 +263,8 @@ struct LogitTile {
             const int row = p.row + i * 16;
             const int64_t y = target(v, row), m = p.tile.m + row;
             const int at = hot(l, p, y);
-            const float xs = v.x_scale[row], g = v.g[row];
-            const float lse = y >= to.classes ? __builtin_nanf("") : v.lse[row];
+            const float xs = v.x_scale[row], gx = v.g[row] * xs * scale_x;
+            const float lse = y >= to.V ? __builtin_nanf("") : v.lse[row];
             float e[COLS], t[COLS];
 #pragma unroll
             for (int k = 0; k < COLS; ++k)
@@ -234,9 +275,8 @@ struct LogitTile {
             }
 #pragma unroll
             for (int k = 0; k < COLS; ++k) {
-                e[k] *= g;
-                t[k] = e[k] * xs;
-                e[k] *= ws[k];
+                t[k] = e[k] * gx;
+                e[k] *= ws[k] * scale_w;
             }
             const bool counts = y >= 0 && m < l.o.M;
             if (__any(!counts) || p.tile.n + TILE > l.o.N) {
@@ -262,8 +302,8 @@ struct LogitTile {
                     for (int k = 0; k < COLS; k += 2)
                         x[k / 8][k % 8 / 2] = take2<PX>(q, e[k], e[k + 1], finite);
                     if (c0 < to.row_ld)
-                        store_whole(x, to.by_row + q * to.row_part + m0 * to.row_ld + c0,
-                                    to.row_ld, l.o.M - m0, p);
+                        store_whole(x, to.by_row + (m0 * PX + q) * to.row_ld + c0,
+                                    PX * to.row_ld, l.o.M - m0, p);
                 }
             }
         }
@@ -292,7 +332,7 @@ struct LogitTile {
                         *reinterpret_cast<u32x4*>(room + at * kRow + ((piece ^ swap(at)) << 4)) = x;
                     }
                 asm volatile("" ::: "memory");
-                by_classes(l, to, p, room, to.by_class + q * to.class_part);
+                by_classes(l, to, p, room, to.by_class + q * to.class_ld, PW * to.class_ld);
                 asm volatile("" ::: "memory");
             }
         }
@@ -303,7 +343,7 @@ struct LogitTile {
     // pieces (see Turn), so that a store covers 128 bytes of 8 classes and not 64 of 16.
     static __device__ __forceinline__ void by_classes(const Logits& l, const Slopes& to,
                                                       const Place& p, const char* room,
-                                                      uint16_t* out) {
+                                                      uint16_t* out, int64_t ld) {
         constexpr int PIECES = MT % 4 == 0 ? 2 : 1;
         const int64_t t0 = p.tile.m + p.wm * MT * 16;
 #pragma unroll
@@ -320,7 +360,7 @@ struct LogitTile {
                 }
                 const int64_t t = t0 + i * 32 * PIECES;
                 if (t < to.class_ld)
-                    store_whole(x, out + v0 * to.class_ld + t, to.class_ld, l.o.N - v0, p);
+                    store_whole(x, out + v0 * ld + t, ld, l.o.N - v0, p);
             }
         }
     }
@@ -358,23 +398,21 @@ struct LogitTile {
         for (int k = 0; k < COLS; ++k) most = fmaxf(most, fabsf(x[k]));
         return !__any(most == __builtin_inff());
     }
-    // Part q of P of two numbers, which is taken off them: the 24 bits of one are three times
-    // 8, so the first two parts are its first bits as they are, the last is the rest.  With
-    // one part, it is rounded.  A NaN's first bits are one; nothing is left of an infinity.
+    // Part q of P of two numbers, which is taken off them; nothing is left of an infinity.
     template <int P>
     static __device__ __forceinline__ uint32_t take2(int q, float& a, float& b, bool finite) {
-        static_assert(P == 1 || P == 3, "rounded, or exactly");
-        if constexpr (P == 1) return narrow2(a, b);
-        const uint32_t u = __float_as_uint(a), w = __float_as_uint(b);
+        const uint32_t part = halves(a, b);
         if (q + 1 < P) {
-            a -= __uint_as_float(u & 0xffff0000u);
-            b -= __uint_as_float(w & 0xffff0000u);
+            const f16x2 h = __builtin_bit_cast(f16x2, part);
+            const float x = a, y = b;
+            a = (a - (float)h[0]) * kSecond;
+            b = (b - (float)h[1]) * kSecond;
             if (!finite) {
-                a = magnitude(__uint_as_float(u)) == 0x7f800000u ? 0.0f : a;
-                b = magnitude(__uint_as_float(w)) == 0x7f800000u ? 0.0f : b;
+                a = magnitude(x) == 0x7f800000u ? 0.0f : a;
+                b = magnitude(y) == 0x7f800000u ? 0.0f : b;
             }
         }
-        return __builtin_amdgcn_perm(w, u, 0x07060302u);
+        return part;
     }
 };
 

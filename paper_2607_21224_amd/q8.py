@@ -33,7 +33,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libcpdp_q8.so")
 
 CPDP_Q8_MAX_K = 131071
-CPDP_Q8_MAX_T = 4194232
+CPDP_Q8_MAX_T = 2097088
 CPDP_ACT_GELU = 0
 CPDP_ACT_SWIGLU = 1
 ACTIVATIONS = {"gelu": CPDP_ACT_GELU, "swiglu": CPDP_ACT_SWIGLU}

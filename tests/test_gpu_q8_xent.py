@@ -11,10 +11,15 @@ of exp and log.
 * p = exp(z - lse): 3 u Z + lse's error + 3 u (Z + |lse|) + e, relative: call it r.
   d = g (p - 1?): |g| (p r + 3 u (p + 1?)).
 * dx, dw: R u of the terms' sizes for R additions in any order, 4 u for scaling, the terms'
-  own errors; b for terms that are rounded to one bfloat16 number, where the result is
-  bf16, and b for that result's rounding.  What of a scaled d falls below the smallest
-  normal bfloat16 number, 2^-126, the matrix cores take as 0: up to three parts' worth, the
-  first of them the largest, 2^-125 in all, for each term and times |q|.
+  own errors, and what the numbers that hold a term leave out: h = 2^-11, half a step of
+  fp16, once for a bf16 result, squared for an fp32 one; and half the smallest fp16 number,
+  2^-25, where the largest scale, M, is brought to 2^14 or more: 2^-39 M |q| for each term,
+  2^-51 M |q| for an fp32 result, whose second number is held 2^12 times as large.  M is the
+  largest |g x_scale| for dw and, times the row's |g|, the largest |w_scale| for dx.
+  Up to 64 tokens: b for terms that are rounded to one bfloat16 number, and for what falls
+  below the smallest normal one, 2^-126, which the matrix cores take as 0, up to three
+  parts' worth, the first of them the largest: 2^-125 in all, for each term and times |q|.
+  b for a bf16 result's own rounding.
 """
 import math
 
@@ -29,6 +34,7 @@ pytestmark = pytest.mark.gpu
 
 DTYPE = (torch.float32, torch.bfloat16)
 E = 4 * U
+H = 2.0 ** -11
 
 
 class Case:
@@ -100,14 +106,20 @@ class Case:
         hot.scatter_(1, self.target.clamp_min(0)[:, None], 1.0)
         return g * (p - hot), g.abs() * (p * r + 3 * U * (p + hot))
 
-    def check(self, got, d, off, q, scale, dt):
-        """got against d (scale q), d known up to off."""
+    def check(self, got, d, off, q, scale, largest, dt):
+        """got against d (scale q), d known up to off; largest: M, for each row."""
         R, right = d.shape[1], q.double() * scale.double()[:, None]
         want, size = torch.mm(d, right), torch.mm(d.abs(), right.abs())
-        slack = torch.mm(off, right.abs()) + ((B if dt == BF16 else 0.0) + (R + 4) * U) * size
-        if dt == BF16:
+        bf16 = dt == BF16
+        if self.T > 64:
+            held = H if bf16 else H * H
+            floor = 2.0 ** (-39 if bf16 else -51) * largest[:, None]
+        else:
+            held, floor = B if bf16 else 0.0, 2.0 ** -125
+        slack = torch.mm(off, right.abs()) + (held + (R + 4) * U) * size
+        slack = slack + floor * q.double().abs().sum(0)
+        if bf16:
             slack = slack + B * (want.abs() + slack)
-        slack = slack + 2.0 ** -125 * q.double().abs().sum(0)
         off = (got.double() - want).abs()
         bad = (~(off <= slack + 1e-37)).nonzero()
         assert len(bad) == 0, (len(bad), [(i, float(got[i]), float(want[i]), float(slack[i]))
@@ -115,11 +127,14 @@ class Case:
 
     def check_backward(self, dx, dw, dx_dt, dw_dt):
         d, off = self.gradients()
+        g = torch.where(self.counts, self.g.double(), 0.0).abs()
         if dx_dt != NONE:
-            self.check(dx, d, off, self.w, self.ws, dx_dt)
+            self.check(dx, d, off, self.w, self.ws, g * self.ws.double().abs().max(), dx_dt)
             assert not dx[~self.counts].any()
         if dw_dt != NONE:
-            self.check(dw, d.t().contiguous(), off.t().contiguous(), self.x, self.xs, dw_dt)
+            largest = (g * self.xs.double().abs()).max().expand(self.V)
+            self.check(dw, d.t().contiguous(), off.t().contiguous(), self.x, self.xs, largest,
+                       dw_dt)
 
 
 @pytest.mark.parametrize("T,V,K", xent_sizes.SMALL + xent_sizes.MIDDLE + xent_sizes.LARGE)
@@ -245,6 +260,32 @@ def test_steep_and_flat_logits(q8, T):  # noqa: F811
     dx, dw = c.backward(q8, lse, 0, 0)
     off = float((c.xs[c.counts] * c.g[c.counts]).abs().sum()) * 127 * 16 * U
     assert float(dw.abs().max()) <= off
+
+
+@pytest.mark.parametrize("types", xent_sizes.TYPES)
+@pytest.mark.parametrize("T", [5, 100, 700])
+def test_small_probabilities(q8, T, types):  # noqa: F811
+    """Half of the classes have logits some 15 to 70 below the others'."""
+    c = Case(T, 700, 128, size=6.0)
+    c.x[:, :32], c.w[1::2, :32], c.w[::2, :32] = 100, -100, 0
+    loss, lse = c.forward(q8)
+    c.check_forward(loss, lse)
+    c.check_backward(*c.backward(q8, lse, *types), *types)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** -30, 2.0 ** 60])
+def test_weights_of_any_size(q8, scale):  # noqa: F811
+    """Tokens' weights of very small and large sizes scale the gradients and nothing else."""
+    c = Case(100, 700, 128, ignored=0.0)
+    lse = c.forward(q8)[1]
+    c.g.uniform_(0.5, 1.0)
+    want = c.backward(q8, lse, 0, 0)
+    c.g *= scale
+    got = c.backward(q8, lse, 0, 0)
+    for a, b in zip(want, got):
+        normal = a.abs() * scale > 2.0 ** -125
+        assert torch.equal((a * scale)[normal], b[normal])
+        assert bool(((a * scale - b)[~normal].abs() <= 2.0 ** -125).all())
 
 
 def test_logits_past_the_largest_number(q8):  # noqa: F811

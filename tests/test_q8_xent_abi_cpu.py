@@ -91,7 +91,7 @@ def test_overlaps(name, out, other):
 
 @pytest.mark.parametrize("name", CALLS)
 @pytest.mark.parametrize("T,V,K", [(1, 32768, 64), (80, 32, 64), (300, 5000, 64), (5000, 300, 64),
-                                   (4194232, 2, 1)])
+                                   (2097088, 2, 1)])
 def test_workspaces(name, T, V, K):
     sizes = dict(T=T, V=V, K=K)
     need = workspace(name, **sizes)

@@ -14,7 +14,8 @@ def compile_calls(folder, optimise="-O0", sources=None):
     csrc = os.path.join(build.PKG, "csrc")
     paths = [os.path.join(csrc, s) for s in sources or build.Q8_SOURCES + build.XENT_SOURCES]
     paths.append(os.path.join(on_cpu.NATIVE, "on_cpu", "xent_calls.cpp"))
-    include = ["-I", os.path.join(on_cpu.NATIVE, "on_cpu"), "-I",
+    include = ["-I", os.path.join(on_cpu.NATIVE, "on_cpu_xent"), "-I",
+               os.path.join(on_cpu.NATIVE, "on_cpu"), "-I",
                os.path.join(build.ROOT, "include"), "-I", csrc]
     jobs, objects = [], []
     for p in paths:
