@@ -40,7 +40,7 @@ __device__ __forceinline__ uint32_t halves(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
 }
 
-constexpr float kSecond = 4096.0f;
+constexpr float kSecond = 4096.0f;  // (see Slopes)
 
 // Where the logits' gradient e = exp(z - lse) - [target] goes, laid out for the gradients'
 // products, in fp16 numbers: one for a bf16 result, 11 bits of it; two for an fp32 one, 22
@@ -52,8 +52,9 @@ constexpr float kSecond = 4096.0f;
 // scale are powers of two that bring the largest |w_scale| and |g x_scale| there are to
 // 2^14 or more and below 2^15.  What fp16 keeps of a number ends at 2^-24: at 2^-38 of that,
 // 2^-50 with two parts, where e itself has an error of 2^-24 at the target.  (In bfloat16
-// numbers, which do not end there, an fp32 result needs three, and its product half as
-// long again.)
+// numbers, which do not end there, an fp32 result needs three, and its product is half as
+// long again: loss and gradients of 4096 x 65536 x 1024 with fp32 dw took 2820 us, and take
+// 2400.)
 // What the products are then scaled by: rows[t] = g[t] / scale[0], classes[v] = 1 / scale[1].
 struct Slopes {
     uint16_t* by_row;
