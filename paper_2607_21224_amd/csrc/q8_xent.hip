@@ -1,11 +1,11 @@
 // Softmax cross entropy of 8-bit rows over the classes of 8-bit weights, and its
 // gradients, without the logits being kept.
 //
-// More than 64 tokens (fewer: q8_xent_few.hip): tiles of the product of rows and weights whose results are used
-// where they are made (q8_xent_tile.h).  The loss takes one launch over all tiles and
-// one that joins what they found of each token.  Its gradients make the logits again, a
-// piece of the classes at a time, and leave the gradient of them laid out for two
-// products of fp16 numbers.
+// More than 64 tokens (fewer: q8_xent_few.hip): tiles of the product of rows and weights
+// whose results are used where they are made (q8_xent_tile.h).  The loss takes one launch
+// over all tiles, or two, and one that joins what they found of each token.  Its gradients
+// make the logits again, a piece of the classes at a time, and leave the gradient of them
+// laid out for two products of fp16 numbers.
 #include "q8_xent_tile.h"
 
 namespace cpdp {
@@ -69,13 +69,13 @@ Logits logits_of(const Loss& l, int64_t first, int64_t n) {
 }
 
 struct ForwardRoom : Room {
-    int tile;
+    TwoTiles split;
     int64_t tiles, part, hit;
 };
 ForwardRoom forward_room(int64_t T, int64_t V, int64_t K) {
     ForwardRoom r;
-    r.tile = logit_tile(T, V, up(K, kStep), 3500, 0);
-    r.tiles = up(V, r.tile);
+    r.split = logit_tiles(T, V, up(K, kStep), 3500, 0);
+    r.tiles = r.split.first / 256 + up(V - r.split.first, r.split.tile);
     if (r.tiles > 1) {
         r.part = r.take(r.tiles * T * (int64_t)sizeof(Stats));
         r.hit = r.take(T * 4);
@@ -83,24 +83,33 @@ ForwardRoom forward_room(int64_t T, int64_t V, int64_t K) {
     return r;
 }
 
+// Statistics of classes v to v + n, the parts of whose tiles are `at` on
+int launch_stats(const Loss& l, const Found& to, int tile, int64_t at, int64_t v, int64_t n,
+                 void* stream) {
+    return with_tile(tile, [&](auto tile) {
+        const int64_t tm = up(l.T, tile);
+        // (a launch holds fewer than 2^32 work items)
+        const int64_t most = (((int64_t)1 << 32) / threads(tile) - 1) / tm;
+        for (int64_t j = 0; j < n; j += most * tile) {
+            const int64_t left = n - j < most * tile ? n - j : most * tile, tn = up(left, tile);
+            if (int e = launch(xent_stats_kernel<tile, across(tile), buffers(tile)>,
+                               dim3((uint32_t)(tm * tn)), threads(tile), stream,
+                               logits_of(l, v + j, left), to, tm, tn, at + j / tile))
+                return e;
+        }
+        return 0;
+    });
+}
+
 int forward(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
     const ForwardRoom r = forward_room(l.T, l.V, l.K);
     const bool one = r.tiles == 1;
     const Found to{one ? nullptr : at<Stats>(ws, r.part), one ? nullptr : at<float>(ws, r.hit), lse,
                    loss};
-    const int e = with_tile(r.tile, [&](auto tile) {
-        const int64_t tm = up(l.T, tile);
-        // (a launch holds fewer than 2^32 work items)
-        const int64_t most = (((int64_t)1 << 32) / threads(tile) - 1) / tm;
-        for (int64_t j = 0; j < r.tiles; j += most) {
-            const int64_t tn = r.tiles - j < most ? r.tiles - j : most, v = j * tile;
-            const Logits z = logits_of(l, v, l.V - v < tn * tile ? l.V - v : tn * tile);
-            if (int s = launch(xent_stats_kernel<tile, across(tile), buffers(tile)>,
-                               dim3((uint32_t)(tm * tn)), threads(tile), stream, z, to, tm, tn, j))
-                return s;
-        }
-        return 0;
-    });
+    const int64_t first = r.split.first;
+    if (first > 0)
+        if (int e = launch_stats(l, to, 256, 0, 0, first, stream)) return e;
+    const int e = launch_stats(l, to, r.split.tile, first / 256, first, l.V - first, stream);
     if (e || one) return e;
     return launch(xent_join_kernel, dim3((uint32_t)up(l.T, 16)), 256, stream, to.part, to.hit, l.T,
                   r.tiles, l.V, l.target, loss, lse);
@@ -415,7 +424,7 @@ int add(const BackwardRoom& r, void* ws, const Loss& l, int slices, bool first, 
 
 template <int PX, int PW>
 int launch_slopes(const Logits& z, const Slopes& to, int64_t K, void* stream) {
-    return with_tile(logit_tile(z.o.M, z.o.N, up(K, kStep), 0, PX + PW), [&](auto tile) {
+    return with_tile(logit_tile(z.o.M, z.o.N, up(K, kStep), 0, PX + PW).tile, [&](auto tile) {
         const int64_t tm = up(z.o.M, tile), tn = up(z.o.N, tile);
         if (tm * tn * threads(tile) >= (int64_t)1 << 32) return (int)hipErrorInvalidValue;
         return launch(xent_slopes_kernel<tile, across(tile), buffers(tile), PX, PW>,
