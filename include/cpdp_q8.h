@@ -199,8 +199,8 @@ int cpdp_q8_grad_weight(const void* dy, int64_t lddy, int dy_dt, const int8_t* a
  *   dw   p[t, v] * g[t] * x_scale[t]
  * is held in two fp16 numbers for an fp32 result: 22 bits, but with an error of up to
  * 2^-51 of the largest |w_scale|, or of the largest |g * x_scale| of the tokens that count;
- * in one for a bf16 result: 11 bits, and 2^-39 of the largest.  (Up to 64 tokens: in bfloat16 numbers, as the gradients of a
- * product from fp32 dy.)
+ * in one for a bf16 result: 11 bits, and 2^-39 of the largest.  (Up to 64 tokens: in
+ * bfloat16 numbers, as the gradients of a product from fp32 dy.)
  */
 #define CPDP_Q8_MAX_T 2097088 /* 2^21 - 64: rows of sums that a tile can address */
 

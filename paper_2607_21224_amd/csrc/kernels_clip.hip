@@ -6,9 +6,9 @@
 // replica (of all replicas for the mean) and leaves one sum for each; a second one adds
 // them up, and a third scales.  Where the gradients are small, the second is left out:
 // every block of the last adds its replica's sums up by itself, in the same order; and a
-// replica of up to 80 KB is one block's, in one launch.  Squares and sums are fp64: they cannot overflow or lose small values, and
-// cost nothing beside the memory (2 instructions a coordinate of 4 bytes).  There
-// are no atomics; the order of a sum is fixed by the sizes.
+// replica of up to 80 KB is one block's, in one launch.  Squares and sums are fp64: they
+// cannot overflow or lose small values, and cost nothing beside the memory (2 instructions a
+// coordinate of 4 bytes).  There are no atomics; the order of a sum is fixed by the sizes.
 #include "cpdp_device.h"
 
 #include "clip_launch.h"

@@ -37,7 +37,8 @@ class CpdpMultiState:
                              flat(self.mom), flat(self.mom2) if adamw else None,
                              flat(self.grads), self.slow_mom, self.anchor, param_dt)
         self.opt_step = 0
-        self._norms = Norms(self.W, self.table.device)
+        self._norms = Norms(self.W, cpdp.cpdp_grad_norm_plan_workspace(self.plan),
+                            self.table.device)
 
     def init(self, theta0_list, stream=None) -> None:
         """Algorithm 1 initialisation from per-tensor initial values.  The
@@ -57,7 +58,7 @@ class CpdpMultiState:
 
     def grad_norm(self, mean: bool = False, norm=None, stream=None) -> torch.Tensor:
         """The norms of the gradients in self.grads (see CpdpState.grad_norm)."""
-        norm, ws = self._norms(cpdp.cpdp_grad_norm_plan_workspace(self.plan), mean, norm, stream)
+        norm, ws = self._norms(mean, norm, stream)
         cpdp.cpdp_grad_norm_plan(self.plan, norm, ws, cpdp.CPDP_NORM_MEAN if mean else 0,
                                  _on(stream))
         return norm
@@ -66,7 +67,7 @@ class CpdpMultiState:
                    stream=None) -> torch.Tensor:
         """Clip the gradients in self.grads by their norms, over all of a replica's tensors
         together (see CpdpState.clip_grads)."""
-        norm, ws = self._norms(cpdp.cpdp_grad_norm_plan_workspace(self.plan), mean, norm, stream)
+        norm, ws = self._norms(mean, norm, stream)
         cpdp.cpdp_clip_grads_plan(self.plan, max_norm, norm, ws,
                                   cpdp.CPDP_NORM_MEAN if mean else 0, _on(stream))
         return norm

@@ -60,20 +60,19 @@ def _on(stream):
 
 class Norms:
     """The workspace of a state's gradient norms, and the tensors that they go to.  One
-    workspace a state: its calls, and replays of graphs that hold them, do not run at the
-    same time."""
+    workspace a state, allocated with it (a first call may be on any stream): its calls, and
+    replays of graphs that hold them, do not run at the same time."""
 
-    def __init__(self, W: int, device):
-        self.W, self.device, self.workspace = W, device, None
+    def __init__(self, W: int, nbytes: int, device):
+        self.W, self.device = W, device
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
 
-    def __call__(self, nbytes: int, mean: bool, norm, stream) -> tuple:
+    def __call__(self, mean: bool, norm, stream) -> tuple:
         if norm is None:
             # torch ties a new tensor to its current stream
             if stream is not None:
                 raise ValueError("norm: needed where a stream is given")
             norm = torch.empty(1 if mean else self.W, dtype=torch.float32, device=self.device)
-        if self.workspace is None:
-            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return norm, self.workspace
 
 
@@ -176,7 +175,8 @@ class CpdpState:
         self.mom2 = torch.empty_like(self.mom) if adamw else None
         self.opt_step = 0         # optimizer updates applied (AdamW bias correction)
         self._count = None        # device word of count_unsynced
-        self._norms = Norms(self.W, self.params.device)
+        self._norms = Norms(self.W, cpdp.cpdp_grad_norm_workspace(self.W, self.P),
+                            self.params.device)
 
     @property
     def torch_param_dtype(self):
@@ -269,9 +269,10 @@ class CpdpState:
                   stream=None) -> torch.Tensor:
         """The norm of every replica's gradient, (W,) fp32, or with ``mean`` that of
         their mean, (1,): of the gradient a synchronisation step uses.  It goes to the
-        tensor ``norm``, or a new one (on torch's current stream only)."""
+        tensor ``norm``, or a new one (on torch's current stream only).  Calls of one state
+        share a workspace: on two streams, one waits for the other."""
         self._check_grads(grads)
-        norm, ws = self._norms(cpdp.cpdp_grad_norm_workspace(self.W, self.P), mean, norm, stream)
+        norm, ws = self._norms(mean, norm, stream)
         cpdp.cpdp_grad_norm(grads, self.W, self.P, self.ld, norm, ws, self.grad_dt,
                             cpdp.CPDP_NORM_MEAN if mean else 0, _on(stream))
         return norm
@@ -284,7 +285,7 @@ class CpdpState:
         gradient (CPDP synchronisation and DDP steps), each replica's own with local and
         LocalSGD steps."""
         self._check_grads(grads)
-        norm, ws = self._norms(cpdp.cpdp_grad_norm_workspace(self.W, self.P), mean, norm, stream)
+        norm, ws = self._norms(mean, norm, stream)
         cpdp.cpdp_clip_grads(grads, self.W, self.P, self.ld, max_norm, norm, ws, self.grad_dt,
                              cpdp.CPDP_NORM_MEAN if mean else 0, _on(stream))
         return norm

@@ -287,3 +287,21 @@ def test_on_a_stream():
     assert torch.equal(bits(x), bits(want))
     with pytest.raises(ValueError, match="norm"):
         st.clip_grads(x, 3.0, stream=s)
+
+
+@pytest.mark.parametrize("plan", [False, True])
+def test_a_first_call_on_a_stream(plan):
+    """It takes no memory: what torch's current stream still writes to stays out of it."""
+    st = CpdpMultiState(2, [40001, 5]) if plan else CpdpState(2, 40001)
+    of = () if plan else (torch.empty((2, st.ld), device="cuda"),)
+    for t in sum(st.grads, []) if plan else of:
+        t.fill_(1.0)
+    s, norm = torch.cuda.Stream(), torch.empty(2, device="cuda")
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_stats()["allocation.all.allocated"]
+    st.grad_norm(*of, norm=norm, stream=s)
+    st.clip_grads(*of, 3.0, norm=norm, stream=s)
+    assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
+    s.synchronize()
+    want = math.sqrt(40006 if plan else 40001)
+    assert bool(((norm - want).abs() <= 2 * U * want).all())
