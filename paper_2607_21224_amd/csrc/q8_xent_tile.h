@@ -434,13 +434,13 @@ __global__ __launch_bounds__(128 * WN) void xent_slopes_kernel(Logits l, Slopes 
 // which their gradient is written (0: the loss).  Measured on one card, us:
 //                              loss                  gradients, bf16 (2 parts)
 //   tokens, classes, channels  256   128   64        256   128   64
-//   128 x 100 x 384            14.4  8.3   7.3       26.6  17.9  11.8
-//   512 x 4096 x 384           15.6  10.5  7.9       42.6  33.7  30.4
-//   997 x 12345 x 385          20.7  24.5  35.6      79.8  84.0  89.6
-//   256 x 32768 x 1024         21.4  18.2  28.2      111   105   110
-//   2048 x 32768 x 1024        81.4  93.1  157       425   445   519
-//   100 x 50000 x 2048         34.0  26.6  38.7      234   227   226
-//   4096 x 4096 x 2048         34.7  45.0  63.9      168   180   197
+//   128 x 100 x 384            14.2  8.2   7.3       27.1  18.5  12.5
+//   512 x 4096 x 384           15.8  10.3  7.9       42.6  34.3  30.7
+//   997 x 12345 x 385          20.5  24.2  35.1      83.4  87.4  93.5
+//   256 x 32768 x 1024         21.6  17.6  26.6      114   108   112
+//   2048 x 32768 x 1024        76.2  91.9  154       461   475   506
+//   100 x 50000 x 2048         33.4  26.7  36.6      253   245   251
+//   4096 x 4096 x 2048         36.0  44.6  62.9      174   182   198
 struct TileTime {
     int tile;
     double ns;
