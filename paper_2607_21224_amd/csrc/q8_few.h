@@ -7,9 +7,9 @@ namespace cpdp {
 namespace q8 {
 namespace {
 
-// For M <= 16 MT tokens, U steps of a wavefront on their way together.  A block takes 16 channels, from n0 on; its wavefronts take
-// the steps of K in turn, each lane 32 consecutive bytes of a weight row, so a
-// step reads 128 bytes of 16 rows.  Those go to the matrix cores as they are: a
+// For M <= 16 MT tokens, U steps of a wavefront on their way together.  A block takes 16
+// channels, from n0 on; its wavefronts take the steps of K in turn, each lane 32
+// consecutive bytes of a weight row, so a step reads 128 bytes of 16 rows.  Those go to the matrix cores as they are: a
 // sum does not depend on which of its terms an instruction takes together, as
 // long as the tokens' bytes, read from L2, are dealt alike.  The wavefronts'
 // sums meet in LDS, as whole numbers, so their order does not matter: `sums` [wavefront]

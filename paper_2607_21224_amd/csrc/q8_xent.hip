@@ -1,8 +1,9 @@
 // Softmax cross entropy of 8-bit rows over the classes of 8-bit weights, and its
 // gradients, without the logits being kept.
 //
-// More than 64 tokens (fewer: q8_xent_few.hip): tiles of the product of rows and weights
-// whose results are used where they are made (q8_xent_tile.h).  The loss takes one launch
+// Logits are made in tiles of the product of rows and weights, whose results are used where
+// they are made (q8_xent_tile.h); very few tokens' otherwise (q8_xent_few.hip), as are the
+// gradients' products of up to 64.  The loss takes one launch
 // over all tiles, or two, and one that joins what they found of each token.  Its gradients
 // make the logits again, a piece of the classes at a time, and leave the gradient of them
 // laid out for two products of fp16 numbers.
@@ -496,15 +497,31 @@ int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, vo
     return 0;
 }
 
+template <int TILE>
+int few_slopes(const Logits& z, const FewSlopes& to, void* stream) {
+    const int64_t tm = up(z.o.M, TILE), tn = up(z.o.N, TILE);
+    return launch(xent_few_grads_kernel<TILE, across(TILE), buffers(TILE)>,
+                  dim3((uint32_t)(tm * tn)), threads(TILE), stream, z, to, tm, tn);
+}
+
 }  // namespace
 
 int64_t xent_workspace(int64_t T, int64_t V, int64_t K) {
-    return T <= kFewTokens ? few_xent_workspace(T, V, K) : forward_room(T, V, K).bytes;
+    return few_logits(T, K) ? few_xent_workspace(T, V) : forward_room(T, V, K).bytes;
 }
 
 int launch_xent(const Loss& l, float* loss, float* lse, void* workspace, void* stream) {
-    return l.T <= kFewTokens ? launch_few_xent(l, loss, lse, workspace, stream)
-                             : forward(l, loss, lse, workspace, stream);
+    return few_logits(l.T, l.K) ? launch_few_xent(l, loss, lse, workspace, stream)
+                                : forward(l, loss, lse, workspace, stream);
+}
+
+int launch_few_slopes(const Loss& l, int64_t first, int64_t n, const float* lse, const float* g,
+                      float* d, int64_t ld, float* scale, void* stream) {
+    const FewSlopes to{d, ld, lse, g, scale, l.V};
+    const Logits z = logits_of(l, first, n);
+    // (tiles of 256 would be mostly empty)
+    return logit_tile(l.T, n, up(l.K, kStep), 0, 1).tile == 64 ? few_slopes<64>(z, to, stream)
+                                                               : few_slopes<128>(z, to, stream);
 }
 
 int64_t xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {

@@ -1,6 +1,6 @@
-// The loss of up to 64 tokens, and its gradients.  What it costs is reading the weights:
-// once for the loss, and for the gradients once for the logits' gradient, which is small
-// and kept in fp32, and once more for dx.
+// The loss of few tokens (see few_logits), and the gradients of up to 64.  What they cost is
+// reading the weights: once for the loss, and for the gradients once for the logits'
+// gradient, which is small and kept in fp32, and once more for dx.
 #include "q8_few.h"
 #include "q8_xent_stats.h"
 
@@ -12,21 +12,20 @@ constexpr int kClasses = 16;  // of a block (see few_sums)
 
 // A block's classes: each token's largest logit and sum of exp's, part [token][block], and
 // the target's logit of the tokens that have it here.
-template <int MT>
-__global__ __launch_bounds__(1024, MT == 1 ? 8 : 4) void xent_few_stats_kernel(Held x, Held w,
-                                                              const int64_t* target, int M,
-                                                              int64_t V, int K, int64_t first,
-                                                              int64_t blocks, Stats* part,
-                                                              float* hit) {
-    __shared__ FewSums<MT> sums;
+__global__ __launch_bounds__(1024, 8) void xent_few_stats_kernel(Held x, Held w,
+                                                                 const int64_t* target, int M,
+                                                                 int64_t V, int K, int64_t first,
+                                                                 int64_t blocks, Stats* part,
+                                                                 float* hit) {
+    __shared__ FewSums<1> sums;
     const int waves = blockDim.x >> 6;
     const int64_t block = first + blockIdx.x, n0 = block * kClasses;
-    few_sums<MT, 2>(x.q, x.ld, w.q, w.ld, M, V, K, n0, sums);
+    few_sums<1, 2>(x.q, x.ld, w.q, w.ld, M, V, K, n0, sums);
     const int64_t n = n0 + threadIdx.x % kClasses, from = n < V ? n : V - 1;
     const float ws = w.scale[from];
-    for (int e = threadIdx.x; e < MT * 256; e += blockDim.x) {
+    for (int e = threadIdx.x; e < 256; e += blockDim.x) {
         const int m = e / kClasses, at = m < M ? m : M - 1;
-        float z = (float)few_sum<MT>(sums, e, waves) * x.scale[at] * ws;
+        float z = (float)few_sum<1>(sums, e, waves) * x.scale[at] * ws;
         if (n >= V) z = -__builtin_inff();
         if (m < M && n < V && n == target[m]) hit[m] = z;
         Stats s = {z, exp_of(z - pivot(z))};
@@ -59,27 +58,26 @@ __global__ __launch_bounds__(1024) void xent_few_join_kernel(const Stats* part, 
 
 // The logits' gradient, d [M x N] for N classes from `first` on, and the tokens' scales
 // with 0 for those that do not count.
-template <int MT>
 __global__ __launch_bounds__(1024) void xent_few_slopes_kernel(Held x, Held w,
                                                                const int64_t* target, int M,
                                                                int64_t N, int K, int64_t first,
                                                                int64_t V, const float* lse,
                                                                const float* g, float* d,
                                                                int64_t ld, float* scale) {
-    __shared__ FewSums<MT> sums;
+    __shared__ FewSums<1> sums;
     const int waves = blockDim.x >> 6;
     const int64_t n0 = (int64_t)blockIdx.x * kClasses;
-    few_sums<MT, 2>(x.q, x.ld, w.q, w.ld, M, N, K, n0, sums);
+    few_sums<1, 2>(x.q, x.ld, w.q, w.ld, M, N, K, n0, sums);
     if (blockIdx.x == 0 && (int)threadIdx.x < M)
         scale[threadIdx.x] = target[threadIdx.x] < 0 ? 0.0f : x.scale[threadIdx.x];
     const int64_t n = n0 + threadIdx.x % kClasses;
     if (n >= N) return;
     const float ws = w.scale[n];
-    for (int e = threadIdx.x; e < MT * 256; e += blockDim.x) {
+    for (int e = threadIdx.x; e < 256; e += blockDim.x) {
         const int m = e / kClasses;
         if (m >= M) break;
         const int64_t y = target[m];
-        const float z = (float)few_sum<MT>(sums, e, waves) * x.scale[m] * ws;
+        const float z = (float)few_sum<1>(sums, e, waves) * x.scale[m] * ws;
         const float l = y >= V ? __builtin_nanf("") : lse[m];
         const float v = g[m] * (exp_of(z - l) - (first + n == y ? 1.0f : 0.0f));
         d[m * ld + n] = y < 0 ? 0.0f : v;
@@ -98,14 +96,6 @@ __global__ __launch_bounds__(256) void xent_few_add_kernel(float* sum, const flo
         else if (out.bf16) narrow(x, static_cast<uint16_t*>(out.c) + t * out.ldc + k);
         else static_cast<float*>(out.c)[t * out.ldc + k] = x;
     }
-}
-
-// f(16-token groups)
-template <class F>
-int with_groups(int64_t T, F f) {
-    if (T <= 16) return f(Int<1>());
-    if (T <= 32) return f(Int<2>());
-    return f(Int<4>());
 }
 
 struct ForwardRoom : Room {
@@ -156,7 +146,7 @@ BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
 
 }  // namespace
 
-int64_t few_xent_workspace(int64_t T, int64_t V, int64_t) { return forward_room(T, V).bytes; }
+int64_t few_xent_workspace(int64_t T, int64_t V) { return forward_room(T, V).bytes; }
 
 int launch_few_xent(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
     const ForwardRoom r = forward_room(l.T, l.V);
@@ -165,12 +155,10 @@ int launch_few_xent(const Loss& l, float* loss, float* lse, void* ws, void* stre
     const int64_t most = (int64_t)1 << 21;
     for (int64_t b = 0; b < r.blocks; b += most) {
         const int64_t n = r.blocks - b < most ? r.blocks - b : most;
-        const int e = with_groups(l.T, [&](auto mt) {
-            return launch(xent_few_stats_kernel<mt>, dim3((uint32_t)n), 64 * waves, stream, l.x, l.w,
-                          l.target, (int)l.T, l.V, (int)l.K, b, r.blocks, at<Stats>(ws, r.part),
-                          at<float>(ws, r.hit));
-        });
-        if (e) return e;
+        if (int e = launch(xent_few_stats_kernel, dim3((uint32_t)n), 64 * waves, stream, l.x, l.w,
+                           l.target, (int)l.T, l.V, (int)l.K, b, r.blocks, at<Stats>(ws, r.part),
+                           at<float>(ws, r.hit)))
+            return e;
     }
     return launch(xent_few_join_kernel, dim3((uint32_t)l.T), 1024, stream, at<Stats>(ws, r.part),
                   r.blocks, at<float>(ws, r.hit), l.V, l.target, loss, lse);
@@ -190,11 +178,13 @@ int launch_few_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx,
     for (int64_t v = 0; v < l.V; v += r.piece) {
         const int64_t n = l.V - v < r.piece ? l.V - v : r.piece;
         const Held w{l.w.q + v * l.w.ld, l.w.ld, l.w.scale + v};
-        const int e = with_groups(l.T, [&](auto mt) {
-            return launch(xent_few_slopes_kernel<mt>, dim3((uint32_t)up(n, kClasses)),
-                          64 * few_waves(l.K), stream, l.x, w, l.target, (int)l.T, n, (int)l.K, v,
-                          l.V, lse, g, static_cast<float*>(d.p), r.ld, x.scale);
-        });
+        auto* scale = at<float>(ws, r.scale);
+        const int e = few_logits(l.T, l.K)
+                          ? launch(xent_few_slopes_kernel, dim3((uint32_t)up(n, kClasses)),
+                                   64 * few_waves(l.K), stream, l.x, w, l.target, (int)l.T, n,
+                                   (int)l.K, v, l.V, lse, g, static_cast<float*>(d.p), r.ld, scale)
+                          : launch_few_slopes(l, v, n, lse, g, static_cast<float*>(d.p), r.ld,
+                                              scale, stream);
         if (e) return e;
         if (dx.p != nullptr) {
             const Mat part{at<float>(ws, r.part), r.ldk, false};

@@ -68,6 +68,17 @@ struct Slopes {
     int64_t V;  // classes of the loss
 };
 
+// Where it goes for few tokens: d[t, v] = e g[t], fp32, 0 for tokens that do not count, and
+// their scales, 0 for those.
+struct FewSlopes {
+    float* d;
+    int64_t ld;
+    const float* lse;
+    const float* g;
+    float* scale;
+    int64_t V;  // classes of the loss
+};
+
 // Where a tile's findings go: its part of each row's statistics [tile][row] and the
 // targets' logits; or, without parts, the loss.
 struct Found {
@@ -115,12 +126,14 @@ struct LogitTile {
         uint32_t target[2][TILE];  // halves
         float lse[TILE], g[TILE];
     };
-    static __device__ __forceinline__ void send(const Logits& l, const Slopes* to, const Place& p,
-                                                Vectors& v) {
+    // (without SLOPES no lse and g)
+    template <bool SLOPES>
+    static __device__ __forceinline__ void send(const Logits& l, const float* lse, const float* g,
+                                                const Place& p, Vectors& v) {
         constexpr int kEach = TILE / 64;
-        const int count = (to != nullptr ? 6 : 4) * kEach;
+        constexpr int count = (SLOPES ? 6 : 4) * kEach;
 #pragma unroll
-        for (int j = 0; j < (6 * kEach + kWaves - 1) / kWaves; ++j) {
+        for (int j = 0; j < (count + kWaves - 1) / kWaves; ++j) {
             const int k = j * kWaves + p.wave;
             if (k >= count) break;
             const int what = k / kEach, at = k % kEach * 64;
@@ -131,9 +144,9 @@ struct LogitTile {
             const void* from = what == 0   ? static_cast<const void*>(l.x_scale + m)
                                : what == 1 ? static_cast<const void*>(l.w_scale + n)
                                : what == 2 ? static_cast<const void*>(half)
-                               : what == 3 ? static_cast<const void*>(half + 1)
-                               : what == 4 ? static_cast<const void*>(to->lse + m)
-                                           : static_cast<const void*>(to->g + m);
+                               : !SLOPES || what == 3 ? static_cast<const void*>(half + 1)
+                               : what == 4            ? static_cast<const void*>(lse + m)
+                                                      : static_cast<const void*>(g + m);
             __builtin_amdgcn_global_load_lds(
                 (__attribute__((address_space(1))) void*)(from),
                 (__attribute__((address_space(3))) void*)(reinterpret_cast<char*>(&v) +
@@ -178,7 +191,7 @@ struct LogitTile {
         __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
         Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
-        send(l, nullptr, p, v);
+        send<false>(l, nullptr, nullptr, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
         float ws[COLS];
@@ -244,7 +257,7 @@ struct LogitTile {
         __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
         Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
-        send(l, &to, p, v);
+        send<true>(l, to.lse, to.g, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
         const int64_t n0 = p.tile.n + p.first;
@@ -339,6 +352,50 @@ struct LogitTile {
         }
     }
 
+    // The gradient of few tokens' logits.
+    static __device__ __forceinline__ void few_grads(const Logits& l, const FewSlopes& to,
+                                                     int64_t tiles_m, int64_t tiles_n) {
+        __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
+        Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
+        const Place p = place(tiles_m, tiles_n);
+        send<true>(l, to.lse, to.g, p, v);
+        i32x4 acc[MT][NT] = {};
+        sums(l, p, lds, acc);
+        if (p.tile.n == 0 && (int)threadIdx.x < TILE && p.tile.m + threadIdx.x < l.o.M)
+            to.scale[p.tile.m + threadIdx.x] =
+                target(v, (int)threadIdx.x) < 0 ? 0.0f : v.x_scale[threadIdx.x];
+        const int64_t n0 = p.tile.n + p.first;
+        float ws[COLS];
+#pragma unroll
+        for (int k = 0; k < COLS; ++k) ws[k] = v.w_scale[p.first + k];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int row = p.row + i * 16;
+            const int64_t y = target(v, row), m = p.tile.m + row;
+            const int at = hot(l, p, y);
+            const float xs = v.x_scale[row], g = v.g[row];
+            const float lse = y >= to.V ? __builtin_nanf("") : v.lse[row];
+            float e[COLS];
+#pragma unroll
+            for (int k = 0; k < COLS; ++k)
+                e[k] = exp_of((float)acc[i][k / 4][k % 4] * xs * ws[k] - lse);
+            if (__any(at >= 0)) {
+#pragma unroll
+                for (int k = 0; k < COLS; ++k) e[k] = k == at ? e[k] - 1.0f : e[k];
+            }
+            if (m >= l.o.M) continue;
+            float* d = to.d + m * to.ld + n0;
+#pragma unroll
+            for (int k = 0; k < COLS; k += 4) {
+                const float a = g * e[k], b = g * e[k + 1], c = g * e[k + 2], h = g * e[k + 3];
+                // (rows are whole pieces)
+                if (n0 + k < l.o.N)
+                    *reinterpret_cast<f32x4*>(d + k) =
+                        y < 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : f32x4{a, b, c, h};
+            }
+        }
+    }
+
     // Stores a part by classes.  16 lanes read 4 rows of 16 classes, and each gets one
     // class' 4 rows; two reads are 8 rows, 16 bytes.  With 64 rows, the lanes exchange
     // pieces (see Turn), so that a store covers 128 bytes of 8 classes and not 64 of 16.
@@ -427,6 +484,13 @@ template <int TILE, int WN, int S, int PX, int PW>
 __global__ __launch_bounds__(128 * WN) void xent_slopes_kernel(Logits l, Slopes to,
                                                                int64_t tiles_m, int64_t tiles_n) {
     LogitTile<TILE, WN, S>::template grads<PX, PW>(l, to, tiles_m, tiles_n);
+}
+
+template <int TILE, int WN, int S>
+__global__ __launch_bounds__(128 * WN) void xent_few_grads_kernel(Logits l, FewSlopes to,
+                                                                  int64_t tiles_m,
+                                                                  int64_t tiles_n) {
+    LogitTile<TILE, WN, S>::few_grads(l, to, tiles_m, tiles_n);
 }
 
 // Rows and classes of the tile that some logits are made in: 256, 128 or 64, whichever
