@@ -237,18 +237,21 @@ __device__ __forceinline__ void store_rows(const Target& t, int64_t m, int64_t n
 }
 
 // The tile of a block.  Blocks are dealt to the 8 XCDs in turn; each XCD takes a
-// run of consecutive tiles, and those go down 8 rows of tiles before the next
-// column, so that the tiles an XCD works on share rows of A and B in its L2.
+// run of consecutive tiles, one slice of K after the other, and those go down 8 rows of
+// tiles before the next column, so that the tiles an XCD works on share rows of A and B in
+// its L2.  (Every XCD in every slice: dx of 300 x 32003 x 257 51 us, and 41 so; of 997 x
+// 12345 x 385 fp32 with dw 126 and 116.)
 struct TileAt {
     int64_t m, n;
     int slice;
 };
-__device__ __forceinline__ TileAt tile_at(int64_t tiles_m, int64_t tiles_n, int BM, int BN) {
-    const int64_t tiles = tiles_m * tiles_n;
-    const int64_t b = blockIdx.x, slice = b / tiles;
-    int64_t t = b % tiles;
-    const int64_t each = tiles / 8, rest = tiles % 8, xcd = t % 8;
-    t = xcd * each + (xcd < rest ? xcd : rest) + t / 8;
+__device__ __forceinline__ TileAt tile_at(int64_t tiles_m, int64_t tiles_n, int BM, int BN,
+                                          int slices = 1) {
+    const int64_t tiles = tiles_m * tiles_n, blocks = tiles * slices, b = blockIdx.x;
+    const int64_t each = blocks / 8, rest = blocks % 8, xcd = b % 8;
+    int64_t t = xcd * each + (xcd < rest ? xcd : rest) + b / 8;
+    const int64_t slice = t / tiles;
+    t -= slice * tiles;
     const int64_t band = t / (8 * tiles_n);
     const int64_t high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
     const int64_t in = t - band * 8 * tiles_n;
@@ -489,7 +492,7 @@ struct Gemm {
         __shared__ __attribute__((aligned(1024))) char lds[S * kBuffer];
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int lane = threadIdx.x & 63;
-        const TileAt tile = tile_at(tiles_m, tiles_n, BM, BN);
+        const TileAt tile = tile_at(tiles_m, tiles_n, BM, BN, slices);
         const Loads l = loads(o, tile.m, tile.n, wave, lane);
         const char* a0 = o.a + tile.m * o.lda;
         const char* b0 = o.b + tile.n * o.ldb;

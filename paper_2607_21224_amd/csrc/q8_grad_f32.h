@@ -191,7 +191,7 @@ struct F32Gemm {
         __shared__ __attribute__((aligned(1024))) char lds[S * kBuffer];
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-        const TileAt tile = tile_at(tiles_m, tiles_n, kTile, kTile);
+        const TileAt tile = tile_at(tiles_m, tiles_n, kTile, kTile, slices);
         const Offsets l = offsets(o, tile, wave, lane);
         const char* a0 = o.a + (DOWN ? tile.m * 4 : tile.m * o.lda);
         const char* b0 = o.b + tile.n * o.ldb;

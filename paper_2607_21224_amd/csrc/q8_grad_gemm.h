@@ -271,7 +271,7 @@ struct GradGemm {
         __shared__ __attribute__((aligned(1024))) char lds[S * kBuffer];
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int lane = threadIdx.x & 63;
-        const TileAt tile = tile_at(tiles_m, tiles_n, BM, BN);
+        const TileAt tile = tile_at(tiles_m, tiles_n, BM, BN, slices);
         const Offsets l = offsets(o, tile, wave, lane);
         // DOWN: a step is 64 rows on, and the tile's columns begin at its first
         const char* a0 = o.a + (ADOWN ? tile.m * 2 : tile.m * o.lda);
