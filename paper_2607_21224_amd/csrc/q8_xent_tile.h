@@ -41,6 +41,16 @@ __device__ __forceinline__ uint32_t halves(float a, float b) {
 }
 
 constexpr float kSecond = 4096.0f;  // (see Slopes)
+constexpr int kLargest = 32;
+
+// the power of two that brings x into [2^14, 2^15), as far as that and its inverse are
+// normal numbers
+__device__ __forceinline__ float scale_for(float x) {
+    if (x == 0.0f) return 1.0f;
+    const int e = (int)(__float_as_uint(x) >> 23) - 127;  // (below 2^-126: -127)
+    const int up = 14 - e;
+    return __uint_as_float((uint32_t)((up > 126 ? 126 : up) + 127) << 23);
+}
 
 // Where the logits' gradient e = exp(z - lse) - [target] goes, laid out for the gradients'
 // products, in fp16 numbers: one for a bf16 result, 11 bits of it; two for an fp32 one, 22
@@ -49,8 +59,8 @@ constexpr float kSecond = 4096.0f;  // (see Slopes)
 // exact in fp16, and so are they over 2^12, which the second part is multiplied by.
 //   by_row    e w_scale[v] * scale[0]          [rows][parts][row_ld]
 //   by_class  e g[t] x_scale[t] * scale[1]     [classes][parts][class_ld]
-// scale are powers of two that bring the largest |w_scale| and |g x_scale| there are to
-// 2^14 or more and below 2^15.  What fp16 keeps of a number ends at 2^-24: at 2^-38 of that,
+// scale are powers of two that bring the largest |w_scale| and |g x_scale| there are, found
+// from those of up to 32 parts, to 2^14 or more and below 2^15.  What fp16 keeps of a number ends at 2^-24: at 2^-38 of that,
 // 2^-50 with two parts, where e itself has an error of 2^-24 at the target.  (In bfloat16
 // numbers, which do not end there, an fp32 result needs three, and its product is half as
 // long again: loss and gradients of 4096 x 65536 x 1024 with fp32 dw took 2820 us, and take
@@ -62,7 +72,7 @@ struct Slopes {
     int64_t row_ld, class_ld;  // of a part; whole steps
     const float* lse;
     const float* g;
-    const float* scale;
+    const float* largest;  // [2][kLargest]
     float* rows;
     float* classes;
     int64_t V;  // classes of the loss
@@ -125,11 +135,18 @@ struct LogitTile {
         float x_scale[TILE], w_scale[TILE];
         uint32_t target[2][TILE];  // halves
         float lse[TILE], g[TILE];
+        float largest[2 * kLargest];
     };
-    // (without SLOPES no lse and g)
+    static_assert(2 * kLargest == 64, "a load of a wavefront");
+    // (without SLOPES no lse and g; `largest` may be null)
     template <bool SLOPES>
     static __device__ __forceinline__ void send(const Logits& l, const float* lse, const float* g,
-                                                const Place& p, Vectors& v) {
+                                                const float* largest, const Place& p, Vectors& v) {
+        if constexpr (SLOPES)
+            if (p.wave == 0 && largest != nullptr)
+                __builtin_amdgcn_global_load_lds(
+                    (__attribute__((address_space(1))) void*)(largest + p.lane),
+                    (__attribute__((address_space(3))) void*)(v.largest), 4, 0, 0);
         constexpr int kEach = TILE / 64;
         constexpr int count = (SLOPES ? 6 : 4) * kEach;
 #pragma unroll
@@ -191,7 +208,7 @@ struct LogitTile {
         __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
         Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
-        send<false>(l, nullptr, nullptr, p, v);
+        send<false>(l, nullptr, nullptr, nullptr, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
         float ws[COLS];
@@ -257,11 +274,19 @@ struct LogitTile {
         __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
         Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
-        send<true>(l, to.lse, to.g, p, v);
+        send<true>(l, to.lse, to.g, to.largest, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
         const int64_t n0 = p.tile.n + p.first;
-        const float scale_w = to.scale[0], scale_x = to.scale[1];
+        float largest = v.largest[p.lane];
+#pragma unroll
+        for (int off = 1; off < kLargest; off <<= 1)
+            largest = fmaxf(largest, __shfl_xor(largest, off));
+        const float other = __shfl_xor(largest, kLargest);  // (the first lane's: of g x_scale)
+        const float scale_w = scale_for(__uint_as_float(
+            __builtin_amdgcn_readfirstlane(__float_as_uint(largest))));
+        const float scale_x = scale_for(__uint_as_float(
+            __builtin_amdgcn_readfirstlane(__float_as_uint(other))));
         if ((int)threadIdx.x < TILE) {
             const int64_t m = p.tile.m + threadIdx.x, n = p.tile.n + threadIdx.x;
             if (p.tile.n == 0 && m < l.o.M)
@@ -358,7 +383,7 @@ struct LogitTile {
         __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
         Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
-        send<true>(l, to.lse, to.g, p, v);
+        send<true>(l, to.lse, to.g, nullptr, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
         if (p.tile.n == 0 && (int)threadIdx.x < TILE && p.tile.m + threadIdx.x < l.o.M)
