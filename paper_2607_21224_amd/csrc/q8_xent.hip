@@ -257,16 +257,16 @@ int64_t piece_of(int64_t T, int64_t V) {
 }
 
 // Whether a product is small: tiles that find a CU each, and few steps.  What it takes is
-// mostly its launch, and two of them are made in one (128 x 100 x 384: gradients in 13.0 us,
-// and 18.1 with two).
+// mostly its launch, and two of them are made in one (128 x 100 x 384: gradients in 13 us,
+// and 18 with two).
 bool small(int64_t M, int64_t N, int64_t steps) {
     return up(M, 64) * up(N, 64) <= kCus / 2 && steps <= 16;
 }
 // The tile of a gradient's product, and the slices that its sum is cut into where there are
 // fewer tiles than CUs.  A step of a tile takes what it takes in shape_of; here the large
 // tiles are cut, too: dx of 4096 x 1024 over 32768 classes has 64 tiles of 256 x 256, and is
-// made in 4 slices (with dw: 750 us in bf16, 1415 in fp32; in tiles of 128 x 128 and 256 x
-// 128 844 and 1548).
+// made in 4 slices (with dw an eighth less time than in tiles of 128 x 128 and 256 x 128,
+// 750 and 844 us in bf16).
 Shape product_shape(int64_t M, int64_t N, int64_t steps) {
     if (small(M, N, steps)) return {64, 64, 1, 0};
     struct {

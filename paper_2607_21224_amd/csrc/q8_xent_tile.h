@@ -63,8 +63,8 @@ __device__ __forceinline__ float scale_for(float x) {
 // from those of up to 32 parts, to 2^14 or more and below 2^15.  What fp16 keeps of a number ends at 2^-24: at 2^-38 of that,
 // 2^-50 with two parts, where e itself has an error of 2^-24 at the target.  (In bfloat16
 // numbers, which do not end there, an fp32 result needs three, and its product is half as
-// long again: loss and gradients of 4096 x 65536 x 1024 with fp32 dw took 2820 us, and take
-// 2400.)
+// long again: loss and gradients of 4096 x 65536 x 1024 with fp32 dw 2820 us, and 2400 when
+// this was all that changed.)
 // What the products are then scaled by: rows[t] = g[t] / scale[0], classes[v] = 1 / scale[1].
 struct Slopes {
     uint16_t* by_row;
@@ -526,13 +526,13 @@ __global__ __launch_bounds__(128 * WN) void xent_few_grads_kernel(Logits l, FewS
 // which their gradient is written (0: the loss).  Measured on one card, us:
 //                              loss                  gradients, bf16 (2 parts)
 //   tokens, classes, channels  256   128   64        256   128   64
-//   128 x 100 x 384            14.2  8.2   7.3       27.1  18.5  12.5
-//   512 x 4096 x 384           15.8  10.3  7.9       42.6  34.3  30.7
-//   997 x 12345 x 385          20.5  24.2  35.1      83.4  87.4  93.5
-//   256 x 32768 x 1024         21.6  17.6  26.6      114   108   112
-//   2048 x 32768 x 1024        76.2  91.9  154       461   475   506
-//   100 x 50000 x 2048         33.4  26.7  36.6      253   245   251
-//   4096 x 4096 x 2048         36.0  44.6  62.9      174   182   198
+//   128 x 100 x 384            14.5  8.3   7.3       27.5  19.0  13.6
+//   512 x 4096 x 384           16.2  10.4  8.4       40.8  31.4  28.7
+//   997 x 12345 x 385          21.2  24.4  34.9      78.5  81.0  89.2
+//   256 x 32768 x 1024         21.8  17.9  26.9      111   107   112
+//   2048 x 32768 x 1024        78.4  91.5  152       424   423   481
+//   100 x 50000 x 2048         33.2  26.6  36.7      241   235   242
+//   4096 x 4096 x 2048         35.8  43.6  62.2      177   182   200
 struct TileTime {
     int tile;
     double ns;
