@@ -192,9 +192,9 @@ int cpdp_q8_grad_weight(const void* dy, int64_t lddy, int dy_dt, const int8_t* a
  * whatever its x and g hold.  One whose target is V or more has a NaN for its loss, its
  * row of dx and all of dw.  dx [T x K] in dx_dt, dw [V x K] in dw_dt; either may be NULL
  * and is then not computed.
- * 0 <= T <= CPDP_Q8_MAX_T, 1 <= K <= CPDP_Q8_MAX_K.  Logits are exact sums, scaled in
- * fp32, and everything that is taken of them is fp32.  The gradients' products have fp32
- * sums.  What they sum, with p the factor of g in d:
+ * 0 <= T <= CPDP_Q8_MAX_T, 1 <= V <= 2^31 - 9, 1 <= K <= CPDP_Q8_MAX_K.  Logits are exact
+ * sums, scaled in fp32, and everything that is taken of them is fp32.  The gradients'
+ * products have fp32 sums.  What they sum, with p the factor of g in d:
  *   dx   p[t, v] * w_scale[v], each sum times g[t]
  *   dw   p[t, v] * g[t] * x_scale[t]
  * is held in two fp16 numbers for an fp32 result: 22 bits, but with an error of up to

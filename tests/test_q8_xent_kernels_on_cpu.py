@@ -58,3 +58,20 @@ def test_every_kernel_is_reached(tmp_path):
                 taken.add(names[k])
     left = sorted((wanted | products) - taken)
     assert not left, "\n".join(left)
+
+
+def test_launches_fit_a_grid(tmp_path):
+    """At the ends of the sizes, as far as a card holds them: no launch of 2^32 work items."""
+    exe = xent_on_cpu.compile_calls(str(tmp_path))
+    some = ["xent 2097088 2 1", "xent 2097088 131072 8", "xent 70 2000000000 8",
+            "xent 64 2000000000 16", "xent 1 2147483639 16", "xent 17 2000000 131071",
+            "xent_bwd 2097088 131072 8 0 0", "xent_bwd 2097088 200000 8 1 1",
+            "xent_bwd 65 2000000 64 0 0", "xent_bwd 1 1000000000 16 0 0",
+            "xent_bwd 16 100000000 2000 0 0", "xent_bwd 64 100000000 1024 1 0",
+            "xent_bwd 70 90000000 8 0 1", "xent_bwd 1000000 1 16384 0 0"]
+    r = subprocess.run([exe, "note"], input="\n".join(some) + "\n", capture_output=True,
+                       text=True, timeout=300)
+    lines = r.stdout.splitlines()
+    assert r.returncode == 0 and len(lines) == len(some)
+    for call, line in zip(some, lines):
+        assert line.split()[0] == "0" and "too large" not in line, (call, line[:80])
