@@ -31,12 +31,13 @@ __device__ __forceinline__ Stats join(Stats a, Stats b) {
     return {top, a.sum * exp_of(a.top - p) + b.sum * exp_of(b.top - p)};
 }
 
-// lse and loss from all of a row's logits; hit: its target's
+// lse and loss from all of a row's logits; hit: its target's.  (lse - hit would lose of log(sum)
+// what lse has no bits for: all of a loss below 2^-24 |lse|.)
 __device__ __forceinline__ void write_loss(Stats s, float hit, int64_t y, int64_t V, float* lse,
                                            float* loss) {
-    const float l = s.top + logf(s.sum);
-    *lse = l;
-    *loss = y < 0 ? 0.0f : l - (y < V ? hit : __builtin_nanf(""));
+    const float more = logf(s.sum);
+    *lse = s.top + more;
+    *loss = y < 0 ? 0.0f : (s.top - (y < V ? hit : __builtin_nanf(""))) + more;
 }
 
 // Takes parts of a workspace, each on a 256-byte boundary.
