@@ -192,8 +192,16 @@ int cpdp_q8_grad_weight(const void* dy, int64_t lddy, int dy_dt, const int8_t* a
  * whatever its x and g hold.  One whose target is V or more has a NaN for its loss, its
  * row of dx and all of dw.  dx [T x K] in dx_dt, dw [V x K] in dw_dt; either may be NULL
  * and is then not computed.
+ * The _miss calls are the same, and hand on, [T] fp32,
+ *   miss[t] = 1 - exp(-loss[t])   what the target's probability lacks of 1
+ * (0 for a token that does not count, NaN for a target of V or more), from which
+ * cpdp_q8_xent_miss_bwd takes -g * miss for the target's d.  cpdp_q8_xent_bwd takes
+ * g * (exp(z - lse) - 1) there, of the lse that was rounded to fp32: it is off by up to |lse| *
+ * 2^-24 |g|, all that there is of it for a token whose loss is below |lse| * 2^-24.
  * 0 <= T <= CPDP_Q8_MAX_T, 1 <= V <= 2^31 - 9, 1 <= K <= CPDP_Q8_MAX_K.  Logits are exact
- * sums, scaled in fp32, and everything that is taken of them is fp32.  The gradients'
+ * sums, scaled in fp32, and everything that is taken of them is fp32; a loss is the sum of
+ * (the largest logit - the target's) and the logarithm, so its error does not grow with lse,
+ * while that of a probability, relative, does: |lse| * 2^-24.  The gradients'
  * products have fp32 sums.  What they sum, with p the factor of g in d:
  *   dx   p[t, v] * w_scale[v], each sum times g[t]
  *   dw   p[t, v] * g[t] * x_scale[t]
@@ -208,12 +216,22 @@ int64_t cpdp_q8_xent_workspace(int64_t T, int64_t V, int64_t K);
 int cpdp_q8_xent(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw,
                  const float* w_scale, const int64_t* target, int64_t T, int64_t V, int64_t K,
                  float* loss, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+int cpdp_q8_xent_miss(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w,
+                      int64_t ldw, const float* w_scale, const int64_t* target, int64_t T,
+                      int64_t V, int64_t K, float* loss, float* lse, float* miss, void* workspace,
+                      int64_t workspace_bytes, void* stream);
 int64_t cpdp_q8_xent_bwd_workspace(int64_t T, int64_t V, int64_t K, int dx_dt, int dw_dt);
 int cpdp_q8_xent_bwd(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w,
                      int64_t ldw, const float* w_scale, const int64_t* target, const float* lse,
                      const float* g, int64_t T, int64_t V, int64_t K, void* dx, int64_t lddx,
                      int dx_dt, void* dw, int64_t lddw, int dw_dt, void* workspace,
                      int64_t workspace_bytes, void* stream);
+int cpdp_q8_xent_miss_bwd(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w,
+                          int64_t ldw, const float* w_scale, const int64_t* target,
+                          const float* lse, const float* miss, const float* g, int64_t T,
+                          int64_t V, int64_t K, void* dx, int64_t lddx, int dx_dt, void* dw,
+                          int64_t lddw, int dw_dt, void* workspace, int64_t workspace_bytes,
+                          void* stream);
 
 #ifdef __cplusplus
 }

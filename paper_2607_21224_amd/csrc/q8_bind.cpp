@@ -370,9 +370,9 @@ PyObject* grad_weight(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
-// x, x_scale, w, w_scale, target, loss, lse, workspace, stream
+// x, x_scale, w, w_scale, target, loss, lse, miss, workspace, stream
 PyObject* xent(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    return entry(args, n, 9, [](PyObject* const* a) {
+    return entry(args, n, 10, [](PyObject* const* a) {
         Call c;
         const Mat x = c.mat(a[0], "x", at::kChar);
         const int64_t T = x.rows, K = x.cols;
@@ -382,17 +382,23 @@ PyObject* xent(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const int64_t* target = c.wholes(a[4], "target", T);
         float* loss = c.scales(a[5], "loss", T);
         float* lse = c.scales(a[6], "lse", T);
-        void* stream = c.stream(a[8]);
+        float* miss = c.maybe_scales(a[7], "miss", T);
+        void* stream = c.stream(a[9]);
         int64_t bytes;
-        void* room = c.workspace(a[7], cpdp_q8_xent_workspace(T, w.rows, K), &bytes);
-        return cpdp_q8_xent(static_cast<int8_t*>(x.p), x.ld, xs, static_cast<int8_t*>(w.p), w.ld,
-                            ws, target, T, w.rows, K, loss, lse, room, bytes, stream);
+        void* room = c.workspace(a[8], cpdp_q8_xent_workspace(T, w.rows, K), &bytes);
+        const auto* xq = static_cast<int8_t*>(x.p);
+        const auto* wq = static_cast<int8_t*>(w.p);
+        return a[7] == Py_None
+                   ? cpdp_q8_xent(xq, x.ld, xs, wq, w.ld, ws, target, T, w.rows, K, loss, lse,
+                                  room, bytes, stream)
+                   : cpdp_q8_xent_miss(xq, x.ld, xs, wq, w.ld, ws, target, T, w.rows, K, loss, lse,
+                                       miss, room, bytes, stream);
     });
 }
 
-// x, x_scale, w, w_scale, target, lse, g, dx, dw, workspace, stream
+// x, x_scale, w, w_scale, target, lse, miss, g, dx, dw, workspace, stream
 PyObject* xent_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    return entry(args, n, 11, [](PyObject* const* a) {
+    return entry(args, n, 12, [](PyObject* const* a) {
         Call c;
         const Mat x = c.mat(a[0], "x", at::kChar);
         const int64_t T = x.rows, K = x.cols;
@@ -401,19 +407,25 @@ PyObject* xent_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const float* ws = c.scales(a[3], "w_scale", w.rows);
         const int64_t* target = c.wholes(a[4], "target", T);
         const float* lse = c.scales(a[5], "lse", T);
-        const float* g = c.scales(a[6], "g", T);
-        Mat dx = c.maybe(a[7], "dx", kEither, T, K);
-        Mat dw = c.maybe(a[8], "dw", kEither, w.rows, K);
-        if (a[7] == Py_None && a[8] == Py_None) refuse("dx", "neither dx nor dw is given");
-        if (a[7] == Py_None) dx.dt = dw.dt;
-        if (a[8] == Py_None) dw.dt = dx.dt;
-        void* stream = c.stream(a[10]);
+        const float* miss = c.maybe_scales(a[6], "miss", T);
+        const float* g = c.scales(a[7], "g", T);
+        Mat dx = c.maybe(a[8], "dx", kEither, T, K);
+        Mat dw = c.maybe(a[9], "dw", kEither, w.rows, K);
+        if (a[8] == Py_None && a[9] == Py_None) refuse("dx", "neither dx nor dw is given");
+        if (a[8] == Py_None) dx.dt = dw.dt;
+        if (a[9] == Py_None) dw.dt = dx.dt;
+        void* stream = c.stream(a[11]);
         int64_t bytes;
         void* room = c.workspace(
-            a[9], cpdp_q8_xent_bwd_workspace(T, w.rows, K, dx.dt, dw.dt), &bytes);
-        return cpdp_q8_xent_bwd(static_cast<int8_t*>(x.p), x.ld, xs, static_cast<int8_t*>(w.p),
-                                w.ld, ws, target, lse, g, T, w.rows, K, dx.p, dx.ld, dx.dt, dw.p,
-                                dw.ld, dw.dt, room, bytes, stream);
+            a[10], cpdp_q8_xent_bwd_workspace(T, w.rows, K, dx.dt, dw.dt), &bytes);
+        const auto* xq = static_cast<int8_t*>(x.p);
+        const auto* wq = static_cast<int8_t*>(w.p);
+        return a[6] == Py_None
+                   ? cpdp_q8_xent_bwd(xq, x.ld, xs, wq, w.ld, ws, target, lse, g, T, w.rows, K,
+                                      dx.p, dx.ld, dx.dt, dw.p, dw.ld, dw.dt, room, bytes, stream)
+                   : cpdp_q8_xent_miss_bwd(xq, x.ld, xs, wq, w.ld, ws, target, lse, miss, g, T,
+                                           w.rows, K, dx.p, dx.ld, dx.dt, dw.p, dw.ld, dw.dt,
+                                           room, bytes, stream);
     });
 }
 

@@ -18,8 +18,7 @@ constexpr int64_t kFewTokens = 64;
 // Joins the tiles' parts of each row's statistics: 16 rows a block, 16 threads a row.
 __global__ __launch_bounds__(256) void xent_join_kernel(const Stats* part, const float* hit,
                                                         int64_t T, int64_t tiles, int64_t V,
-                                                        const int64_t* target, float* loss,
-                                                        float* lse) {
+                                                        const int64_t* target, LossOut to) {
     __shared__ Stats words[16][17];
     const int row = threadIdx.x % 16, slice = threadIdx.x / 16;
     const int64_t t = (int64_t)blockIdx.x * 16 + row, from = t < T ? t : T - 1;
@@ -38,7 +37,7 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const Stats* part, const
     if (slice != 0 || t >= T) return;
 #pragma unroll
     for (int i = 1; i < 16; ++i) s = join(s, words[i][row]);
-    write_loss(s, hit[t], target[t], V, lse + t, loss + t);
+    write_loss(s, hit[t], target[t], V, to, t);
 }
 
 // f(tile) with the tile's size as a compile-time number
@@ -102,18 +101,18 @@ int launch_stats(const Loss& l, const Found& to, int tile, int64_t at, int64_t v
     });
 }
 
-int forward(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
+int forward(const Loss& l, const LossOut& out, void* ws, void* stream) {
     const ForwardRoom r = forward_room(l.T, l.V, l.K);
     const bool one = r.tiles == 1;
-    const Found to{one ? nullptr : at<Stats>(ws, r.part), one ? nullptr : at<float>(ws, r.hit), lse,
-                   loss};
+    const Found to{one ? nullptr : at<Stats>(ws, r.part), one ? nullptr : at<float>(ws, r.hit),
+                   out};
     const int64_t first = r.split.first;
     if (first > 0)
         if (int e = launch_stats(l, to, 256, 0, 0, first, stream)) return e;
     const int e = launch_stats(l, to, r.split.tile, first / 256, first, l.V - first, stream);
     if (e || one) return e;
     return launch(xent_join_kernel, dim3((uint32_t)up(l.T, 16)), 256, stream, to.part, to.hit, l.T,
-                  r.tiles, l.V, l.target, loss, lse);
+                  r.tiles, l.V, l.target, out);
 }
 
 // ---- what the products of the gradients need first ----------------------------------
@@ -433,8 +432,7 @@ int launch_slopes(const Logits& z, const Slopes& to, int64_t K, void* stream) {
     });
 }
 
-int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, void* ws,
-             void* stream) {
+int backward(const Loss& l, const LossIn& in, Mat dx, Mat dw, void* ws, void* stream) {
     const BackwardRoom r = backward_room(l.T, l.V, l.K, dx.bf16, dw.bf16);
     const bool x = dx.p != nullptr, w = dw.p != nullptr;
     const int px = x ? r.px : 0, pw = w ? r.pw : 0;
@@ -449,8 +447,7 @@ int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, vo
         to.by_class = at<uint16_t>(ws, r.by_class);
         to.row_ld = up(n, kRound) * kRound;
         to.class_ld = r.class_ld;
-        to.lse = lse;
-        to.g = g;
+        to.in = in;
         to.largest = at<const float>(ws, r.largest);
         to.rows = at<float>(ws, r.rows);
         to.classes = at<float>(ws, r.classes);
@@ -463,7 +460,7 @@ int backward(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, vo
         if (first) {
             const int64_t parts = up(l.V, kClasses), rows = up(l.T, kTokens);
             const int64_t some = parts > rows ? parts : rows;
-            largest = {l.x, l.w, l.target, g, l.T, l.V, l.K, at<float>(ws, r.largest), ones,
+            largest = {l.x, l.w, l.target, in.g, l.T, l.V, l.K, at<float>(ws, r.largest), ones,
                        (int)(some < kLargest ? some : kLargest)};
         }
         if (int e = launch_turn(of_x, of_w, largest, stream)) return e;
@@ -514,14 +511,14 @@ int64_t xent_workspace(int64_t T, int64_t V, int64_t K) {
     return few_logits(T, K) ? few_xent_workspace(T, V) : forward_room(T, V, K).bytes;
 }
 
-int launch_xent(const Loss& l, float* loss, float* lse, void* workspace, void* stream) {
-    return few_logits(l.T, l.K) ? launch_few_xent(l, loss, lse, workspace, stream)
-                                : forward(l, loss, lse, workspace, stream);
+int launch_xent(const Loss& l, const LossOut& to, void* workspace, void* stream) {
+    return few_logits(l.T, l.K) ? launch_few_xent(l, to, workspace, stream)
+                                : forward(l, to, workspace, stream);
 }
 
-int launch_few_slopes(const Loss& l, int64_t first, int64_t n, const float* lse, const float* g,
-                      float* d, int64_t ld, float* scale, void* stream) {
-    const FewSlopes to{d, ld, lse, g, scale, l.V};
+int launch_few_slopes(const Loss& l, int64_t first, int64_t n, const LossIn& in, float* d,
+                      int64_t ld, float* scale, void* stream) {
+    const FewSlopes to{d, ld, in, scale, l.V};
     const Logits z = logits_of(l, first, n);
     // (tiles of 256 would be mostly empty)
     return logit_tile(l.T, n, up(l.K, kStep), 0, 1).tile == 64 ? few_slopes<64>(z, to, stream)
@@ -533,13 +530,13 @@ int64_t xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
                            : backward_room(T, V, K, dx_bf16, dw_bf16).bytes;
 }
 
-int launch_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw,
-                    void* workspace, void* stream) {
+int launch_xent_bwd(const Loss& l, const LossIn& in, Mat dx, Mat dw, void* workspace,
+                    void* stream) {
     // a sum over no tokens
     if (l.T == 0)
         return launch_grad_weight(Mat{nullptr, 0, false}, l.x, 0, l.V, l.K, dw, workspace, stream);
-    return l.T <= kFewTokens ? launch_few_xent_bwd(l, lse, g, dx, dw, workspace, stream)
-                             : backward(l, lse, g, dx, dw, workspace, stream);
+    return l.T <= kFewTokens ? launch_few_xent_bwd(l, in, dx, dw, workspace, stream)
+                             : backward(l, in, dx, dw, workspace, stream);
 }
 
 }  // namespace q8

@@ -39,8 +39,7 @@ __global__ __launch_bounds__(1024, 8) void xent_few_stats_kernel(Held x, Held w,
 // A block joins a token's parts.
 __global__ __launch_bounds__(1024) void xent_few_join_kernel(const Stats* part, int64_t blocks,
                                                              const float* hit, int64_t V,
-                                                             const int64_t* target, float* loss,
-                                                             float* lse) {
+                                                             const int64_t* target, LossOut to) {
     __shared__ Stats words[16];
     const int64_t t = blockIdx.x;
     Stats s = {-__builtin_inff(), 0.0f};
@@ -53,7 +52,7 @@ __global__ __launch_bounds__(1024) void xent_few_join_kernel(const Stats* part, 
     if (threadIdx.x != 0) return;
 #pragma unroll
     for (int i = 1; i < 16; ++i) s = join(s, words[i]);
-    write_loss(s, hit[t], target[t], V, lse + t, loss + t);
+    write_loss(s, hit[t], target[t], V, to, t);
 }
 
 // The logits' gradient, d [M x N] for N classes from `first` on, and the tokens' scales
@@ -61,8 +60,7 @@ __global__ __launch_bounds__(1024) void xent_few_join_kernel(const Stats* part, 
 __global__ __launch_bounds__(1024) void xent_few_slopes_kernel(Held x, Held w,
                                                                const int64_t* target, int M,
                                                                int64_t N, int K, int64_t first,
-                                                               int64_t V, const float* lse,
-                                                               const float* g, float* d,
+                                                               int64_t V, LossIn in, float* d,
                                                                int64_t ld, float* scale) {
     __shared__ FewSums<1> sums;
     const int waves = blockDim.x >> 6;
@@ -78,8 +76,10 @@ __global__ __launch_bounds__(1024) void xent_few_slopes_kernel(Held x, Held w,
         if (m >= M) break;
         const int64_t y = target[m];
         const float z = (float)few_sum<1>(sums, e, waves) * x.scale[m] * ws;
-        const float l = y >= V ? __builtin_nanf("") : lse[m];
-        const float v = g[m] * (exp_of(z - l) - (first + n == y ? 1.0f : 0.0f));
+        const float l = y >= V ? __builtin_nanf("") : in.lse[m];
+        float p = exp_of(z - l);
+        if (first + n == y) p = in.miss != nullptr ? -in.miss[m] : p - 1.0f;
+        const float v = in.g[m] * p;
         d[m * ld + n] = y < 0 ? 0.0f : v;
     }
 }
@@ -148,7 +148,7 @@ BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
 
 int64_t few_xent_workspace(int64_t T, int64_t V) { return forward_room(T, V).bytes; }
 
-int launch_few_xent(const Loss& l, float* loss, float* lse, void* ws, void* stream) {
+int launch_few_xent(const Loss& l, const LossOut& to, void* ws, void* stream) {
     const ForwardRoom r = forward_room(l.T, l.V);
     const int waves = few_waves(l.K);
     // (a launch holds fewer than 2^32 work items)
@@ -161,14 +161,14 @@ int launch_few_xent(const Loss& l, float* loss, float* lse, void* ws, void* stre
             return e;
     }
     return launch(xent_few_join_kernel, dim3((uint32_t)l.T), 1024, stream, at<Stats>(ws, r.part),
-                  r.blocks, at<float>(ws, r.hit), l.V, l.target, loss, lse);
+                  r.blocks, at<float>(ws, r.hit), l.V, l.target, to);
 }
 
 int64_t few_xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
     return backward_room(T, V, K, dx_bf16, dw_bf16).bytes;
 }
 
-int launch_few_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw, void* ws,
+int launch_few_xent_bwd(const Loss& l, const LossIn& in, Mat dx, Mat dw, void* ws,
                         void* stream) {
     const BackwardRoom r = backward_room(l.T, l.V, l.K, dx.bf16, dw.bf16);
     const bool whole = r.piece == l.V;
@@ -182,9 +182,9 @@ int launch_few_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx,
         const int e = few_logits(l.T, l.K)
                           ? launch(xent_few_slopes_kernel, dim3((uint32_t)up(n, kClasses)),
                                    64 * few_waves(l.K), stream, l.x, w, l.target, (int)l.T, n,
-                                   (int)l.K, v, l.V, lse, g, static_cast<float*>(d.p), r.ld, scale)
-                          : launch_few_slopes(l, v, n, lse, g, static_cast<float*>(d.p), r.ld,
-                                              scale, stream);
+                                   (int)l.K, v, l.V, in, static_cast<float*>(d.p), r.ld, scale)
+                          : launch_few_slopes(l, v, n, in, static_cast<float*>(d.p), r.ld, scale,
+                                              stream);
         if (e) return e;
         if (dx.p != nullptr) {
             const Mat part{at<float>(ws, r.part), r.ldk, false};

@@ -13,13 +13,27 @@ struct Loss {
     int64_t T, V, K;
 };
 
+// Of each token; miss, 1 - exp(-loss), may be null.
+struct LossOut {
+    float* loss;
+    float* lse;
+    float* miss;
+};
+
 int64_t xent_workspace(int64_t T, int64_t V, int64_t K);
-int launch_xent(const Loss& l, float* loss, float* lse, void* workspace, void* stream);
+int launch_xent(const Loss& l, const LossOut& to, void* workspace, void* stream);
+
+// What the gradients have of each token; without miss, a target's p - 1 is exp(z - lse) - 1.
+struct LossIn {
+    const float* lse;
+    const float* miss;
+    const float* g;
+};
 
 // dx.p or dw.p may be null; the workspace is that of the types of both.
 int64_t xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16);
-int launch_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw,
-                    void* workspace, void* stream);
+int launch_xent_bwd(const Loss& l, const LossIn& in, Mat dx, Mat dw, void* workspace,
+                    void* stream);
 
 // Whether a loss' logits are made by q8_xent_few.hip, whose blocks read 16 classes' weights
 // and all tokens.  Loss in us, here and in tiles:
@@ -34,14 +48,14 @@ inline bool few_logits(int64_t T, int64_t K) { return T <= 16 && T * K <= 16384;
 
 // The loss of few tokens, and the gradients of up to 64 (q8_xent_few.hip).
 int64_t few_xent_workspace(int64_t T, int64_t V);
-int launch_few_xent(const Loss& l, float* loss, float* lse, void* workspace, void* stream);
+int launch_few_xent(const Loss& l, const LossOut& to, void* workspace, void* stream);
 int64_t few_xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16);
-int launch_few_xent_bwd(const Loss& l, const float* lse, const float* g, Mat dx, Mat dw,
-                        void* workspace, void* stream);
+int launch_few_xent_bwd(const Loss& l, const LossIn& in, Mat dx, Mat dw, void* workspace,
+                        void* stream);
 // The logits' gradient of classes first to first + n, in tiles (q8_xent.hip): d [T x n], fp32,
 // ld a multiple of 4, and the tokens' scales, 0 for those that do not count.
-int launch_few_slopes(const Loss& l, int64_t first, int64_t n, const float* lse, const float* g,
-                      float* d, int64_t ld, float* scale, void* stream);
+int launch_few_slopes(const Loss& l, int64_t first, int64_t n, const LossIn& in, float* d,
+                      int64_t ld, float* scale, void* stream);
 
 }  // namespace q8
 }  // namespace cpdp

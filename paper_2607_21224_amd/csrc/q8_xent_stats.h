@@ -31,13 +31,15 @@ __device__ __forceinline__ Stats join(Stats a, Stats b) {
     return {top, a.sum * exp_of(a.top - p) + b.sum * exp_of(b.top - p)};
 }
 
-// lse and loss from all of a row's logits; hit: its target's.  (lse - hit would lose of log(sum)
+// lse, loss and miss from all of a row's logits; hit: its target's.  (lse - hit would lose of log(sum)
 // what lse has no bits for: all of a loss below 2^-24 |lse|.)
-__device__ __forceinline__ void write_loss(Stats s, float hit, int64_t y, int64_t V, float* lse,
-                                           float* loss) {
+__device__ __forceinline__ void write_loss(Stats s, float hit, int64_t y, int64_t V,
+                                           const LossOut& to, int64_t t) {
     const float more = logf(s.sum);
-    *lse = s.top + more;
-    *loss = y < 0 ? 0.0f : (s.top - (y < V ? hit : __builtin_nanf(""))) + more;
+    const float l = y < 0 ? 0.0f : (s.top - (y < V ? hit : __builtin_nanf(""))) + more;
+    to.lse[t] = s.top + more;
+    to.loss[t] = l;
+    if (to.miss != nullptr) to.miss[t] = -expm1f(-l);
 }
 
 // Takes parts of a workspace, each on a 256-byte boundary.

@@ -61,7 +61,8 @@ __device__ __forceinline__ float scale_for(float x) {
 //   by_class  e g[t] x_scale[t] * scale[1]     [classes][parts][class_ld]
 // scale are powers of two that bring the largest |w_scale| and |g x_scale| there are, found
 // from those of up to 32 parts, to 2^14 or more and below 2^15.  What fp16 keeps of a number ends at 2^-24: at 2^-38 of that,
-// 2^-50 with two parts, where e itself has an error of 2^-24 at the target.  (In bfloat16
+// 2^-50 with two parts, where e itself has an error of 2^-24 or more at the target (from miss:
+// that of the loss; else lse's, 2^-24 |lse|).  (In bfloat16
 // numbers, which do not end there, an fp32 result needs three, and its product is half as
 // long again: loss and gradients of 4096 x 65536 x 1024 with fp32 dw 2820 us, and 2400 when
 // this was all that changed.)
@@ -70,8 +71,7 @@ struct Slopes {
     uint16_t* by_row;
     uint16_t* by_class;
     int64_t row_ld, class_ld;  // of a part; whole steps
-    const float* lse;
-    const float* g;
+    LossIn in;
     const float* largest;  // [2][kLargest]
     float* rows;
     float* classes;
@@ -83,8 +83,7 @@ struct Slopes {
 struct FewSlopes {
     float* d;
     int64_t ld;
-    const float* lse;
-    const float* g;
+    LossIn in;
     float* scale;
     int64_t V;  // classes of the loss
 };
@@ -94,8 +93,7 @@ struct FewSlopes {
 struct Found {
     Stats* part;
     float* hit;
-    float* lse;
-    float* loss;
+    LossOut out;
 };
 
 // Tiles of TILE rows and classes by 2 x WN wavefronts, with S LDS buffers.
@@ -134,13 +132,13 @@ struct LogitTile {
     struct Vectors {
         float x_scale[TILE], w_scale[TILE];
         uint32_t target[2][TILE];  // halves
-        float lse[TILE], g[TILE];
+        float lse[TILE], g[TILE], miss[TILE];
         float largest[2 * kLargest];
     };
     static_assert(2 * kLargest == 64, "a load of a wavefront");
-    // (without SLOPES no lse and g; `largest` may be null)
+    // (without SLOPES nothing of `in`; `largest` may be null)
     template <bool SLOPES>
-    static __device__ __forceinline__ void send(const Logits& l, const float* lse, const float* g,
+    static __device__ __forceinline__ void send(const Logits& l, const LossIn& in,
                                                 const float* largest, const Place& p, Vectors& v) {
         if constexpr (SLOPES)
             if (p.wave == 0 && largest != nullptr)
@@ -148,7 +146,7 @@ struct LogitTile {
                     (__attribute__((address_space(1))) void*)(largest + p.lane),
                     (__attribute__((address_space(3))) void*)(v.largest), 4, 0, 0);
         constexpr int kEach = TILE / 64;
-        constexpr int count = (SLOPES ? 6 : 4) * kEach;
+        constexpr int count = (SLOPES ? 7 : 4) * kEach;
 #pragma unroll
         for (int j = 0; j < (count + kWaves - 1) / kWaves; ++j) {
             const int k = j * kWaves + p.wave;
@@ -162,8 +160,11 @@ struct LogitTile {
                                : what == 1 ? static_cast<const void*>(l.w_scale + n)
                                : what == 2 ? static_cast<const void*>(half)
                                : !SLOPES || what == 3 ? static_cast<const void*>(half + 1)
-                               : what == 4            ? static_cast<const void*>(lse + m)
-                                                      : static_cast<const void*>(g + m);
+                               : what == 4            ? static_cast<const void*>(in.lse + m)
+                               : what == 5            ? static_cast<const void*>(in.g + m)
+                               // (something, where there is none)
+                               : in.miss != nullptr ? static_cast<const void*>(in.miss + m)
+                                                    : static_cast<const void*>(in.lse + m);
             __builtin_amdgcn_global_load_lds(
                 (__attribute__((address_space(1))) void*)(from),
                 (__attribute__((address_space(3))) void*)(reinterpret_cast<char*>(&v) +
@@ -201,6 +202,14 @@ struct LogitTile {
         return at >= 0 && at < COLS ? (int)at : -1;
     }
 
+    // p of the target less 1: what its loss leaves of it, where that is known
+    static __device__ __forceinline__ void less_one(float (&e)[COLS], int at, const LossIn& in,
+                                                    float miss) {
+#pragma unroll
+        for (int k = 0; k < COLS; ++k)
+            if (k == at) e[k] = in.miss != nullptr ? -miss : e[k] - 1.0f;
+    }
+
     // Each row's largest logit and sum of exp's over the tile's classes, and its target's
     // logit where the tile has it; the loss, if these are all the classes.
     static __device__ __forceinline__ void stats(const Logits& l, const Found& to, int64_t tiles_m,
@@ -208,7 +217,7 @@ struct LogitTile {
         __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
         Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
-        send<false>(l, nullptr, nullptr, nullptr, p, v);
+        send<false>(l, LossIn{}, nullptr, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
         float ws[COLS];
@@ -259,7 +268,7 @@ struct LogitTile {
         const int64_t at = y - l.first - p.tile.n;
         const bool here = at >= 0 && at < TILE && p.tile.n + at < l.o.N;
         if (to.part == nullptr) {
-            write_loss(s, hit[threadIdx.x], y, here ? y + 1 : 0, to.lse + m, to.loss + m);
+            write_loss(s, hit[threadIdx.x], y, here ? y + 1 : 0, to.out, m);
             return;
         }
         to.part[(first_tile + p.tile.n / TILE) * l.o.M + m] = s;
@@ -274,7 +283,7 @@ struct LogitTile {
         __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
         Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
-        send<true>(l, to.lse, to.g, to.largest, p, v);
+        send<true>(l, to.in, to.largest, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
         const int64_t n0 = p.tile.n + p.first;
@@ -308,10 +317,7 @@ struct LogitTile {
 #pragma unroll
             for (int k = 0; k < COLS; ++k)
                 e[k] = exp_of((float)acc[i][k / 4][k % 4] * xs * ws[k] - lse);
-            if (__any(at >= 0)) {
-#pragma unroll
-                for (int k = 0; k < COLS; ++k) e[k] = k == at ? e[k] - 1.0f : e[k];
-            }
+            if (__any(at >= 0)) less_one(e, at, to.in, v.miss[row]);
 #pragma unroll
             for (int k = 0; k < COLS; ++k) {
                 t[k] = e[k] * gx;
@@ -383,7 +389,7 @@ struct LogitTile {
         __shared__ __attribute__((aligned(1024))) char lds[kBuffers + sizeof(Vectors)];
         Vectors& v = *reinterpret_cast<Vectors*>(lds + kBuffers);
         const Place p = place(tiles_m, tiles_n);
-        send<true>(l, to.lse, to.g, nullptr, p, v);
+        send<true>(l, to.in, nullptr, p, v);
         i32x4 acc[MT][NT] = {};
         sums(l, p, lds, acc);
         if (p.tile.n == 0 && (int)threadIdx.x < TILE && p.tile.m + threadIdx.x < l.o.M)
@@ -404,10 +410,7 @@ struct LogitTile {
 #pragma unroll
             for (int k = 0; k < COLS; ++k)
                 e[k] = exp_of((float)acc[i][k / 4][k % 4] * xs * ws[k] - lse);
-            if (__any(at >= 0)) {
-#pragma unroll
-                for (int k = 0; k < COLS; ++k) e[k] = k == at ? e[k] - 1.0f : e[k];
-            }
+            if (__any(at >= 0)) less_one(e, at, to.in, v.miss[row]);
             if (m >= l.o.M) continue;
             float* d = to.d + m * to.ld + n0;
 #pragma unroll

@@ -222,6 +222,8 @@ class HeadSaved:
         self.n, self.n_scale, self.rstd = rows(T, D, i8), vec(T), vec(T)
         self.w = rows(V, D, i8), vec(V)  # the weights as they were used
         self.loss, self.lse = vec(T), vec(T)
+        # what the gradients have of the loss, whatever becomes of the tensor that is handed out
+        self.of_loss = {"miss": vec(T)}
         self.h, self.dn, self.dx = rows(T, D), rows(T, D), rows(T, D)
         self.target = self.norm_of = None
         self.workspace = torch.empty(head.workspace_bytes(T), dtype=torch.uint8, device=device)
@@ -276,7 +278,7 @@ class Q8Head(_Tensors):
                         rstd=s.rstd, stream=stream, **kw)
         q8.cpdp_q8_rows(self.view(params, "w"), *s.w, stream=stream)
         q8.cpdp_q8_xent(s.n, s.n_scale, *s.w, target, s.loss, s.lse, workspace=s.workspace,
-                        stream=stream)
+                        stream=stream, **s.of_loss)
         return s.loss
 
     def backward(self, params, g, saved: HeadSaved, grads, dres=None,
@@ -288,7 +290,7 @@ class Q8Head(_Tensors):
         s = saved
         kw = {"workspace": s.workspace, "stream": stream}
         q8.cpdp_q8_xent_bwd(s.n, s.n_scale, *s.w, s.target, s.lse, g, s.dn,
-                            self.view(grads, "w"), **kw)
+                            self.view(grads, "w"), **s.of_loss, **kw)
         q8.cpdp_q8_norm_bwd(s.dn, s.norm_of, self.view(params, "norm"), s.rstd, s.dx,
                             self.view(grads, "norm"), dres=dres, **kw)
         return s.dx

@@ -43,7 +43,8 @@ EXPORTS = ("cpdp_q8_rows", "cpdp_q8_values", "cpdp_q8_norm", "cpdp_q8_norm_bwd_w
            "cpdp_q8_norm_bwd", "cpdp_q8_matmul_workspace", "cpdp_q8_matmul", "cpdp_q8_act",
            "cpdp_q8_act_bwd", "cpdp_q8_grad_input_workspace", "cpdp_q8_grad_input",
            "cpdp_q8_grad_weight_workspace", "cpdp_q8_grad_weight", "cpdp_q8_xent_workspace",
-           "cpdp_q8_xent", "cpdp_q8_xent_bwd_workspace", "cpdp_q8_xent_bwd")
+           "cpdp_q8_xent", "cpdp_q8_xent_bwd_workspace", "cpdp_q8_xent_bwd",
+           "cpdp_q8_xent_miss", "cpdp_q8_xent_miss_bwd")
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -73,6 +74,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "cpdp_q8_xent": [p, n, p, p, n, p, p, n, n, n, p, p, p, n, p],
         "cpdp_q8_xent_bwd_workspace": [n, n, n, i, i],
         "cpdp_q8_xent_bwd": [p, n, p, p, n, p, p, p, p, n, n, n, p, n, i, p, n, i, p, n, p],
+        "cpdp_q8_xent_miss": [p, n, p, p, n, p, p, n, n, n, p, p, p, p, n, p],
+        "cpdp_q8_xent_miss_bwd": [p, n, p, p, n, p, p, p, p, p, n, n, n, p, n, i, p, n, i, p, n, p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -189,10 +192,11 @@ def cpdp_q8_xent_workspace(T, V, K) -> int:
 
 
 def cpdp_q8_xent(x, x_scale, w, w_scale, target, loss, lse, workspace=None, stream=None,
-                 check=True):
+                 check=True, miss=None):
     """lse, loss <- the softmax cross entropy of the logits x w^T (rows of both scaled) and
-    target, (T,) int64; tokens whose target is negative do not count."""
-    s = _q8.xent(x, x_scale, w, w_scale, target, loss, lse, workspace, _stream(stream))
+    target, (T,) int64; tokens whose target is negative do not count.  miss, (T,), if given:
+    1 - exp(-loss), for the gradients (cpdp_q8_xent_miss)."""
+    s = _q8.xent(x, x_scale, w, w_scale, target, loss, lse, miss, workspace, _stream(stream))
     return _done(s, "cpdp_q8_xent", check)
 
 
@@ -202,8 +206,10 @@ def cpdp_q8_xent_bwd_workspace(T, V, K, dx_dtype, dw_dtype) -> int:
 
 
 def cpdp_q8_xent_bwd(x, x_scale, w, w_scale, target, lse, g, dx=None, dw=None, workspace=None,
-                     stream=None, check=True):
+                     stream=None, check=True, miss=None):
     """dx, dw (the ones that are given) <- the gradients of x's and w's values, where g (T,)
-    is the gradient of the loss and lse is cpdp_q8_xent's."""
-    s = _q8.xent_bwd(x, x_scale, w, w_scale, target, lse, g, dx, dw, workspace, _stream(stream))
+    is the gradient of the loss and lse is cpdp_q8_xent's; with its miss, those of tokens of
+    small loss are as exact as the loss (cpdp_q8_xent_miss_bwd)."""
+    s = _q8.xent_bwd(x, x_scale, w, w_scale, target, lse, miss, g, dx, dw, workspace,
+                     _stream(stream))
     return _done(s, "cpdp_q8_xent_bwd", check)

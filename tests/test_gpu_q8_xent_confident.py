@@ -1,5 +1,5 @@
-"""The loss of tokens whose target has nearly all of the probability, at large logits that
-fp32 holds exactly: what is lost there is the loss' own.
+"""The loss of tokens whose target has nearly all of the probability, and its gradients, at
+large logits that fp32 holds exactly: what is lost there is the operators' own.
 
 Every class has the logit `base`, a whole number of 16ths, and a token's target one of base +
 gap: with s = (V - 1) exp(-gap) its loss is log(1 + s), whatever base is.
@@ -14,13 +14,19 @@ product where parts are joined is as an addition.  So the sum is off by
 
 at most, the loss by that over 1 + s, its logarithm 2 u of it, and the last addition u.
 lse: the same, and u |lse| for its own rounding.
+miss, 1 - exp(-loss): as the loss, and 2 u of it.
+p of the others: lse's error and 2 (gap + loss) u + 4 u, relative.  d has that times |g|, the
+target's the error of miss, and u for the product.  Without miss the target's is 1 - exp(z - lse):
+lse's error, 2 loss u and 4 u.
 """
 import math
 
 import pytest
 import torch
 
+import xent_sizes
 from test_gpu_q8 import U, q8  # noqa: F401
+from test_gpu_q8_xent import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -28,8 +34,8 @@ GAP = 5.75  # and twice and three times that
 SIZES = [(1, 33), (9, 700), (16, 5003), (40, 5003), (65, 700), (130, 33), (300, 5003)]
 
 
-class Confident:
-    def __init__(self, T, V, base, K=40, pad=0):
+class Confident(Case):
+    def __init__(self, T, V, base, K=40):
         self.T, self.V, self.K = T, V, K
         hot = min(V, K - 2)
         classes = torch.arange(hot, device="cuda") * (V // hot)
@@ -51,14 +57,24 @@ class Confident:
         self.top = base + self.gap
         A = 35 + V / 1024
         self.off = (self.s * (2 * self.gap + 4 + 2 * A) / (1 + self.s) + A) * U
+        self.g = (1 + t % 5) / T
+        self.counts = self.target >= 0
+        self.with_miss = True
 
-    def held(self):
-        return self.x, self.xs, self.w, self.ws, self.target
-
-    def forward(self, q8, **kw):  # noqa: F811
-        loss, lse = (torch.empty(self.T, device="cuda") for _ in range(2))
-        q8.cpdp_q8_xent(*self.held(), loss, lse, **kw)
-        return loss, lse
+    def gradients(self):
+        """d with its error: of the others p alike, of the target 1 less all of theirs."""
+        loss = torch.log1p(self.s)[:, None]
+        p = (1 / (torch.exp(self.gap) + self.V - 1))[:, None].expand(-1, self.V).clone()
+        miss = (self.s / (1 + self.s))[:, None]
+        lse_off = self.off[:, None] + 3 * U * loss + U * (loss + self.top[:, None])
+        off = p * (lse_off + (2 * (self.gap[:, None] + loss) + 4) * U)
+        hit = self.off[:, None] + (3 * loss + 2 * miss) * U
+        if not self.with_miss:
+            hit = lse_off + (2 * loss + 4) * U
+        at = self.target[:, None]
+        p.scatter_(1, at, -miss), off.scatter_(1, at, hit)
+        g = self.g.double()[:, None]
+        return g * p, g * (off + U * p.abs())
 
 
 @pytest.mark.parametrize("base", [0, 50, 100, 300])
@@ -93,3 +109,124 @@ def test_a_target_that_has_no_probability(q8):  # noqa: F811
         c.w.fill_(-1), c.ws.fill_(math.inf)
         loss, lse = c.forward(q8)
         assert bool(loss.isnan().all()) and bool((lse == -math.inf).all())
+
+
+@pytest.mark.parametrize("types", [(0, 0), (1, 1)])
+@pytest.mark.parametrize("base", [0, 50, 100, 300])
+@pytest.mark.parametrize("T,V", SIZES)
+def test_gradients(q8, T, V, base, types):  # noqa: F811
+    """With miss, to the bounds above; without, to those that the header gives, |lse| 2^-24."""
+    c = Confident(T, V, base)
+    miss = torch.empty(T, device="cuda")
+    loss, lse = c.forward(q8, miss=miss)
+    want = c.s / (1 + c.s)
+    assert bool(((miss.double() - want).abs() <= c.off + (3 * torch.log1p(c.s) + 2 * want) * U).all())
+    assert all(torch.equal(a, b) for a, b in zip(c.forward(q8), (loss, lse)))
+    c.check_backward(*c.backward(q8, lse, *types, miss=miss), *types)
+    c.with_miss = False
+    c.check_backward(*c.backward(q8, lse, *types), *types)
+
+
+@pytest.mark.parametrize("T,V", SIZES)
+def test_slopes_add_up_to_nothing(q8, T, V):  # noqa: F811
+    """All classes have the same weights in two channels, and the sum of d over the classes is 0:
+    with miss what is left of it there does not grow with the logits but as the others' p do."""
+    c = Confident(T, V, 300)
+    miss = torch.empty(T, device="cuda")
+    loss, lse = c.forward(q8, miss=miss)
+    dx = c.backward(q8, lse, 0, xent_sizes.NONE, miss=miss)[0][:, 0].double().abs()
+    d, off = c.gradients()
+    size = d.abs().sum(1)
+    # (a floor of 2^-51 or less of the largest scale for each term, as in the other tests)
+    room = off.sum(1) + ((V + 4) * U + 2.0 ** -22) * size + V * 2.0 ** -51 * c.g.double()
+    assert bool((dx <= room * float(c.w[0, 0]) * 0.25).all())
+
+
+@pytest.mark.parametrize("T", [1, 9, 40, 130])
+def test_miss_of_tokens_without_one(q8, T):  # noqa: F811
+    """A token that does not count has 0, one whose target is not there NaN, one whose target has
+    no probability 1."""
+    c = Confident(T, 700, 50)
+    miss = torch.full((T + 1,), 7.0, device="cuda")
+    for target, scale in ((-5, 0.25), (700, 0.25), (3, math.inf)):
+        c.target.fill_(target)
+        c.w[3], c.ws[3] = -1, scale
+        c.forward(q8, miss=miss[:-1])
+        got = miss[:-1]
+        assert bool((got.isnan() if target == 700 else got == float(target == 3)).all())
+    assert miss[-1] == 7
+
+
+@pytest.mark.parametrize("T,V,K", [(9, 1001, 130), (63, 1000, 63), (128, 100, 384),
+                                   (700, 9001, 130), (33, 300007, 40), (2100, 70001, 130)])
+@pytest.mark.parametrize("types", xent_sizes.TYPES)
+def test_ordinary_tokens(q8, T, V, K, types):  # noqa: F811
+    """The other tests' rows with miss: their bounds hold, and tokens that do not count or are not
+    finite are what they are without it."""
+    c = Case(T, V, K)
+    miss = torch.empty(T, device="cuda")
+    loss, lse = c.forward(q8, miss=miss)
+    c.check_forward(loss, lse)
+    c.check_backward(*c.backward(q8, lse, *types, miss=miss), *types)
+    c.target[T // 2], c.g[T // 2] = V, 1.0
+    loss, lse = c.forward(q8, miss=miss)
+    dx, dw = c.backward(q8, lse, *types, miss=miss)
+    assert bool(dx[T // 2].isnan().all()) and bool(dw.isnan().all())
+
+
+@pytest.mark.parametrize("T,V", [(9, 700), (40, 700), (300, 700)])
+def test_captured(q8, T, V):  # noqa: F811
+    c, miss = Confident(T, V, 100), torch.empty(T, device="cuda")
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    out = [torch.zeros(T, device="cuda"), torch.zeros(T, device="cuda"),
+           torch.zeros((T, 48), device="cuda")[:, :40], torch.zeros((V, 48), device="cuda")[:, :40]]
+
+    def step():
+        q8.cpdp_q8_xent(*c.held(), *out[:2], workspace=ws, miss=miss)
+        q8.cpdp_q8_xent_bwd(*c.held(), out[1], c.g, *out[2:], workspace=ws, miss=miss)
+
+    step()
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for shift in (1, 2, 3):
+        c.target.copy_(c.target.roll(shift))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in (*out, miss)]
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(got, (*out, miss)))
+
+
+def test_refusals(q8):  # noqa: F811
+    c = Confident(6, 40, 0)
+    loss, lse = c.forward(q8)
+    for bad, what in ((loss[:5], "vector"), (loss.double(), "float32"), (loss.cpu(), "GPU"),
+                      (torch.empty(12, device="cuda")[::2], "vector")):
+        with pytest.raises(ValueError, match=what):
+            c.forward(q8, miss=bad)
+        with pytest.raises(ValueError, match=what):
+            c.backward(q8, lse, 0, 0, miss=bad)
+
+
+def test_a_head_s_gradients_are_those_of_its_miss(q8):  # noqa: F811
+    """Whatever the caller does with the losses that it was given."""
+    from paper_2607_21224_amd.layer import Q8Head
+    T, D, V = 96, 64, 300
+    head, g = Q8Head(D, V, act_dt="f32"), torch.Generator(device="cuda").manual_seed(1)
+    row = head.init(g)
+    target = torch.randint(0, V, (T,), generator=g, device="cuda")
+    x = torch.randn((T, D), generator=g, device="cuda") + 60 * head.view(row, "w")[target]
+    head.view(row, "norm").fill_(8.0)  # steep: most tokens are confident
+    s, grads = head.saved(T), torch.zeros(head.numel, device="cuda")
+    weight = torch.rand(T, generator=g, device="cuda")
+    loss = head.forward(row, x, target, s)
+    assert float(loss.median()) < 1e-3
+    miss, dx = torch.empty(T, device="cuda"), torch.empty((T, D), device="cuda")
+    dw = torch.empty((V, D), device="cuda")
+    q8.cpdp_q8_xent(s.n, s.n_scale, *s.w, target, loss.clone(), s.lse, miss=miss)
+    q8.cpdp_q8_xent_bwd(s.n, s.n_scale, *s.w, target, s.lse, weight, dx, dw, miss=miss)
+    loss.zero_()
+    head.backward(row, weight, s, grads)
+    assert torch.equal(s.dn, dx) and torch.equal(head.view(grads, "w"), dw)

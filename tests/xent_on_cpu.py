@@ -10,10 +10,10 @@ from paper_2607_21224_amd import build
 NAMES = ("xent", "head")
 
 
-def compile_calls(folder, optimise="-O0", sources=None):
+def compile_calls(folder, optimise="-O0", sources=None, calls="xent_calls.cpp"):
     csrc = os.path.join(build.PKG, "csrc")
     paths = [os.path.join(csrc, s) for s in sources or build.Q8_SOURCES + build.XENT_SOURCES]
-    paths.append(os.path.join(on_cpu.NATIVE, "on_cpu", "xent_calls.cpp"))
+    paths.append(os.path.join(on_cpu.NATIVE, "on_cpu", calls))
     include = ["-I", os.path.join(on_cpu.NATIVE, "on_cpu_xent"), "-I",
                os.path.join(on_cpu.NATIVE, "on_cpu"), "-I",
                os.path.join(build.ROOT, "include"), "-I", csrc]
