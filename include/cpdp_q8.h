@@ -179,7 +179,10 @@ int cpdp_q8_grad_weight(const void* dy, int64_t lddy, int dy_dt, const int8_t* a
 /*
  * Softmax cross entropy over V classes, of the logits
  *   z[t, v] = x_scale[t] * w_scale[v] * sum_k x[t, k] * w[v, k]
- * which are never held as a whole: the classes are taken in pieces.
+ * which are not kept from one pass to the next: the forward pass uses them a tile at a time
+ * and holds none, the gradients make them again and hold what they are of a piece of the
+ * classes, up to 2^27 of them (with fewer logits that is all), laid out in 2 to 8 bytes a
+ * logit, and the piece's weights in 2 or 4 bytes each, up to 512 MB.
  *   cpdp_q8_xent      lse[t]  = log sum_v exp z[t, v]
  *                     loss[t] = lse[t] - z[t, target[t]]
  *   cpdp_q8_xent_bwd  d[t, v] = g[t] * (exp(z[t, v] - lse[t]) - (v == target[t] ? 1 : 0))
@@ -209,6 +212,8 @@ int cpdp_q8_grad_weight(const void* dy, int64_t lddy, int dy_dt, const int8_t* a
  * 2^-51 of the largest |w_scale|, or of the largest |g * x_scale| of the tokens that count;
  * in one for a bf16 result: 11 bits, and 2^-39 of the largest.  (Up to 64 tokens: in
  * bfloat16 numbers, as the gradients of a product from fp32 dy.)
+ * The gradients' workspace, whatever V is: less than 512 MiB up to 64 tokens, and else less than
+ * max(1 GiB, 2048 T) + 640 MiB + 12 (T + 64) (K + 64) bytes.
  */
 #define CPDP_Q8_MAX_T 2097088 /* 2^21 - 64: rows of sums that a tile can address */
 

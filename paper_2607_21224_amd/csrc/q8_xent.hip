@@ -247,12 +247,16 @@ int launch_turn(const Source& a, const Source& b, const Largest& s, void* stream
 
 // ---- the products --------------------------------------------------------------------
 
-// Classes of a piece: 2^27 slopes at most (268 MB a part), whole tiles, and rows that a tile
-// can address.
-int64_t piece_of(int64_t T, int64_t V) {
-    int64_t n = ((int64_t)1 << 27) / T / 1024 * 1024;
-    n = n < 1024 ? 1024 : n > (int64_t)1 << 20 ? (int64_t)1 << 20 : n;
-    return n < V ? n : V;
+// Classes of a piece: 2^27 slopes (268 MB a part) and 512 MB of weights, laid out, at most; whole
+// tiles, one at least, and rows that a tile can address.  A piece costs 50 to 100 us, its
+// launches' ends (gradients of 128 x 151936 x 4096 bf16 1305 us in one piece with 1.3 GB of
+// workspace, 1445 in three with 0.46; fp32 2170 with 2.7 and 2540 with 0.55; with 512 MB for
+// slopes and weights together, 8192 x 32768 x 4096 bf16 took 4800 us, and takes 4570).
+int64_t piece_of(int64_t T, int64_t V, int64_t K, int px) {
+    const int64_t slopes = ((int64_t)1 << 27) / T, weights = ((int64_t)1 << 28) / (px * K);
+    int64_t n = (slopes < weights ? slopes : weights) / 256 * 256;
+    n = n < 256 ? 256 : n > (int64_t)1 << 20 ? (int64_t)1 << 20 : n;
+    return piece_size(V, up(V, n), 256);
 }
 
 // Whether a product is small: tiles that find a CU each, and few steps.  What it takes is
@@ -355,11 +359,11 @@ struct BackwardRoom : Room {
 };
 BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
     BackwardRoom r;
-    r.piece = piece_of(T, V);
-    r.row_ld = up(r.piece, kRound) * kRound;
-    r.class_ld = up(T, kRound) * kRound;
     r.px = dx_bf16 ? 1 : 2;
     r.pw = dw_bf16 ? 1 : 2;
+    r.piece = piece_of(T, V, K, r.px);
+    r.row_ld = up(r.piece, kRound) * kRound;
+    r.class_ld = up(T, kRound) * kRound;
     r.by_row = r.take(r.px * T * r.row_ld * 2);
     r.by_class = r.take(r.pw * r.piece * r.class_ld * 2);
     r.x = r.take(r.pw * K * r.class_ld * 2);

@@ -42,6 +42,13 @@ __device__ __forceinline__ void write_loss(Stats s, float hit, int64_t y, int64_
     if (to.miss != nullptr) to.miss[t] = -expm1f(-l);
 }
 
+// The gradients are made a piece of the classes at a time: V of them in `pieces`, as even as
+// whole `unit`s are.
+inline int64_t piece_size(int64_t V, int64_t pieces, int64_t unit) {
+    const int64_t n = up(up(V, pieces), unit) * unit;
+    return n < V ? n : V;
+}
+
 // Takes parts of a workspace, each on a 256-byte boundary.
 struct Room {
     int64_t bytes = 0;

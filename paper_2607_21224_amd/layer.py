@@ -234,8 +234,9 @@ class Q8Head(_Tensors):
     cross entropy of the targets:
         h = x + residual;  n = 8(norm(h) * w_norm)
         loss[t] = log sum_v exp z[t, v] - z[t, target[t]],  z = n 8(W)^T
-    The logits z are never held as a whole.  Its weights and gradients are slices of a
-    replica's row, as Q8Mlp's::
+    The logits z are not kept between the passes.  The backward pass makes them again and needs
+    a workspace for a piece of the classes (``workspace_bytes``: bounded whatever ``classes``
+    is).  Its weights and gradients are slices of a replica's row, as Q8Mlp's::
 
         head = Q8Head(dim=384, classes=32768)
         row = torch.cat([mlp.init(), head.init()])       # one model of both
