@@ -230,3 +230,24 @@ def test_a_head_s_gradients_are_those_of_its_miss(q8):  # noqa: F811
     loss.zero_()
     head.backward(row, weight, s, grads)
     assert torch.equal(s.dn, dx) and torch.equal(head.view(grads, "w"), dw)
+
+
+@pytest.mark.parametrize("T", [3, 40, 130])
+def test_the_smallest_and_largest_targets(q8, T):  # noqa: F811
+    """A token of the smallest target does not count, as any negative one; one of the largest has
+    no class."""
+    c, ref = Confident(T, 700, 50), Confident(T, 700, 50)
+    miss = torch.empty(T, device="cuda")
+    c.target[1], ref.target[1] = -2 ** 63, -1
+    for types in xent_sizes.TYPES:
+        out = []
+        for v in (c, ref):
+            loss, lse = v.forward(q8, miss=miss)
+            out.append((loss, lse, miss.clone(), *v.backward(q8, lse, *types, miss=miss)))
+        assert all(torch.equal(a, b) for a, b in zip(*out)) and float(out[0][0][1]) == 0
+    c.target[1] = 2 ** 63 - 1
+    loss, lse = c.forward(q8, miss=miss)
+    dx, dw = c.backward(q8, lse, 0, 0, miss=miss)
+    assert bool(loss[1].isnan() & miss[1].isnan() & dx[1].isnan().all() & dw.isnan().all())
+    others = torch.arange(T, device="cuda") != 1
+    assert torch.equal(loss[others], out[0][0][others])
