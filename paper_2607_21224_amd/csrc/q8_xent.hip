@@ -247,16 +247,20 @@ int launch_turn(const Source& a, const Source& b, const Largest& s, void* stream
 
 // ---- the products --------------------------------------------------------------------
 
-// Classes of a piece: 2^27 slopes (268 MB a part) and 512 MB of weights, laid out, at most; whole
-// tiles, one at least, and rows that a tile can address.  A piece costs 50 to 100 us, its
-// launches' ends (gradients of 128 x 151936 x 4096 bf16 1305 us in one piece with 1.3 GB of
-// workspace, 1445 in three with 0.46; fp32 2170 with 2.7 and 2540 with 0.55; with 512 MB for
-// slopes and weights together, 8192 x 32768 x 4096 bf16 took 4800 us, and takes 4570).
-int64_t piece_of(int64_t T, int64_t V, int64_t K, int px) {
-    const int64_t slopes = ((int64_t)1 << 27) / T, weights = ((int64_t)1 << 28) / (px * K);
-    int64_t n = (slopes < weights ? slopes : weights) / 256 * 256;
+// Classes of a piece: 2^27 slopes (268 MB a part) at most, whole tiles, one at least, and rows
+// that a tile can address.
+int64_t piece_of(int64_t T, int64_t V) {
+    int64_t n = ((int64_t)1 << 27) / T / 256 * 256;
     n = n < 256 ? 256 : n > (int64_t)1 << 20 ? (int64_t)1 << 20 : n;
     return piece_size(V, up(V, n), 256);
+}
+// With dx, 512 MB of weights, laid out, at most, too.  A piece costs 50 to 100 us, its launches'
+// ends (gradients of 128 x 151936 x 4096 bf16 1305 us in one piece with 1.3 GB of workspace, 1445
+// in three with 0.46; fp32 2170 with 2.7 and 2540 with 0.55; with 512 MB for slopes and weights
+// together, 8192 x 32768 x 4096 bf16 took 4800 us, and takes 4570).
+int64_t piece_of(int64_t T, int64_t V, int64_t K, int px) {
+    const int64_t slopes = piece_of(T, V), weights = ((int64_t)1 << 28) / (px * K) / 256 * 256;
+    return slopes <= weights ? slopes : piece_size(V, up(V, weights < 256 ? 256 : weights), 256);
 }
 
 // Whether a product is small: tiles that find a CU each, and few steps.  What it takes is
@@ -357,11 +361,12 @@ struct BackwardRoom : Room {
     int px, pw;                       // parts
     int64_t by_row, by_class, x, w, largest, ones, rows, classes, sum, slices;
 };
-BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
+// (px: 0 without dx)
+BackwardRoom room_of(int64_t T, int64_t V, int64_t K, int px, int pw, int64_t piece) {
     BackwardRoom r;
-    r.px = dx_bf16 ? 1 : 2;
-    r.pw = dw_bf16 ? 1 : 2;
-    r.piece = piece_of(T, V, K, r.px);
+    r.px = px;
+    r.pw = pw;
+    r.piece = piece;
     r.row_ld = up(r.piece, kRound) * kRound;
     r.class_ld = up(T, kRound) * kRound;
     r.by_row = r.take(r.px * T * r.row_ld * 2);
@@ -372,7 +377,7 @@ BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
     r.ones = r.take(K * 4);
     r.rows = r.take(T * 4);
     r.classes = r.take(r.piece * 4);
-    const bool pieces = r.piece < V;
+    const bool pieces = r.piece < V && px > 0;
     if (pieces) r.sum = r.take(T * slices_ld(K) * 4);
     int64_t most = 0;
     const int64_t last = V - (V - 1) / r.piece * r.piece;
@@ -380,13 +385,28 @@ BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool d
         const int64_t n = i ? last : r.piece;
         const Shape x = product_shape(T, K, r.px * up(n, kRound));
         const Shape w = product_shape(n, K, r.pw * up(T, kRound));
-        const int64_t a = pieces ? T * slices_ld(K) * 4 * x.slices : slices_bytes(T, K, x);
+        const int64_t a = px == 0 ? 0
+                          : pieces ? T * slices_ld(K) * 4 * x.slices : slices_bytes(T, K, x);
         const int64_t b = slices_bytes(n, K, w);
         most = a > most ? a : most;
         most = b > most ? b : most;
     }
     r.slices = r.take(most);
     return r;
+}
+BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
+    const int px = dx_bf16 ? 1 : 2, pw = dw_bf16 ? 1 : 2;
+    return room_of(T, V, K, px, pw, piece_of(T, V, K, px));
+}
+// Without dx, in the room for both: no weights are laid out, and pieces are as large as fit
+// (dw alone of 128 x 151936 x 4096 fp32 968 us, in the pieces for both 1054).
+BackwardRoom weight_room(const BackwardRoom& both, int64_t T, int64_t V, int64_t K) {
+    for (int64_t pieces = up(V, piece_of(T, V)); pieces < up(V, both.piece);
+         pieces += 1 + pieces / 8) {
+        const BackwardRoom r = room_of(T, V, K, 0, both.pw, piece_size(V, pieces, 256));
+        if (r.bytes <= both.bytes) return r;
+    }
+    return both;
 }
 
 // sum <- sum and the slices of a piece, to dx, its rows scaled, after the last piece; 4
@@ -437,8 +457,9 @@ int launch_slopes(const Logits& z, const Slopes& to, int64_t K, void* stream) {
 }
 
 int backward(const Loss& l, const LossIn& in, Mat dx, Mat dw, void* ws, void* stream) {
-    const BackwardRoom r = backward_room(l.T, l.V, l.K, dx.bf16, dw.bf16);
+    const BackwardRoom both = backward_room(l.T, l.V, l.K, dx.bf16, dw.bf16);
     const bool x = dx.p != nullptr, w = dw.p != nullptr;
+    const BackwardRoom r = x ? both : weight_room(both, l.T, l.V, l.K);
     const int px = x ? r.px : 0, pw = w ? r.pw : 0;
     auto* turned_x = at<uint16_t>(ws, r.x);
     auto* turned_w = at<uint16_t>(ws, r.w);

@@ -109,44 +109,50 @@ ForwardRoom forward_room(int64_t T, int64_t V) {
     return r;
 }
 
-// Classes of a piece: 2^25 logits at most, so that their gradient takes 128 MB; and where dx's
-// product lays the weights out, as many as fit the same (64 x 151936 x 4096 in one piece, ten,
-// and twenty: fp32 1505, 1463, 1809 us, bf16 1302, 1414, 1747).
-int64_t piece_of(int64_t T, int64_t V, int64_t K) {
-    constexpr int64_t kRoom = (int64_t)128 << 20;
-    int64_t pieces = up(V, ((int64_t)1 << 25) / T / kClasses * kClasses);
-    for (;;) {
-        const int64_t n = piece_size(V, pieces, kClasses);
+// Classes of a piece: 2^25 logits at most, so that their gradient takes 128 MB.
+int64_t piece_of(int64_t T, int64_t V) {
+    return piece_size(V, up(V, ((int64_t)1 << 25) / T / kClasses * kClasses), kClasses);
+}
+// Classes of a piece that a product for dx takes: where it lays their weights out, 120 MB of them
+// at most, which the memory-side cache holds until they are multiplied (64 x 151936 x 4096 whole,
+// 1.2 GB, and so: fp32 1505 and 1465 us, bf16 1300 and 1395, whose terms are then held in three
+// numbers; 64 x 116960 x 3264 fp32 1048 and 968, bf16 857 and 901; in 60 MB 1709 at the first).
+int64_t part_of(int64_t T, int64_t piece, int64_t K) {
+    constexpr int64_t kRoom = (int64_t)120 << 20;
+    for (int64_t parts = 1;;) {
+        const int64_t n = piece_size(piece, parts, kClasses);
         const int64_t room = grad_input_workspace(T, n, K, false, false);
         if (room <= kRoom || n <= 1024) return n;
-        pieces = up(pieces * room, kRoom);
+        parts = up(parts * room, kRoom);
     }
 }
 
 struct BackwardRoom : Room {
-    int64_t piece, ld, ldk;  // classes of a piece; row strides of d and of dx' parts
-    int64_t d, scale, sum, part, product;
+    int64_t piece, part;  // classes of a piece, and of its product for dx
+    int64_t ld, ldk;      // row strides of d and of dx' sums
+    int64_t d, scale, sum, term, product;
 };
 BackwardRoom backward_room(int64_t T, int64_t V, int64_t K, bool dx_bf16, bool dw_bf16) {
     BackwardRoom r;
-    r.piece = piece_of(T, V, K);
+    r.piece = piece_of(T, V);
+    r.part = part_of(T, r.piece, K);
     r.ld = up(r.piece, 4) * 4;
     r.ldk = up(K, 4) * 4;
     r.d = r.take(T * r.ld * 4);
     r.scale = r.take(T * 4);
-    const bool pieces = r.piece < V;
-    if (pieces) {
+    const bool several = r.part < V;
+    if (several) {
         r.sum = r.take(T * r.ldk * 4);
-        r.part = r.take(T * r.ldk * 4);
+        r.term = r.take(T * r.ldk * 4);
     }
     int64_t most = 0;
-    const int64_t last = V - (V - 1) / r.piece * r.piece;
-    for (int i = 0; i < 2; ++i) {
-        const int64_t n = i ? last : r.piece;
-        const int64_t a = grad_input_workspace(T, n, K, false, dx_bf16 && !pieces);
-        const int64_t b = grad_weight_workspace(T, n, K, false, dw_bf16);
-        most = a > most ? a : most;
-        most = b > most ? b : most;
+    const auto need = [&](int64_t bytes) { most = bytes > most ? bytes : most; };
+    const int64_t pieces[] = {r.piece, V - (V - 1) / r.piece * r.piece};
+    for (const int64_t n : pieces) {
+        need(grad_weight_workspace(T, n, K, false, dw_bf16));
+        const int64_t whole = r.part < n ? r.part : n, last = n - (n - 1) / whole * whole;
+        need(grad_input_workspace(T, whole, K, false, dx_bf16 && !several));
+        need(grad_input_workspace(T, last, K, false, dx_bf16 && !several));
     }
     r.product = r.take(most);
     return r;
@@ -179,8 +185,7 @@ int64_t few_xent_bwd_workspace(int64_t T, int64_t V, int64_t K, bool dx_bf16, bo
 int launch_few_xent_bwd(const Loss& l, const LossIn& in, Mat dx, Mat dw, void* ws,
                         void* stream) {
     const BackwardRoom r = backward_room(l.T, l.V, l.K, dx.bf16, dw.bf16);
-    const bool whole = r.piece == l.V;
-    const Mat d{at<float>(ws, r.d), r.ld, false};
+    const Mat d{at<float>(ws, r.d), r.ld, false}, term{at<float>(ws, r.term), r.ldk, false};
     const Held x{l.x.q, l.x.ld, at<float>(ws, r.scale)};
     char* room = at<char>(ws, r.product);
     for (int64_t v = 0; v < l.V; v += r.piece) {
@@ -194,25 +199,28 @@ int launch_few_xent_bwd(const Loss& l, const LossIn& in, Mat dx, Mat dw, void* w
                           : launch_few_slopes(l, v, n, in, static_cast<float*>(d.p), r.ld, scale,
                                               stream);
         if (e) return e;
-        if (dx.p != nullptr) {
-            const Mat part{at<float>(ws, r.part), r.ldk, false};
-            if (int s = launch_grad_input(d, w, l.T, n, l.K, whole ? dx : part, room, stream))
+        for (int64_t i = 0; i < n && dx.p != nullptr; i += r.part) {
+            const int64_t m = n - i < r.part ? n - i : r.part;
+            const Mat some{static_cast<float*>(d.p) + i, r.ld, false};
+            const Held of{w.q + i * w.ld, w.ld, w.scale + i};
+            const bool first = v + i == 0, last = v + i + m == l.V;
+            if (int s = launch_grad_input(some, of, l.T, m, l.K, first && last ? dx : term, room,
+                                          stream))
                 return s;
-            if (!whole) {
-                Target out{};
-                out.c = dx.p;
-                out.ldc = dx.ld;
-                out.bf16 = dx.bf16;
-                if (int s = launch(xent_few_add_kernel, dim3((uint32_t)l.T), 256, stream,
-                                   at<float>(ws, r.sum), at<float>(ws, r.part), r.ldk, l.K,
-                                   (int)(v == 0), (int)(v + n == l.V), out))
-                    return s;
-            }
+            if (first && last) continue;
+            Target out{};
+            out.c = dx.p;
+            out.ldc = dx.ld;
+            out.bf16 = dx.bf16;
+            if (int s = launch(xent_few_add_kernel, dim3((uint32_t)l.T), 256, stream,
+                               at<float>(ws, r.sum), static_cast<const float*>(term.p), r.ldk,
+                               l.K, (int)first, (int)last, out))
+                return s;
         }
         if (dw.p != nullptr) {
-            const Mat part{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4), dw.ld,
+            const Mat rows{static_cast<char*>(dw.p) + v * dw.ld * (dw.bf16 ? 2 : 4), dw.ld,
                            dw.bf16};
-            if (int s = launch_grad_weight(d, x, l.T, n, l.K, part, room, stream)) return s;
+            if (int s = launch_grad_weight(d, x, l.T, n, l.K, rows, room, stream)) return s;
         }
     }
     return 0;

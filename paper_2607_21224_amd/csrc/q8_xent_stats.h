@@ -31,8 +31,8 @@ __device__ __forceinline__ Stats join(Stats a, Stats b) {
     return {top, a.sum * exp_of(a.top - p) + b.sum * exp_of(b.top - p)};
 }
 
-// lse, loss and miss from all of a row's logits; hit: its target's.  (lse - hit would lose of log(sum)
-// what lse has no bits for: all of a loss below 2^-24 |lse|.)
+// lse, loss and miss from all of a row's logits; hit: its target's.  (lse - hit would lose of
+// log(sum) what lse has no bits for: all of a loss below 2^-24 |lse|.)
 __device__ __forceinline__ void write_loss(Stats s, float hit, int64_t y, int64_t V,
                                            const LossOut& to, int64_t t) {
     const float more = logf(s.sum);
